@@ -248,6 +248,179 @@ int dynb_model_aggregate_update(dynb_model* m, const float* grads, const int32_t
 int dynb_lr_schedule(int64_t step, const int64_t* boundaries, const double* values,
                      int32_t n_values, double* lr);
 
+/* ---- operators of a residual block with routed experts ---------------------------
+ * What stands around the products of such a block when it is trained on ragged workers: the norm
+ * in front of them, the way of the tokens to their experts and back, the gradients of both, and the
+ * optimizer step.  They are independent of dynb_model.  `dtype` is DYNB_F32 or DYNB_BF16 and is the
+ * type of all rows (activations and their gradients); gains, weights, statistics and the gradients of
+ * parameters are fp32.  Arithmetic is fp32 with one rounding (nearest-even) per stored value.
+ * Rows are [rows][ld] with ld >= cols elements (0 in a description means cols); a row may start at any
+ * address that is a multiple of its element's size.  Results are the same from run to run. */
+
+enum { DYNB_OUT_SAME = 0, DYNB_OUT_FP8 = 1, DYNB_OUT_INT8 = 2 };
+
+/* Root-mean-square norm.  cols: 1 .. 2^20.  out: the type of y -- the rows' own, or 8 bits with fp32
+ * scales: DYNB_OUT_FP8 (e4m3, largest value 448) or DYNB_OUT_INT8 (-127 .. 127).  scale_block: columns
+ * that share a scale, a positive multiple of 32, or 0 for one scale per row (ignored for DYNB_OUT_SAME). */
+typedef struct {
+  int32_t dtype;
+  int32_t out;
+  int32_t cols;
+  int32_t scale_block;
+  float eps;
+  int64_t ld_x, ld_residual, ld_sum, ld_y; /* forward; ld_sum also in the backward pass */
+  int64_t ld_dy, ld_dsum, ld_dx;           /* backward */
+} dynb_rms_norm_desc;
+
+/* s = x + residual;  rstd = (mean_j s_j^2 + eps)^(-1/2);  y = s * rstd * gain, all from the unrounded s.
+ *   residual: rows, or NULL (s = x);  gain: fp32 [cols], or NULL (ones);  sum: receives s, or NULL;
+ *   y: rows of dtype or of 8 bits;  rstd: receives fp32 [rows], or NULL;
+ *   scales: fp32 [rows][ceil(cols / scale_block)], 8-bit outputs only: with a = max |y| of the block and
+ *   q = 448 or 127, scale = a / q and y is stored as round(y / scale) (nearest-even).  A block of zeros
+ *   has scale 0; a block with an infinity or NaN has scale NaN and stored zeros, so that what it stands
+ *   for is NaN.
+ * sum and a y of dtype may be x's or residual's memory (same pointer, same ld).  rows >= 0.
+ * DYNB_ERR_BADARG: null pointers, unknown type, cols, scale_block, eps (negative or not finite), an ld
+ * below cols, a pointer that is not a multiple of its element's size, rows beyond 2^31 - 1. */
+int dynb_rms_norm(const dynb_rms_norm_desc* d, int64_t rows, const void* x, const void* residual,
+                  const float* gain, void* sum, void* y, float* scales, float* rstd, void* stream);
+
+/* Scales per row of d's output (0 for DYNB_OUT_SAME; -1 on a bad description). */
+int32_t dynb_scale_blocks(const dynb_rms_norm_desc* d);
+
+/* out[r][c] = (value of y[r][c]) * (its scale), stored as out_dtype: what the 8-bit rows that
+ * dynb_rms_norm wrote with this description stand for.  out: rows of ld_out (0: cols) elements. */
+int dynb_dequantise(const dynb_rms_norm_desc* d, int64_t rows, const void* y, const float* scales,
+                    int32_t out_dtype, void* out, int64_t ld_out, void* stream);
+
+/* Gradients of dynb_rms_norm (16- or 32-bit y) from s as stored (or x where there was no residual) and
+ * rstd: with shat = s * rstd,
+ *   dx = rstd * (gain * dy - shat * mean_j(gain_j dy_j shat_j)) + dsum     (the residual's gradient too)
+ *   dgain[k] = sum over worker k's rows of dy * shat      (fp32; zeros for an idle worker)
+ *   dsum: gradient that reached the sum past the norm, or NULL;  dx: rows, may be dy's or dsum's memory
+ *   (same pointer, same ld);  dgain: row k at dgain + k * dgain_stride (>= cols), or NULL;  b: host [K],
+ *   rows = sum(b), worker k's rows as everywhere in this library.
+ * workspace: device, 16-byte aligned, dynb_rms_norm_backward_workspace_bytes(d, b, K) bytes (0 on bad
+ * arguments; may be 0, and workspace NULL, where nothing is needed). */
+size_t dynb_rms_norm_backward_workspace_bytes(const dynb_rms_norm_desc* d, const int32_t* b, int32_t K);
+int dynb_rms_norm_backward(const dynb_rms_norm_desc* d, const int32_t* b, int32_t K, const void* sum,
+                           const float* rstd, const float* gain, const void* dy, const void* dsum,
+                           void* dx, float* dgain, int64_t dgain_stride, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Tokens sorted by expert.  Choice (t, j), j < top_k, of token t has number t * top_k + j; choices =
+ * tokens * top_k must stay below 2^31.  1 <= top_k <= DYNB_MAX_TOP_K, 1 <= n_experts <= DYNB_MAX_EXPERTS.
+ * ld_tokens: rows of one per token (x, gradients of the output); ld_sorted: rows of one per choice;
+ * ld_addend, ld_out: dynb_route_combine. */
+#define DYNB_MAX_TOP_K 64
+#define DYNB_MAX_EXPERTS 1024
+typedef struct {
+  int32_t dtype;
+  int32_t cols;
+  int32_t top_k;
+  int32_t n_experts;
+  int64_t tokens;
+  int64_t ld_tokens, ld_sorted, ld_addend, ld_out;
+} dynb_route_desc;
+
+/* The plan of a sort by expert that keeps the order of the tokens inside each expert.  experts: device
+ * int32 [tokens][top_k]; a choice outside [0, n_experts) is dropped (a token may lose all of them).
+ *   offsets: int32 [n_experts + 1], expert e owns sorted rows [offsets[e], offsets[e + 1]);
+ *   slot:    int32 [tokens][top_k], sorted row of a choice, -1 if dropped;
+ *   source:  int32 [tokens * top_k], choice number of a sorted row, -1 from row offsets[n_experts] on.
+ * workspace: device, 16-byte aligned, dynb_route_workspace_bytes(d) bytes. */
+size_t dynb_route_workspace_bytes(const dynb_route_desc* d);
+int dynb_route_plan(const dynb_route_desc* d, const int32_t* experts, int32_t* offsets, int32_t* slot,
+                    int32_t* source, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Where each worker's rows begin inside each expert's: segments int32 [n_experts][K + 1]; rows
+ * [segments[e][k], segments[e][k + 1]) are expert e's from worker k (b: host [K], sum(b) = tokens).  The
+ * ragged segments of per-worker gradients of the experts' weights. */
+int dynb_route_segments(const dynb_route_desc* d, const int32_t* offsets, const int32_t* source,
+                        const int32_t* b, int32_t K, int32_t* segments, void* stream);
+
+/* sorted[slot[t][j]] = x[t]; sorted rows from offsets[n_experts] to tokens * top_k are zeros. */
+int dynb_route_gather(const dynb_route_desc* d, const void* x, const int32_t* offsets,
+                      const int32_t* slot, void* sorted, void* stream);
+
+/* out[t] = addend[t] + sum_j weights[t][j] * sorted[slot[t][j]] over the choices that were kept, j
+ * ascending; weights fp32 [tokens][top_k] or NULL (ones: then this is the gradient of
+ * dynb_route_gather); addend or NULL.  A dropped choice's weight and row are not read into the sum
+ * (nor is an infinity or NaN there).  out may be addend's memory (same pointer, same ld). */
+int dynb_route_combine(const dynb_route_desc* d, const void* sorted, const int32_t* slot,
+                       const float* weights, const void* addend, void* out, void* stream);
+
+/* Gradients of dynb_route_combine with weights: dsorted[slot[t][j]] = weights[t][j] * dout[t] (rows
+ * from offsets[n_experts] on: zeros) and dweights[t][j] = sum_c dout[t][c] * sorted[slot[t][j]][c]
+ * (0 for a dropped choice).  dsorted may be sorted's memory. */
+int dynb_route_combine_backward(const dynb_route_desc* d, const void* dout, const void* sorted,
+                                const int32_t* offsets, const int32_t* slot, const float* weights,
+                                void* dsorted, float* dweights, void* stream);
+
+/* AdamW over a list of tensors in one call: Adam with weight decay taken from the parameter itself,
+ *   g = sum_k (b_k / sum_i b_i) g_k;  m = beta1 m + (1-beta1) g;  v = beta2 v + (1-beta2) g^2;
+ *   p -= lr * (weight_decay * p + (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)).
+ *
+ * States in 8 bits (DYNB_STATE_8BIT) are uint8 [n] with one fp32 scale per 256 elements (the last block
+ * may be shorter): state1 holds m, state2 holds sqrt(v), whose range is half as many octaves as v's.  With
+ * a the largest magnitude of a block and t = magnitude * top / a, a code is the integer part of
+ * (bits(t + 2^-15) - bits(2^-15)) / 2^shift + u, bits() the fp32 encoding as an integer: equal steps in
+ * each of 16 octaves below the largest magnitude, exact zero.  m: sign in the highest bit, 8 steps an
+ * octave (top 1.875, shift 20); sqrt(v): 16 steps (top 1.9375, shift 19).  scale = a / top (0 for a below
+ * 2^-100: stored zeros; NaN where the block has an infinity or NaN: all of it reads as NaN then).  u in [0, 1) makes the
+ * rounding unbiased: rounded to nearest, a step of 1/16 would hold v where it is (it changes by 1 - beta2
+ * at most when it falls).  u is a function of the element's index i in its tensor, the tensor's position o
+ * in the list and `seed`, modulo 2^32: x = i * 0x9E3779B1 + o * 0x7F4A7C15 + seed; x = (x ^ x >> 16) *
+ * 0x6A09E667; x = (x ^ x >> 15) * 0xBB67AE85; x ^= x >> 16; u = (x >> 16) / 65536 for m,
+ * (x & 65535) / 65536 for sqrt(v).  Pass another seed each step.  The step itself uses the m and v that
+ * have not been rounded. */
+enum { DYNB_STATE_F32 = 0, DYNB_STATE_8BIT = 1 };
+#define DYNB_STATE_BLOCK 256
+typedef struct {
+  void* param;         /* device, the description's param_dtype [n] */
+  void* copy;          /* device bf16 [n] that receives the rounded fp32 parameter, or NULL */
+  void* state1;        /* device fp32 or uint8 [n], zero before the first step */
+  void* state2;
+  float* scale1;       /* device fp32 [ceil(n / 256)], zero before the first step; 8-bit states only */
+  float* scale2;
+  int64_t n;           /* >= 0 */
+  float weight_decay;  /* >= 0 */
+} dynb_adamw_tensor;
+typedef struct {
+  int32_t param_dtype; /* DYNB_F32, or DYNB_BF16: computed in fp32, rounded once (no copies then) */
+  int32_t grad_dtype;  /* DYNB_F32 or DYNB_BF16 */
+  int32_t state;       /* DYNB_STATE_* */
+  int32_t n_tensors;   /* >= 1 */
+  const dynb_adamw_tensor* tensors; /* host, copied by dynb_adamw_create */
+} dynb_adamw_desc;
+typedef struct {
+  float lr, eps;
+  double beta1, beta2; /* in [0, 1): rounded to fp32 after 1 - beta and the corrections are formed */
+  int64_t step;        /* >= 1 */
+  uint32_t seed;       /* 8-bit states */
+} dynb_adamw_rule;
+typedef struct dynb_adamw dynb_adamw;
+
+/* Host bookkeeping.  *out is released with dynb_adamw_destroy.  DYNB_ERR_BADARG: null or misaligned
+ * pointers, unknown types, copies of bf16 parameters, bad sizes or decay.  Tensors must not overlap. */
+int dynb_adamw_create(const dynb_adamw_desc* d, dynb_adamw** out);
+void dynb_adamw_destroy(dynb_adamw* h);
+
+/* The table of the tensors on the device: caller-owned memory, 16-byte aligned, written on `stream` by
+ * dynb_adamw_bind (which waits for it) and read by every step. */
+size_t dynb_adamw_workspace_bytes(const dynb_adamw* h);
+int dynb_adamw_bind(dynb_adamw* h, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One step.  grads: host [n_tensors], device pointers to worker 0's gradients of each tensor; worker k's
+ * are worker_stride elements further (K = 1: any).  sum(b) > 0.  A worker with b_k = 0 is not read. */
+int dynb_adamw_step(dynb_adamw* h, const void* const* grads, const int32_t* b, int32_t K,
+                    int64_t worker_stride, const dynb_adamw_rule* rule, void* stream);
+
+/* What 8-bit states stand for: m to out1[i] and v to out2[i] ([n] of out_dtype per tensor; host arrays of
+ * n_tensors device pointers).  DYNB_ERR_BADARG for fp32 states, which are in hand. */
+int dynb_adamw_read_states(dynb_adamw* h, void* const* out1, void* const* out2, int32_t out_dtype,
+                           void* stream);
+
 /* ---- controller (host only) ---------------------------------------------------- */
 
 /* One controller invocation (four-step summary of "Control stability"): from the

@@ -31,6 +31,11 @@ SYMBOLS = [
     "dynb_profile_enable", "dynb_profile_reset", "dynb_profile_collect",
     "dynb_profile_num_classes", "dynb_profile_name", "dynb_profile_get",
     "dynb_static_scratch_bytes", "dynb_forward_backward_static", "dynb_estimate_throughput",
+    "dynb_rms_norm", "dynb_scale_blocks", "dynb_dequantise", "dynb_rms_norm_backward_workspace_bytes",
+    "dynb_rms_norm_backward", "dynb_route_workspace_bytes", "dynb_route_plan", "dynb_route_segments",
+    "dynb_route_gather", "dynb_route_combine", "dynb_route_combine_backward", "dynb_adamw_create",
+    "dynb_adamw_destroy", "dynb_adamw_workspace_bytes", "dynb_adamw_bind", "dynb_adamw_step",
+    "dynb_adamw_read_states",
 ]
 
 
@@ -73,6 +78,41 @@ class ControllerConfig(C.Structure):
 
 class WorkerResources(C.Structure):
     _fields_ = [("cpu_cores", C.c_int32), ("half_precision_flops", C.c_double)]
+
+
+OUT_SAME, OUT_FP8, OUT_INT8 = 0, 1, 2
+STATE_F32, STATE_8BIT = 0, 1
+STATE_BLOCK = 256
+MAX_TOP_K, MAX_EXPERTS = 64, 1024
+
+
+class RmsNormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("out", C.c_int32), ("cols", C.c_int32),
+                ("scale_block", C.c_int32), ("eps", C.c_float), ("ld_x", C.c_int64),
+                ("ld_residual", C.c_int64), ("ld_sum", C.c_int64), ("ld_y", C.c_int64),
+                ("ld_dy", C.c_int64), ("ld_dsum", C.c_int64), ("ld_dx", C.c_int64)]
+
+
+class RouteDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("cols", C.c_int32), ("top_k", C.c_int32),
+                ("n_experts", C.c_int32), ("tokens", C.c_int64), ("ld_tokens", C.c_int64),
+                ("ld_sorted", C.c_int64), ("ld_addend", C.c_int64), ("ld_out", C.c_int64)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("copy", C.c_void_p), ("state1", C.c_void_p),
+                ("state2", C.c_void_p), ("scale1", C.c_void_p), ("scale2", C.c_void_p),
+                ("n", C.c_int64), ("weight_decay", C.c_float)]
+
+
+class AdamWDesc(C.Structure):
+    _fields_ = [("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("state", C.c_int32),
+                ("n_tensors", C.c_int32), ("tensors", C.POINTER(AdamWTensor))]
+
+
+class AdamWRule(C.Structure):
+    _fields_ = [("lr", C.c_float), ("eps", C.c_float), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("step", C.c_int64), ("seed", C.c_uint32)]
 
 
 _lib = None
@@ -131,6 +171,24 @@ def load():
         "dynb_estimate_throughput": (C.c_int, [C.POINTER(WorkerResources), i32, pf64]),
         "dynb_static_scratch_bytes": (C.c_size_t, []),
         "dynb_forward_backward_static": (C.c_int, [vp, vp, vp, vp, pi32, i32, vp, vp]),
+        "dynb_rms_norm": (C.c_int, [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "dynb_scale_blocks": (i32, [vp]),
+        "dynb_dequantise": (C.c_int, [vp, i64, vp, vp, i32, vp, i64, vp]),
+        "dynb_rms_norm_backward_workspace_bytes": (C.c_size_t, [vp, pi32, i32]),
+        "dynb_rms_norm_backward": (C.c_int, [vp, pi32, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp,
+                                             C.c_size_t, vp]),
+        "dynb_route_workspace_bytes": (C.c_size_t, [vp]),
+        "dynb_route_plan": (C.c_int, [vp, vp, vp, vp, vp, vp, C.c_size_t, vp]),
+        "dynb_route_segments": (C.c_int, [vp, vp, vp, pi32, i32, vp, vp]),
+        "dynb_route_gather": (C.c_int, [vp, vp, vp, vp, vp, vp]),
+        "dynb_route_combine": (C.c_int, [vp, vp, vp, vp, vp, vp, vp]),
+        "dynb_route_combine_backward": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "dynb_adamw_create": (C.c_int, [C.POINTER(AdamWDesc), C.POINTER(vp)]),
+        "dynb_adamw_destroy": (None, [vp]),
+        "dynb_adamw_workspace_bytes": (C.c_size_t, [vp]),
+        "dynb_adamw_bind": (C.c_int, [vp, vp, C.c_size_t, vp]),
+        "dynb_adamw_step": (C.c_int, [vp, C.POINTER(vp), pi32, i32, i64, C.POINTER(AdamWRule), vp]),
+        "dynb_adamw_read_states": (C.c_int, [vp, C.POINTER(vp), C.POINTER(vp), i32, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -318,6 +376,135 @@ def lr_schedule(step, boundaries, values):
     out = C.c_double()
     _check(load().dynb_lr_schedule(int(step), bd, _f64(values), n, C.byref(out)))
     return out.value
+
+
+# ---- operators of a residual block with routed experts
+
+_DTYPES = {"f32": F32, "bf16": BF16}
+_OUTS = {"same": OUT_SAME, "fp8": OUT_FP8, "int8": OUT_INT8}
+
+
+def rms_norm_desc(dtype, cols, out="same", scale_block=0, eps=1e-6, ld_x=0, ld_residual=0, ld_sum=0,
+                  ld_y=0, ld_dy=0, ld_dsum=0, ld_dx=0):
+    return RmsNormDesc(_DTYPES[dtype], _OUTS[out], int(cols), int(scale_block), float(eps), int(ld_x),
+                       int(ld_residual), int(ld_sum), int(ld_y), int(ld_dy), int(ld_dsum), int(ld_dx))
+
+
+def rms_norm(desc, rows, x, residual, gain, sum, y, scales=None, rstd=None, stream=None):
+    _check(load().dynb_rms_norm(C.addressof(desc), rows, _ptr(x), _ptr(residual), _ptr(gain), _ptr(sum),
+                                _ptr(y), _ptr(scales), _ptr(rstd), _stream(stream)))
+
+
+def scale_blocks(desc):
+    n = int(load().dynb_scale_blocks(C.addressof(desc)))
+    if n < 0:
+        _check(-1)
+    return n
+
+
+def dequantise(desc, rows, y, scales, out, out_dtype="f32", ld_out=0, stream=None):
+    _check(load().dynb_dequantise(C.addressof(desc), rows, _ptr(y), _ptr(scales), _DTYPES[out_dtype],
+                                  _ptr(out), ld_out, _stream(stream)))
+
+
+def rms_norm_backward_workspace_bytes(desc, b):
+    return int(load().dynb_rms_norm_backward_workspace_bytes(C.addressof(desc), _i32(b), len(b)))
+
+
+def rms_norm_backward(desc, b, sum, rstd, gain, dy, dsum, dx, dgain, dgain_stride, workspace,
+                      workspace_bytes, stream=None):
+    _check(load().dynb_rms_norm_backward(C.addressof(desc), _i32(b), len(b), _ptr(sum), _ptr(rstd),
+                                         _ptr(gain), _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dgain),
+                                         dgain_stride, _ptr(workspace), workspace_bytes,
+                                         _stream(stream)))
+
+
+def route_desc(dtype, cols, tokens, top_k, n_experts, ld_tokens=0, ld_sorted=0, ld_addend=0, ld_out=0):
+    return RouteDesc(_DTYPES[dtype], int(cols), int(top_k), int(n_experts), int(tokens), int(ld_tokens),
+                     int(ld_sorted), int(ld_addend), int(ld_out))
+
+
+def route_workspace_bytes(desc):
+    return int(load().dynb_route_workspace_bytes(C.addressof(desc)))
+
+
+def route_plan(desc, experts, offsets, slot, source, workspace, workspace_bytes, stream=None):
+    _check(load().dynb_route_plan(C.addressof(desc), _ptr(experts), _ptr(offsets), _ptr(slot),
+                                  _ptr(source), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def route_segments(desc, offsets, source, b, segments, stream=None):
+    _check(load().dynb_route_segments(C.addressof(desc), _ptr(offsets), _ptr(source), _i32(b), len(b),
+                                      _ptr(segments), _stream(stream)))
+
+
+def route_gather(desc, x, offsets, slot, sorted, stream=None):
+    _check(load().dynb_route_gather(C.addressof(desc), _ptr(x), _ptr(offsets), _ptr(slot), _ptr(sorted),
+                                    _stream(stream)))
+
+
+def route_combine(desc, sorted, slot, weights, addend, out, stream=None):
+    _check(load().dynb_route_combine(C.addressof(desc), _ptr(sorted), _ptr(slot), _ptr(weights),
+                                     _ptr(addend), _ptr(out), _stream(stream)))
+
+
+def route_combine_backward(desc, dout, sorted, offsets, slot, weights, dsorted, dweights, stream=None):
+    _check(load().dynb_route_combine_backward(C.addressof(desc), _ptr(dout), _ptr(sorted), _ptr(offsets),
+                                              _ptr(slot), _ptr(weights), _ptr(dsorted), _ptr(dweights),
+                                              _stream(stream)))
+
+
+def pointers(tensors):
+    """Device addresses as the array that AdamW.step and read_states take: built once where they stay."""
+    return (C.c_void_p * len(tensors))(*[_ptr(t) for t in tensors])
+
+
+class AdamW:
+    """Handle of a list of tensors and their optimizer states (dynb_adamw_*).  A tensor is a dict with
+    param, state1, state2, n, and where used copy, scale1, scale2, weight_decay."""
+
+    def __init__(self, tensors, param="f32", grad="f32", state="f32"):
+        self.n = len(tensors)
+        self._keep = [tensors]
+        self._h = None
+        rows = (AdamWTensor * max(1, self.n))(*[
+            AdamWTensor(_ptr(t["param"]), _ptr(t.get("copy")), _ptr(t["state1"]), _ptr(t["state2"]),
+                        _ptr(t.get("scale1")), _ptr(t.get("scale2")), int(t["n"]),
+                        float(t.get("weight_decay", 0.0))) for t in tensors])
+        d = AdamWDesc(_DTYPES[param], _DTYPES[grad], {"f32": STATE_F32, "8bit": STATE_8BIT}[state],
+                      self.n, rows)
+        h = C.c_void_p()
+        _check(load().dynb_adamw_create(C.byref(d), C.byref(h)))
+        self._h = h
+
+    def workspace_bytes(self):
+        return int(load().dynb_adamw_workspace_bytes(self._h))
+
+    def bind(self, workspace, workspace_bytes, stream=None):
+        self._keep[1:] = [workspace]
+        _check(load().dynb_adamw_bind(self._h, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+    def _array(self, tensors):
+        if not isinstance(tensors, C.Array):
+            tensors = pointers(tensors)
+        if len(tensors) != self.n:
+            raise ValueError("one device address per tensor")
+        return tensors
+
+    def step(self, grads, b=(1,), worker_stride=0, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1,
+             seed=0, stream=None):
+        rule = AdamWRule(lr, eps, beta1, beta2, step, seed)
+        _check(load().dynb_adamw_step(self._h, self._array(grads), _i32(b), len(b), worker_stride,
+                                      C.byref(rule), _stream(stream)))
+
+    def read_states(self, out1, out2, out_dtype="f32", stream=None):
+        _check(load().dynb_adamw_read_states(self._h, self._array(out1), self._array(out2),
+                                             _DTYPES[out_dtype], _stream(stream)))
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.dynb_adamw_destroy(self._h)
+            self._h = None
 
 
 def make_gains(kp=1.0, deadband=0.05, ewma_alpha=1.0, b_min=1, b_max=1 << 30, **_ignored):

@@ -24,6 +24,9 @@ struct Segs {
   int off[DYNB_MAX_WORKERS + 1];
 };
 
+// Prefix sums of the sizes b[K]; refuses null, K out of range, negative sizes and sums beyond 2^31 - 1 in `who`'s name.
+int segments_of(const int32_t* b, int32_t K, const char* who, Segs& s);
+
 struct Lambdas {
   int K;
   float w[DYNB_MAX_WORKERS];
@@ -57,6 +60,7 @@ enum KClass {
   KC_GEMM_WGRAD_64,      // bf16 weight gradients on the 64 x 64-tile kernel
   KC_GEMM_64,            // bf16 forward / input-gradient products on the 64 x 64-tile kernel
   KC_GEMM_128X64,        // ... on 128 x 64 tiles
+  KC_ROUTE,              // tokens sorted by expert and back
   KC_COUNT
 };
 

@@ -1,0 +1,426 @@
+// AdamW over a list of tensors: the weighted average of the workers' gradients, the step, the states in fp32 or in 8 bits
+// and the 16-bit copy of the parameters, in one pass over all of them.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "dynb_internal.h"
+#include "row_access.h"
+
+namespace dynb {
+namespace {
+
+constexpr int BLOCK = DYNB_STATE_BLOCK;   // elements that share a scale: a wave, 4 neighbouring ones per lane
+constexpr int CHUNK = 4096;               // elements of a workgroup
+
+struct Tensor {
+  void *param, *copy, *s1, *s2;
+  float *c1, *c2;
+  int64_t n;
+  float decay;
+  int32_t ordinal;
+};
+struct Chunk {
+  int32_t tensor, at;                     // elements [at * CHUNK, (at + 1) * CHUNK) of the tensor
+};
+constexpr int POINTERS = 256;             // tensors of a launch
+struct Pointers {
+  const void* p[POINTERS];
+};
+struct Pointers2 {
+  void *a[POINTERS / 2], *b[POINTERS / 2];
+};
+struct Workers {                          // those with rows
+  int n;
+  float w[DYNB_MAX_WORKERS];
+  uint8_t index[DYNB_MAX_WORKERS];
+};
+struct Rule {
+  float lr, eps, beta1, beta2, omb1, omb2, inv_c1, inv_c2;
+  uint32_t seed;
+};
+
+// ---- 4 neighbouring elements, of which the first n exist ------------------------------------------------------
+struct __attribute__((packed, aligned(4))) Float4 { float v[4]; };
+struct __attribute__((packed, aligned(2))) Half4 { u32x2 v; };
+struct __attribute__((packed, aligned(1))) Byte4 { uint32_t v; };
+
+__device__ inline void load4(const float* p, int n, float (&f)[4]) {
+  if (n >= 4) {
+    const Float4 q = *(const Float4*)p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = q.v[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = e < n ? p[e] : 0.f;
+  }
+}
+__device__ inline void load4(const bf16* p, int n, float (&f)[4]) {
+  if (n >= 4) {
+    const u32x2 q = ((const Half4*)p)->v;
+    f[0] = __uint_as_float(q[0] << 16);
+    f[1] = __uint_as_float(q[0] & 0xffff0000u);
+    f[2] = __uint_as_float(q[1] << 16);
+    f[3] = __uint_as_float(q[1] & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = e < n ? (float)p[e] : 0.f;
+  }
+}
+__device__ inline void store4(float* p, int n, const float (&f)[4]) {
+  if (n >= 4) {
+    Float4 q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q.v[e] = f[e];
+    *(Float4*)p = q;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) p[e] = f[e];
+  }
+}
+__device__ inline void store4(bf16* p, int n, const float (&f)[4]) {
+  if (n >= 4) {
+    ((Half4*)p)->v = u32x2{two_bf16(f[0], f[1]), two_bf16(f[2], f[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) p[e] = (bf16)f[e];
+  }
+}
+__device__ inline uint32_t load_codes(const uint8_t* p, int n) {
+  if (n >= 4) return ((const Byte4*)p)->v;
+  uint32_t q = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < n) q |= (uint32_t)p[e] << (8 * e);
+  return q;
+}
+__device__ inline void store_codes(uint8_t* p, int n, uint32_t q) {
+  if (n >= 4) {
+    ((Byte4*)p)->v = q;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < n) p[e] = (uint8_t)(q >> (8 * e));
+  }
+}
+
+// ---- 8-bit states ---------------------------------------------------------------------------------------------
+// A magnitude t in [0, top] is coded by the bits of the float t + 2^-15: 16 octaves of equal steps, linear below the
+// lowest, and encoding and decoding are an addition and a shift.  MAG magnitude bits: 7 (m, with a sign) or 8 (sqrt v).
+constexpr uint32_t LOW_BITS = 112u << 23;           // bits of 2^-15
+template <int MAG> struct Code {
+  static constexpr int SHIFT = MAG == 7 ? 20 : 19;
+  static constexpr float TOP = MAG == 7 ? 1.875f : 1.9375f;
+};
+template <int MAG> __device__ inline float decode(uint32_t code) {
+  return __uint_as_float((code << Code<MAG>::SHIFT) + LOW_BITS) - 0x1p-15f;
+}
+// u16: 16 random bits, 65536ths of a step
+template <int MAG> __device__ inline uint32_t encode(float magnitude, float inv, uint32_t u16) {
+  const uint32_t bits = __float_as_uint(magnitude * inv + 0x1p-15f) - LOW_BITS + (u16 << (Code<MAG>::SHIFT - 16));
+  return inv > 0.f ? min(bits >> Code<MAG>::SHIFT, (1u << MAG) - 1) : 0u;
+}
+__device__ inline Scale state_scale(uint32_t amax_bits, float top) {
+  if (amax_bits < (27u << 23)) return {0.f, 0.f};   // below 2^-100
+  return scale_of(amax_bits, top);
+}
+__device__ inline uint32_t random_bits(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x6A09E667u;
+  x = (x ^ (x >> 15)) * 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+
+template <typename P, typename G, bool EIGHT>
+__global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const Chunk* chunks, Pointers grads,
+                                                    int first_tensor, int64_t worker_stride, Workers workers,
+                                                    Rule rule) {
+  const Chunk chunk = chunks[blockIdx.x];
+  const Tensor t = tensors[chunk.tensor];
+  const G* const grad = (const G*)grads.p[chunk.tensor - first_tensor];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float keep = 1.f - rule.lr * t.decay;
+  for (int b = wave; b < CHUNK / BLOCK; b += 4) {
+    const int64_t begin = (int64_t)chunk.at * CHUNK + b * BLOCK;
+    if (begin >= t.n) break;
+    const int64_t i = begin + 4 * lane, left = t.n - i;
+    const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
+    float p[4], m[4], v[4], g[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < workers.n; ++k) {
+      float d[4];
+      load4(grad + workers.index[k] * worker_stride + i, n, d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] += workers.w[k] * d[e];
+    }
+    load4((const P*)t.param + i, n, p);
+    if (EIGHT) {
+      const float s1 = t.c1[begin / BLOCK], s2 = t.c2[begin / BLOCK];
+      const uint32_t q1 = load_codes((const uint8_t*)t.s1 + i, n), q2 = load_codes((const uint8_t*)t.s2 + i, n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a = decode<7>(q1 >> (8 * e) & 0x7f) * s1, r = decode<8>(q2 >> (8 * e) & 0xff) * s2;
+        m[e] = q1 >> (8 * e) & 0x80 ? -a : a;
+        v[e] = r * r;
+      }
+    } else {
+      load4((const float*)t.s1 + i, n, m);
+      load4((const float*)t.s2 + i, n, v);
+    }
+    float root[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      m[e] = rule.beta1 * m[e] + rule.omb1 * g[e];
+      v[e] = rule.beta2 * v[e] + rule.omb2 * g[e] * g[e];
+      root[e] = sqrtf(v[e]);
+      p[e] = p[e] * keep - rule.lr * (m[e] * rule.inv_c1) / (root[e] * rule.inv_c2 + rule.eps);
+    }
+    store4((P*)t.param + i, n, p);
+    if (t.copy) store4((bf16*)t.copy + i, n, p);
+    if (!EIGHT) {
+      store4((float*)t.s1 + i, n, m);
+      store4((float*)t.s2 + i, n, v);
+      continue;
+    }
+    uint32_t a1 = 0, a2 = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= n) m[e] = root[e] = 0.f;
+      a1 = max(a1, __float_as_uint(m[e]) & 0x7fffffffu);
+      a2 = max(a2, __float_as_uint(root[e]) & 0x7fffffffu);
+    }
+    const Scale s1 = state_scale(wave_max(a1), Code<7>::TOP), s2 = state_scale(wave_max(a2), Code<8>::TOP);
+    uint32_t q1 = 0, q2 = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t u = random_bits((uint32_t)(i + e) * 0x9E3779B1u + t.ordinal * 0x7F4A7C15u + rule.seed);
+      q1 |= (encode<7>(fabsf(m[e]), s1.inv, u >> 16) | (m[e] < 0.f ? 0x80u : 0u)) << (8 * e);
+      q2 |= encode<8>(root[e], s2.inv, u & 0xffffu) << (8 * e);
+    }
+    store_codes((uint8_t*)t.s1 + i, n, q1);
+    store_codes((uint8_t*)t.s2 + i, n, q2);
+    if (lane == 0) {
+      t.c1[begin / BLOCK] = s1.scale;
+      t.c2[begin / BLOCK] = s2.scale;
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void read_states_kernel(const Tensor* tensors, const Chunk* chunks, Pointers2 out,
+                                                          int first_tensor) {
+  const Chunk chunk = chunks[blockIdx.x];
+  const Tensor t = tensors[chunk.tensor];
+  T *const to1 = (T*)out.a[chunk.tensor - first_tensor], *const to2 = (T*)out.b[chunk.tensor - first_tensor];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = wave; b < CHUNK / BLOCK; b += 4) {
+    const int64_t begin = (int64_t)chunk.at * CHUNK + b * BLOCK;
+    if (begin >= t.n) break;
+    const int64_t i = begin + 4 * lane, left = t.n - i;
+    const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
+    const float s1 = t.c1[begin / BLOCK], s2 = t.c2[begin / BLOCK];
+    const uint32_t q1 = load_codes((const uint8_t*)t.s1 + i, n), q2 = load_codes((const uint8_t*)t.s2 + i, n);
+    float m[4], v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float a = decode<7>(q1 >> (8 * e) & 0x7f) * s1, r = decode<8>(q2 >> (8 * e) & 0xff) * s2;
+      m[e] = q1 >> (8 * e) & 0x80 ? -a : a;
+      v[e] = r * r;
+    }
+    store4(to1 + i, n, m);
+    store4(to2 + i, n, v);
+  }
+}
+
+}  // namespace
+}  // namespace dynb
+
+using namespace dynb;
+
+struct dynb_adamw {
+  int32_t param_dtype, grad_dtype, state;
+  std::vector<Tensor> tensors;
+  std::vector<Chunk> chunks;
+  std::vector<int64_t> first_chunk;       // [n_tensors + 1]
+  const Tensor* d_tensors = nullptr;      // in the bound workspace
+  const Chunk* d_chunks = nullptr;
+};
+
+namespace {
+bool off(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }
+size_t tensor_bytes(const dynb_adamw* h) { return (size_t)round_up((int64_t)(h->tensors.size() * sizeof(Tensor)), 16); }
+
+template <typename P, typename G>
+void launch_step(const dynb_adamw* h, const Pointers& g, int first, int64_t blocks, int64_t stride, const Workers& w,
+                 const Rule& r, hipStream_t st) {
+  const Chunk* c = h->d_chunks + h->first_chunk[first];
+  if (h->state == DYNB_STATE_8BIT)
+    hipLaunchKernelGGL((adamw_kernel<P, G, true>), dim3((unsigned)blocks), dim3(256), 0, st, h->d_tensors, c, g, first,
+                       stride, w, r);
+  else
+    hipLaunchKernelGGL((adamw_kernel<P, G, false>), dim3((unsigned)blocks), dim3(256), 0, st, h->d_tensors, c, g, first,
+                       stride, w, r);
+}
+}  // namespace
+
+extern "C" int dynb_adamw_create(const dynb_adamw_desc* d, dynb_adamw** out) {
+  if (!d || !out || !d->tensors) return fail(DYNB_ERR_BADARG, "adamw: null pointer");
+  *out = nullptr;
+  if ((d->param_dtype != DYNB_F32 && d->param_dtype != DYNB_BF16) ||
+      (d->grad_dtype != DYNB_F32 && d->grad_dtype != DYNB_BF16))
+    return fail(DYNB_ERR_BADARG, "adamw: unknown dtype");
+  if (d->state != DYNB_STATE_F32 && d->state != DYNB_STATE_8BIT) return fail(DYNB_ERR_BADARG, "adamw: unknown state type");
+  if (d->n_tensors < 1) return fail(DYNB_ERR_BADARG, "adamw: at least one tensor");
+  const bool eight = d->state == DYNB_STATE_8BIT;
+  int64_t chunks = 0;
+  for (int i = 0; i < d->n_tensors; ++i) {
+    const dynb_adamw_tensor& t = d->tensors[i];
+    if (t.n < 0 || t.n > ((int64_t)1 << 40)) return fail(DYNB_ERR_BADARG, "adamw: tensor %d: size out of range", i);
+    if (!(t.weight_decay >= 0.f) || !std::isfinite(t.weight_decay))
+      return fail(DYNB_ERR_BADARG, "adamw: tensor %d: weight decay must be finite and not negative", i);
+    if (t.copy && d->param_dtype == DYNB_BF16)
+      return fail(DYNB_ERR_BADARG, "adamw: tensor %d: a copy of a bf16 parameter", i);
+    if (t.n > 0 && (!t.param || !t.state1 || !t.state2 || (eight && (!t.scale1 || !t.scale2))))
+      return fail(DYNB_ERR_BADARG, "adamw: tensor %d: null pointer", i);
+    if (off(t.param, d->param_dtype == DYNB_F32 ? 4 : 2) || off(t.copy, 2) ||
+        (!eight && (off(t.state1, 4) || off(t.state2, 4))) || (eight && (off(t.scale1, 4) || off(t.scale2, 4))))
+      return fail(DYNB_ERR_BADARG, "adamw: tensor %d: a pointer is not a multiple of its element's size", i);
+    chunks += (t.n + CHUNK - 1) / CHUNK;
+  }
+  if (chunks > (1 << 24)) return fail(DYNB_ERR_UNSUPPORTED, "adamw: more than 2^36 elements");
+  dynb_adamw* h = new (std::nothrow) dynb_adamw;
+  if (!h) return fail(DYNB_ERR_STATE, "adamw: out of host memory");
+  try {
+    h->param_dtype = d->param_dtype;
+    h->grad_dtype = d->grad_dtype;
+    h->state = d->state;
+    h->chunks.reserve((size_t)chunks);
+    for (int i = 0; i < d->n_tensors; ++i) {
+      const dynb_adamw_tensor& t = d->tensors[i];
+      h->tensors.push_back({t.param, t.copy, t.state1, t.state2, t.scale1, t.scale2, t.n, t.weight_decay, i});
+      h->first_chunk.push_back((int64_t)h->chunks.size());
+      for (int64_t c = 0; c * CHUNK < t.n; ++c) h->chunks.push_back({i, (int32_t)c});
+    }
+    h->first_chunk.push_back((int64_t)h->chunks.size());
+  } catch (...) {
+    delete h;
+    return fail(DYNB_ERR_STATE, "adamw: out of host memory");
+  }
+  *out = h;
+  return DYNB_OK;
+}
+
+extern "C" void dynb_adamw_destroy(dynb_adamw* h) { delete h; }
+
+extern "C" size_t dynb_adamw_workspace_bytes(const dynb_adamw* h) {
+  return h ? tensor_bytes(h) + (h->chunks.empty() ? 1 : h->chunks.size()) * sizeof(Chunk) : 0;
+}
+
+extern "C" int dynb_adamw_bind(dynb_adamw* h, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!h || !workspace) return fail(DYNB_ERR_BADARG, "adamw_bind: null pointer");
+  if (off(workspace, 16)) return fail(DYNB_ERR_BADARG, "adamw_bind: workspace must be 16-byte aligned");
+  if (workspace_bytes < dynb_adamw_workspace_bytes(h)) return fail(DYNB_ERR_BADARG, "adamw_bind: workspace too small");
+  char* w = (char*)workspace;
+  hipStream_t st = (hipStream_t)stream;
+  h->d_tensors = nullptr;
+  hipError_t e = hipMemcpyAsync(w, h->tensors.data(), h->tensors.size() * sizeof(Tensor), hipMemcpyHostToDevice, st);
+  if (e == hipSuccess && !h->chunks.empty())
+    e = hipMemcpyAsync(w + tensor_bytes(h), h->chunks.data(), h->chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice, st);
+  if (e == hipSuccess) e = hipStreamSynchronize(st);
+  if (e != hipSuccess) return fail(DYNB_ERR_HIP, "adamw_bind: %s", hipGetErrorString(e));
+  h->d_tensors = (const Tensor*)w;
+  h->d_chunks = (const Chunk*)(w + tensor_bytes(h));
+  return DYNB_OK;
+}
+
+extern "C" int dynb_adamw_step(dynb_adamw* h, const void* const* grads, const int32_t* b, int32_t K,
+                               int64_t worker_stride, const dynb_adamw_rule* rule, void* stream) {
+  if (!h || !grads || !rule) return fail(DYNB_ERR_BADARG, "adamw_step: null pointer");
+  Segs seg;
+  if (int rc = segments_of(b, K, "adamw_step", seg)) return rc;
+  if (seg.off[K] <= 0) return fail(DYNB_ERR_BADARG, "adamw_step: sum(b) must be positive");
+  if (K > 1 && worker_stride < 0) return fail(DYNB_ERR_BADARG, "adamw_step: negative worker_stride");
+  if (!(rule->beta1 >= 0.0 && rule->beta1 < 1.0 && rule->beta2 >= 0.0 && rule->beta2 < 1.0))
+    return fail(DYNB_ERR_BADARG, "adamw_step: betas must lie in [0, 1)");
+  if (rule->step < 1) return fail(DYNB_ERR_BADARG, "adamw_step: steps count from 1");
+  if (!std::isfinite(rule->lr) || !(rule->eps >= 0.f) || !std::isfinite(rule->eps))
+    return fail(DYNB_ERR_BADARG, "adamw_step: lr and eps must be finite, eps not negative");
+  const int n = (int)h->tensors.size();
+  for (int i = 0; i < n; ++i)
+    if (h->tensors[i].n > 0 && (!grads[i] || off(grads[i], h->grad_dtype == DYNB_F32 ? 4 : 2)))
+      return fail(DYNB_ERR_BADARG, "adamw_step: gradient %d is null or not a multiple of its element's size", i);
+  if (!h->d_tensors) return fail(DYNB_ERR_STATE, "adamw_step: not bound");
+  Workers w = {};
+  for (int k = 0; k < K; ++k)
+    if (b[k] > 0) {
+      w.w[w.n] = (float)((double)b[k] / (double)seg.off[K]);
+      w.index[w.n++] = (uint8_t)k;
+    }
+  Rule r;
+  r.lr = rule->lr;
+  r.eps = rule->eps;
+  r.beta1 = (float)rule->beta1;
+  r.beta2 = (float)rule->beta2;
+  r.omb1 = (float)(1.0 - rule->beta1);
+  r.omb2 = (float)(1.0 - rule->beta2);
+  r.inv_c1 = (float)(1.0 / (1.0 - std::pow(rule->beta1, (double)rule->step)));
+  r.inv_c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(rule->beta2, (double)rule->step)));   // (of the root)
+  r.seed = rule->seed;
+  double elements = 0;
+  for (const Tensor& t : h->tensors) elements += (double)t.n;
+  const double gs = h->grad_dtype == DYNB_F32 ? 4 : 2, ps = h->param_dtype == DYNB_F32 ? 4 : 2;
+  Timed timed(KC_UPDATE, stream, elements * (2.0 * w.n + 14.0),
+              elements * (2 * ps + gs * w.n + (h->state == DYNB_STATE_F32 ? 16 : 4)));
+  for (int first = 0; first < n; first += POINTERS) {
+    const int last = first + POINTERS < n ? first + POINTERS : n;
+    const int64_t blocks = h->first_chunk[last] - h->first_chunk[first];
+    if (blocks == 0) continue;
+    Pointers g = {};
+    for (int i = first; i < last; ++i) g.p[i - first] = grads[i];
+    const hipStream_t st = (hipStream_t)stream;
+    if (h->param_dtype == DYNB_F32 && h->grad_dtype == DYNB_F32) launch_step<float, float>(h, g, first, blocks, worker_stride, w, r, st);
+    else if (h->param_dtype == DYNB_F32) launch_step<float, bf16>(h, g, first, blocks, worker_stride, w, r, st);
+    else if (h->grad_dtype == DYNB_F32) launch_step<bf16, float>(h, g, first, blocks, worker_stride, w, r, st);
+    else launch_step<bf16, bf16>(h, g, first, blocks, worker_stride, w, r, st);
+    if (hipGetLastError() != hipSuccess) return fail(DYNB_ERR_HIP, "adamw_step launch failed");
+  }
+  return DYNB_OK;
+}
+
+extern "C" int dynb_adamw_read_states(dynb_adamw* h, void* const* out1, void* const* out2, int32_t out_dtype,
+                                      void* stream) {
+  if (!h || !out1 || !out2) return fail(DYNB_ERR_BADARG, "adamw_read_states: null pointer");
+  if (h->state != DYNB_STATE_8BIT) return fail(DYNB_ERR_BADARG, "adamw_read_states: the states are fp32");
+  if (out_dtype != DYNB_F32 && out_dtype != DYNB_BF16) return fail(DYNB_ERR_BADARG, "adamw_read_states: unknown dtype");
+  const int n = (int)h->tensors.size();
+  const size_t size = out_dtype == DYNB_F32 ? 4 : 2;
+  double elements = 0;
+  for (int i = 0; i < n; ++i) {
+    elements += (double)h->tensors[i].n;
+    if (h->tensors[i].n > 0 && (!out1[i] || !out2[i] || off(out1[i], size) || off(out2[i], size)))
+      return fail(DYNB_ERR_BADARG, "adamw_read_states: output %d is null or not a multiple of its element's size", i);
+  }
+  if (!h->d_tensors) return fail(DYNB_ERR_STATE, "adamw_read_states: not bound");
+  Timed timed(KC_UPDATE, stream, 0.0, elements * (2.0 + 2 * size));
+  for (int first = 0; first < n; first += POINTERS / 2) {
+    const int last = first + POINTERS / 2 < n ? first + POINTERS / 2 : n;
+    const int64_t blocks = h->first_chunk[last] - h->first_chunk[first];
+    if (blocks == 0) continue;
+    Pointers2 o = {};
+    for (int i = first; i < last; ++i) {
+      o.a[i - first] = out1[i];
+      o.b[i - first] = out2[i];
+    }
+    const Chunk* c = h->d_chunks + h->first_chunk[first];
+    if (out_dtype == DYNB_F32)
+      hipLaunchKernelGGL(read_states_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream,
+                         h->d_tensors, c, o, first);
+    else
+      hipLaunchKernelGGL(read_states_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream,
+                         h->d_tensors, c, o, first);
+    if (hipGetLastError() != hipSuccess) return fail(DYNB_ERR_HIP, "adamw_read_states launch failed");
+  }
+  return DYNB_OK;
+}

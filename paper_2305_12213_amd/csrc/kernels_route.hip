@@ -1,0 +1,329 @@
+// Tokens sorted by expert and back: the plan (a stable counting sort), the rows' way there, their weighted sum on the
+// way back, and the gradients.
+#include <hip/hip_runtime.h>
+
+#include "dynb_internal.h"
+#include "row_access.h"
+
+namespace dynb {
+namespace {
+
+// ---- the plan -----------------------------------------------------------------------------------------------
+// One workgroup of 16 waves, each with a stretch of the choices: the waves count their stretches, the counts are
+// summed in the order (expert, wave), and each wave goes over its stretch again and hands out the places in order.
+constexpr int PLAN_WAVES = 16;
+
+// Lanes of the wave with the same key as this one (all lanes take part; keys below 2^bits).
+__device__ inline uint64_t same_key(int key, int bits) {
+  uint64_t same = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot((key >> b) & 1);
+    same &= ((key >> b) & 1) ? set : ~set;
+  }
+  return same;
+}
+
+// LDS written by some lanes of a wave and read by others: in order, with nothing moved across.
+__device__ inline void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__global__ __launch_bounds__(PLAN_WAVES * 64) void plan_kernel(const int32_t* experts, int n, int n_experts,
+                                                               int bits, int32_t* offsets, int32_t* slot,
+                                                               int32_t* source) {
+  __shared__ int count[PLAN_WAVES * DYNB_MAX_EXPERTS];
+  __shared__ int first[DYNB_MAX_EXPERTS + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int* mine = count + wave * n_experts;
+  for (int i = threadIdx.x; i < PLAN_WAVES * n_experts; i += PLAN_WAVES * 64) count[i] = 0;
+  __syncthreads();
+  const int per = ((n + PLAN_WAVES - 1) / PLAN_WAVES + 63) / 64 * 64;
+  const int64_t begin = (int64_t)wave * per, end = begin + per < n ? begin + per : n;
+  for (int64_t i = begin + lane; i < end; i += 64) {
+    const int e = experts[i];
+    if ((uint32_t)e < (uint32_t)n_experts) atomicAdd(&mine[e], 1);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int at = 0;
+    for (int e = 0; e < n_experts; ++e) {
+      first[e] = at;
+      for (int w = 0; w < PLAN_WAVES; ++w) {
+        const int c = count[w * n_experts + e];
+        count[w * n_experts + e] = at;
+        at += c;
+      }
+    }
+    first[n_experts] = at;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e <= n_experts; e += PLAN_WAVES * 64) offsets[e] = first[e];
+  for (int64_t i0 = begin; i0 < end; i0 += 64) {
+    const int64_t i = i0 + lane;
+    int e = i < end ? experts[i] : -1;
+    const bool kept = (uint32_t)e < (uint32_t)n_experts;
+    if (!kept) e = n_experts;
+    const uint64_t same = same_key(e, bits);
+    const int before = __popcll(same & ((1ull << lane) - 1));
+    int place = -1;
+    if (kept) place = mine[e] + before;
+    wave_fence();                        // every lane has read its expert's place before the first of them moves it on
+    if (kept && before == 0) mine[e] += __popcll(same);
+    wave_fence();
+    if (i < end) slot[i] = place;
+    if (kept) source[place] = (int)i;
+  }
+  for (int64_t r = first[n_experts] + (int64_t)threadIdx.x; r < n; r += PLAN_WAVES * 64) source[r] = -1;
+}
+
+// segments[e][k]: the first of expert e's rows whose choice is at or behind worker k's first (choices ascend there).
+__global__ __launch_bounds__(256) void segments_kernel(const int32_t* offsets, const int32_t* source, Segs seg,
+                                                       int top_k, int n_experts, int32_t* segments) {
+  const int i = blockIdx.x * 256 + threadIdx.x, e = i / (seg.K + 1), k = i - e * (seg.K + 1);
+  if (e >= n_experts) return;
+  int lo = offsets[e], hi = offsets[e + 1];
+  if (k == seg.K) lo = hi;
+  const int from = k < seg.K ? seg.off[k] * top_k : 0;
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (source[mid] < from) lo = mid + 1;
+    else hi = mid;
+  }
+  segments[i] = lo;
+}
+
+// ---- rows ---------------------------------------------------------------------------------------------------
+struct RowArgs {
+  const void *in, *addend;        // rows of tokens or choices, and the combination's addend
+  void* out;
+  const int32_t *slot, *offsets;
+  const float* weights;
+  float* dweights;
+  const void* sorted;             // backward: the experts' outputs
+  int64_t ld_in, ld_out, ld_addend, ld_sorted;
+  int64_t tokens, choices;
+  int cols, granules, top_k, n_experts;
+};
+
+// Sorted rows that no choice has: zeros.
+template <typename T> __device__ void clear_rows(const RowArgs& p, int64_t block, int64_t blocks) {
+  const float zeros[GRANULE] = {};
+  for (int64_t r = p.offsets[p.n_experts] + block; r < p.choices; r += blocks)
+    for (int c = threadIdx.x * GRANULE; c < p.cols; c += 256 * GRANULE)
+      store_part((T*)p.out + r * p.ld_out + c, p.cols - c, zeros);
+}
+
+// A thread takes a granule of a token: one load, top_k stores.
+template <typename T> __global__ __launch_bounds__(256) void gather_kernel(RowArgs p) {
+  const int64_t total = p.tokens * p.granules;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / p.granules;
+    const int c = (int)(i - t * p.granules) * GRANULE;
+    float v[GRANULE];
+    load_part((const T*)p.in + t * p.ld_in + c, p.cols - c, v);
+    for (int j = 0; j < p.top_k; ++j) {
+      const int s = p.slot[t * p.top_k + j];
+      if (s >= 0) store_part((T*)p.out + (int64_t)s * p.ld_out + c, p.cols - c, v);
+    }
+  }
+  clear_rows<T>(p, blockIdx.x, gridDim.x);
+}
+
+// A thread takes a granule of a token: the sum over its choices, j ascending, in fp32.
+template <typename T> __global__ __launch_bounds__(256) void combine_kernel(RowArgs p) {
+  const int64_t total = p.tokens * p.granules;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / p.granules;
+    const int c = (int)(i - t * p.granules) * GRANULE;
+    float a[GRANULE] = {};
+    if (p.addend) load_part((const T*)p.addend + t * p.ld_addend + c, p.cols - c, a);
+    for (int j = 0; j < p.top_k; ++j) {
+      const int s = p.slot[t * p.top_k + j];
+      if (s < 0) continue;
+      const float w = p.weights ? p.weights[t * p.top_k + j] : 1.f;
+      float v[GRANULE];
+      load_part((const T*)p.in + (int64_t)s * p.ld_in + c, p.cols - c, v);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) a[e] += w * v[e];
+    }
+    store_part((T*)p.out + t * p.ld_out + c, p.cols - c, a);
+  }
+}
+
+// A wave takes a choice: its row of dsorted, and the product of the two rows.
+template <typename T> __global__ __launch_bounds__(256) void combine_grad_kernel(RowArgs p) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < p.choices; i += (int64_t)gridDim.x * 4) {
+    const int64_t t = i / p.top_k, s = p.slot[i];
+    float dot = 0.f;
+    if (s >= 0) {
+      const float w = p.weights[i];
+      for (int c = lane * GRANULE; c < p.cols; c += 64 * GRANULE) {
+        float g[GRANULE], y[GRANULE];
+        load_part((const T*)p.in + t * p.ld_in + c, p.cols - c, g);
+        load_part((const T*)p.sorted + s * p.ld_sorted + c, p.cols - c, y);
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) {
+          dot += g[e] * y[e];
+          g[e] *= w;
+        }
+        store_part((T*)p.out + s * p.ld_out + c, p.cols - c, g);
+      }
+      dot = wave_sum(dot);
+    }
+    if (lane == 0) p.dweights[i] = dot;
+  }
+  clear_rows<T>(p, blockIdx.x, gridDim.x);
+}
+
+int grid_for(int64_t threads) {
+  const int64_t blocks = (threads + 255) / 256;
+  return (int)(blocks < 1 ? 1 : blocks < (1 << 20) ? blocks : 1 << 20);
+}
+
+bool off_by(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }
+
+int describe(const dynb_route_desc* d, const char* who) {
+  if (!d) return fail(DYNB_ERR_BADARG, "%s: null pointer", who);
+  if (d->dtype != DYNB_F32 && d->dtype != DYNB_BF16) return fail(DYNB_ERR_BADARG, "%s: unknown dtype", who);
+  if (d->cols < 1 || d->cols > (1 << 20)) return fail(DYNB_ERR_BADARG, "%s: cols out of range", who);
+  if (d->top_k < 1 || d->top_k > DYNB_MAX_TOP_K) return fail(DYNB_ERR_BADARG, "%s: top_k out of range", who);
+  if (d->n_experts < 1 || d->n_experts > DYNB_MAX_EXPERTS) return fail(DYNB_ERR_BADARG, "%s: n_experts out of range", who);
+  if (d->tokens < 0 || d->tokens > INT32_MAX / d->top_k) return fail(DYNB_ERR_BADARG, "%s: tokens out of range", who);
+  for (int64_t ld : {d->ld_tokens, d->ld_sorted, d->ld_addend, d->ld_out})
+    if (ld != 0 && ld < d->cols) return fail(DYNB_ERR_BADARG, "%s: a row pitch is below cols", who);
+  return DYNB_OK;
+}
+
+RowArgs row_args(const dynb_route_desc* d) {
+  RowArgs a = {};
+  a.tokens = d->tokens;
+  a.choices = d->tokens * d->top_k;
+  a.cols = d->cols;
+  a.granules = (d->cols + GRANULE - 1) / GRANULE;
+  a.top_k = d->top_k;
+  a.n_experts = d->n_experts;
+  return a;
+}
+int64_t pitch(const dynb_route_desc* d, int64_t ld) { return ld ? ld : d->cols; }
+int launched(const char* what) {
+  return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "%s launch failed", what);
+}
+
+}  // namespace
+}  // namespace dynb
+
+using namespace dynb;
+
+extern "C" size_t dynb_route_workspace_bytes(const dynb_route_desc* d) {
+  if (describe(d, "route_workspace_bytes")) return 0;
+  return 0;
+}
+
+extern "C" int dynb_route_plan(const dynb_route_desc* d, const int32_t* experts, int32_t* offsets, int32_t* slot,
+                               int32_t* source, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = describe(d, "route_plan")) return rc;
+  const int n = (int)(d->tokens * d->top_k);
+  if (!offsets || (n > 0 && (!experts || !slot || !source))) return fail(DYNB_ERR_BADARG, "route_plan: null pointer");
+  if (off_by(experts, 4) || off_by(offsets, 4) || off_by(slot, 4) || off_by(source, 4))
+    return fail(DYNB_ERR_BADARG, "route_plan: a pointer is not a multiple of its element's size");
+  (void)workspace;
+  (void)workspace_bytes;
+  int bits = 0;
+  while ((1 << bits) <= d->n_experts) ++bits;      // (keys 0 .. n_experts: the last one stands for a dropped choice)
+  Timed t(KC_ROUTE, stream, 0.0, 12.0 * n);
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_WAVES * 64), 0, (hipStream_t)stream, experts, n, d->n_experts,
+                     bits, offsets, slot, source);
+  return launched("route_plan");
+}
+
+extern "C" int dynb_route_segments(const dynb_route_desc* d, const int32_t* offsets, const int32_t* source,
+                                   const int32_t* b, int32_t K, int32_t* segments, void* stream) {
+  Segs seg;
+  if (int rc = describe(d, "route_segments")) return rc;
+  if (int rc = segments_of(b, K, "route_segments", seg)) return rc;
+  if (seg.off[K] != d->tokens) return fail(DYNB_ERR_BADARG, "route_segments: sum(b) is not the number of tokens");
+  if (!offsets || !segments || (d->tokens > 0 && !source)) return fail(DYNB_ERR_BADARG, "route_segments: null pointer");
+  if (off_by(offsets, 4) || off_by(source, 4) || off_by(segments, 4))
+    return fail(DYNB_ERR_BADARG, "route_segments: a pointer is not a multiple of its element's size");
+  Timed t(KC_ROUTE, stream, 0.0, 4.0 * d->n_experts * (K + 1));
+  hipLaunchKernelGGL(segments_kernel, dim3((d->n_experts * (K + 1) + 255) / 256), dim3(256), 0, (hipStream_t)stream,
+                     offsets, source, seg, d->top_k, d->n_experts, segments);
+  return launched("route_segments");
+}
+
+extern "C" int dynb_route_gather(const dynb_route_desc* d, const void* x, const int32_t* offsets, const int32_t* slot,
+                                 void* sorted, void* stream) {
+  if (int rc = describe(d, "route_gather")) return rc;
+  if (d->tokens == 0) return DYNB_OK;
+  if (!x || !offsets || !slot || !sorted) return fail(DYNB_ERR_BADARG, "route_gather: null pointer");
+  const size_t size = d->dtype == DYNB_F32 ? 4 : 2;
+  if (off_by(x, size) || off_by(sorted, size) || off_by(offsets, 4) || off_by(slot, 4))
+    return fail(DYNB_ERR_BADARG, "route_gather: a pointer is not a multiple of its element's size");
+  RowArgs a = row_args(d);
+  a.in = x;
+  a.ld_in = pitch(d, d->ld_tokens);
+  a.out = sorted;
+  a.ld_out = pitch(d, d->ld_sorted);
+  a.offsets = offsets;
+  a.slot = slot;
+  const dim3 grid(grid_for(a.tokens * a.granules)), block(256);
+  Timed t(KC_ROUTE, stream, 0.0, (double)size * d->cols * (a.tokens + a.choices));
+  if (d->dtype == DYNB_F32) hipLaunchKernelGGL(gather_kernel<float>, grid, block, 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(gather_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a);
+  return launched("route_gather");
+}
+
+extern "C" int dynb_route_combine(const dynb_route_desc* d, const void* sorted, const int32_t* slot,
+                                  const float* weights, const void* addend, void* out, void* stream) {
+  if (int rc = describe(d, "route_combine")) return rc;
+  if (d->tokens == 0) return DYNB_OK;
+  if (!sorted || !slot || !out) return fail(DYNB_ERR_BADARG, "route_combine: null pointer");
+  const size_t size = d->dtype == DYNB_F32 ? 4 : 2;
+  if (off_by(sorted, size) || off_by(addend, size) || off_by(out, size) || off_by(slot, 4) || off_by(weights, 4))
+    return fail(DYNB_ERR_BADARG, "route_combine: a pointer is not a multiple of its element's size");
+  RowArgs a = row_args(d);
+  a.in = sorted;
+  a.ld_in = pitch(d, d->ld_sorted);
+  a.slot = slot;
+  a.weights = weights;
+  a.addend = addend;
+  a.ld_addend = pitch(d, d->ld_addend);
+  a.out = out;
+  a.ld_out = pitch(d, d->ld_out);
+  const dim3 grid(grid_for(a.tokens * a.granules)), block(256);
+  Timed t(KC_ROUTE, stream, 2.0 * a.choices * d->cols,
+          (double)size * d->cols * (a.choices + a.tokens * (1 + (addend != nullptr))));
+  if (d->dtype == DYNB_F32) hipLaunchKernelGGL(combine_kernel<float>, grid, block, 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(combine_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a);
+  return launched("route_combine");
+}
+
+extern "C" int dynb_route_combine_backward(const dynb_route_desc* d, const void* dout, const void* sorted,
+                                           const int32_t* offsets, const int32_t* slot, const float* weights,
+                                           void* dsorted, float* dweights, void* stream) {
+  if (int rc = describe(d, "route_combine_backward")) return rc;
+  if (d->tokens == 0) return DYNB_OK;
+  if (!dout || !sorted || !offsets || !slot || !weights || !dsorted || !dweights)
+    return fail(DYNB_ERR_BADARG, "route_combine_backward: null pointer");
+  const size_t size = d->dtype == DYNB_F32 ? 4 : 2;
+  if (off_by(dout, size) || off_by(sorted, size) || off_by(dsorted, size) || off_by(offsets, 4) || off_by(slot, 4) ||
+      off_by(weights, 4) || off_by(dweights, 4))
+    return fail(DYNB_ERR_BADARG, "route_combine_backward: a pointer is not a multiple of its element's size");
+  RowArgs a = row_args(d);
+  a.in = dout;
+  a.ld_in = pitch(d, d->ld_tokens);
+  a.sorted = sorted;
+  a.ld_sorted = a.ld_out = pitch(d, d->ld_sorted);
+  a.out = dsorted;
+  a.offsets = offsets;
+  a.slot = slot;
+  a.weights = weights;
+  a.dweights = dweights;
+  const dim3 grid(grid_for(a.choices * 64)), block(256);
+  Timed t(KC_ROUTE, stream, 3.0 * a.choices * d->cols, (double)size * d->cols * (a.tokens + 2 * a.choices));
+  if (d->dtype == DYNB_F32) hipLaunchKernelGGL(combine_grad_kernel<float>, grid, block, 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(combine_grad_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a);
+  return launched("route_combine_backward");
+}

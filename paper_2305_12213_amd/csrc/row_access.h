@@ -1,0 +1,131 @@
+// Rows of fp32 or bf16 that may start at any multiple of their element's size, as fp32 values in registers, and
+// sums over a workgroup in a fixed order: shared by the kernels of the norm and of the expert sorting.
+#ifndef DYNB_ROW_ACCESS_H
+#define DYNB_ROW_ACCESS_H
+
+#include <hip/hip_runtime.h>
+
+namespace dynb {
+
+typedef __bf16 bf16;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// A granule is 8 neighbouring elements of a row.  Vector accesses need no alignment beyond the element's on this
+// target: the memory pipeline splits what crosses a line.
+constexpr int GRANULE = 8;
+struct __attribute__((packed, aligned(2))) Any16 { u32x4 v; };
+struct __attribute__((packed, aligned(1))) Any8 { u32x2 v; };
+
+__device__ inline float to_float(float v) { return v; }
+__device__ inline float to_float(bf16 v) { return (float)v; }
+
+__device__ inline void load_granule(const float* p, float (&f)[GRANULE]) {
+  const u32x4 a = ((const Any16*)p)[0].v, b = ((const Any16*)p)[1].v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = __uint_as_float(a[e]);
+    f[4 + e] = __uint_as_float(b[e]);
+  }
+}
+__device__ inline void load_granule(const bf16* p, float (&f)[GRANULE]) {
+  const u32x4 a = ((const Any16*)p)->v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = __uint_as_float(a[e] << 16);
+    f[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+  }
+}
+__device__ inline void store_granule(float* p, const float (&f)[GRANULE]) {
+  u32x4 a, b;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    a[e] = __float_as_uint(f[e]);
+    b[e] = __float_as_uint(f[4 + e]);
+  }
+  ((Any16*)p)[0].v = a;
+  ((Any16*)p)[1].v = b;
+}
+__device__ inline uint32_t two_bf16(float a, float b) {   // round to nearest even
+  return (uint32_t)__builtin_bit_cast(unsigned short, (bf16)a) |
+         ((uint32_t)__builtin_bit_cast(unsigned short, (bf16)b) << 16);
+}
+__device__ inline void store_granule(bf16* p, const float (&f)[GRANULE]) {
+  u32x4 a;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) a[e] = two_bf16(f[2 * e], f[2 * e + 1]);
+  ((Any16*)p)->v = a;
+}
+
+// The first n of 8 elements (n >= 8: all), zeros behind them; nothing past the n-th is touched.
+template <typename T>
+__device__ inline void load_part(const T* p, int n, float (&f)[GRANULE]) {
+  if (n >= GRANULE) {
+    load_granule(p, f);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < GRANULE; ++e) f[e] = e < n ? to_float(p[e]) : 0.f;
+}
+template <typename T>
+__device__ inline void store_part(T* p, int n, const float (&f)[GRANULE]) {
+  if (n >= GRANULE) {
+    store_granule(p, f);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < GRANULE; ++e)
+    if (e < n) p[e] = (T)f[e];
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ inline uint32_t wave_max(uint32_t v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+  return v;
+}
+
+// Over a workgroup of WAVES waves; every thread gets the result.  `red` is workgroup-shared and may be used again
+// right away.
+template <int WAVES>
+__device__ inline float block_sum(float v, float* red) {
+  v = wave_sum(v);
+  if (WAVES == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = red[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) s += red[w];
+  __syncthreads();
+  return s;
+}
+template <int WAVES>
+__device__ inline uint32_t block_max(uint32_t v, uint32_t* red) {
+  v = wave_max(v);
+  if (WAVES == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  uint32_t s = red[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) s = max(s, red[w]);
+  __syncthreads();
+  return s;
+}
+
+// Values of 8 bits with a scale: the largest magnitude's bits (a NaN's are above an infinity's) give scale and factor.
+struct Scale {
+  float scale, inv;
+};
+__device__ inline Scale scale_of(uint32_t amax_bits, float top) {
+  if (amax_bits >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.f};
+  const float a = __uint_as_float(amax_bits), s = a / top;
+  return {s, s > 0.f ? top / a : 0.f};
+}
+
+}  // namespace dynb
+
+#endif

@@ -1,0 +1,245 @@
+"""AdamW over many tensors against 64 bits, in all types.
+
+Bounds, fixed before the first run: the average of K gradients is off by (K + 1) * 2^-24 of the weighted
+magnitudes, each further operation by 2^-24 of its operands (16 are counted), a stored bf16 value by 2^-8.  Codes
+of 8-bit states may be off by one where fp32 and 64 bits fall on two sides of a threshold: of steps 2^-4 wide, with
+errors around 2^-20, fewer than one in a thousand."""
+import numpy as np
+import pytest
+
+from oracle import operators as oo
+from paper_2305_12213_amd import binding
+from tests.operators_harness import EPS, assert_within, host, torch_type
+
+pytestmark = pytest.mark.gpu
+RULE = dict(lr=1e-2, beta1=0.9, beta2=0.98, eps=1e-8)
+
+
+def device_vector(values, dtype, offset=0):
+    """[n] elements behind `offset` others, NaN around them."""
+    import torch
+    flat = torch.full((offset + len(values) + 8,), float("nan"), device="cuda").to(torch_type(dtype))
+    flat[offset:offset + len(values)] = torch.from_numpy(np.asarray(values, np.float32)).cuda().to(torch_type(dtype))
+    return flat[offset:offset + len(values)]
+
+
+def bytes_vector(values, offset=0):
+    import torch
+    flat = torch.full((offset + len(values) + 8,), 0x6d, device="cuda", dtype=torch.uint8)
+    flat[offset:offset + len(values)] = torch.from_numpy(np.asarray(values, np.uint8)).cuda()
+    return flat[offset:offset + len(values)]
+
+
+class Case:
+    """Tensors of the given sizes with gradients of K workers side by side in one matrix."""
+
+    def __init__(self, sizes, b, param="f32", grad="f32", state="f32", copy=True, offset=0, seed=0, odd_stride=False):
+        import torch
+        self.sizes, self.b, self.param, self.grad, self.state, self.seed = sizes, b, param, grad, state, seed
+        rng = np.random.default_rng([7, seed, len(sizes)])
+        self.tensors, self.starts, at = [], [], offset
+        for i, n in enumerate(sizes):
+            self.starts.append(at)
+            at += n + (offset if offset else (-n) % 8)
+            size = 10.0 ** rng.uniform(-3, 0)
+            m, r = rng.standard_normal(n) * 0.2 * size, rng.uniform(0.3, 1.0, n) * size
+            t = dict(n=n, weight_decay=0.1 if i % 2 == 0 else 0.0, size=size,
+                     param=device_vector(rng.standard_normal(n), param, offset),
+                     copy=device_vector(np.zeros(n), "bf16", offset) if copy and param == "f32" else None)
+            if state == "f32":
+                t.update(state1=device_vector(m, "f32", offset), state2=device_vector(r * r, "f32", offset))
+            else:
+                half = np.full(n, 0.5)
+                (q1, s1), (q2, s2) = oo.encode(m, 7, half), oo.encode(r, 8, half)
+                t.update(state1=bytes_vector(q1, offset), state2=bytes_vector(q2, offset),
+                         scale1=device_vector(s1, "f32", 1), scale2=device_vector(s2, "f32", 1))
+            self.tensors.append(t)
+        self.stride = at + (1 if odd_stride else (-at) % 8)
+        g = np.full((len(b), self.stride), np.nan, np.float32)
+        for k in range(len(b)):
+            if b[k]:                                  # (a worker without rows is not read: NaN there)
+                for t, s in zip(self.tensors, self.starts):
+                    g[k, s:s + t["n"]] = rng.standard_normal(t["n"]) * t["size"]
+        self.grads = torch.from_numpy(g).cuda().to(torch_type(grad))
+        self.h = binding.AdamW(self.tensors, param, grad, state)
+        n = self.h.workspace_bytes()
+        self.ws = torch.full((n + 16,), 0x5a, device="cuda", dtype=torch.uint8)
+        self.h.bind(self.ws, n)
+        assert bool((self.ws[n:] == 0x5a).all())
+
+    def read(self):
+        out = []
+        for t in self.tensors:
+            if self.state == "f32":
+                out.append((host(t["param"]), host(t["state1"]), host(t["state2"])))
+            else:
+                m = oo.decode(t["state1"].cpu().numpy(), host(t["scale1"]), 7)
+                r = oo.decode(t["state2"].cpu().numpy(), host(t["scale2"]), 8)
+                out.append((host(t["param"]), m, r * r))
+        return out
+
+    def check_step(self, step, seed=0):
+        import torch
+        before, g = self.read(), host(self.grads)
+        self.h.step([self.grads[0, s:] for s in self.starts], self.b, self.stride, step=step, seed=seed, **RULE)
+        torch.cuda.synchronize()
+        after, live = self.read(), [k for k, n in enumerate(self.b) if n]
+        c1, c2 = 1 - RULE["beta1"] ** step, 1 - RULE["beta2"] ** step
+        for i, (t, s) in enumerate(zip(self.tensors, self.starts)):
+            n = t["n"]
+            mine = g[:, s:s + n]
+            p, m, v = oo.adamw(*before[i], mine, self.b, t["weight_decay"], step=step, **RULE)
+            lam = np.array(self.b) / sum(self.b)
+            gmag = sum((lam[k] * np.abs(mine[k]) for k in live), np.zeros(n))
+            graw = sum((lam[k] * mine[k] for k in live), np.zeros(n))
+            ge = (len(live) + 16) * EPS * gmag                                  # error of the average
+            me = 0.1 * ge + 16 * EPS * (np.abs(before[i][1]) + gmag)
+            ve = 0.04 * np.abs(graw) * ge + 0.02 * ge * ge + 16 * EPS * (before[i][2] + 0.02 * gmag ** 2)
+            root = np.sqrt(v / c2) + RULE["eps"]
+            with np.errstate(all="ignore"):
+                hat = np.abs(m / c1) / root
+                he = me / c1 / root + hat * (0.5 * ve / np.maximum(v, 1e-60) + 8 * EPS)
+            pe = 16 * EPS * np.abs(before[i][0]) + RULE["lr"] * np.where(v > 0, he, 0) + 4 * EPS * RULE["lr"] * hat
+            stored = 1.01 * 2.0 ** -8 * np.abs(p) if self.param == "bf16" else 0.0
+            assert_within(after[i][0], p, pe + stored, "param %d" % i)
+            if t["copy"] is not None:
+                assert torch.equal(t["copy"], t["param"].to(torch.bfloat16))
+            if self.state == "f32":
+                assert_within(after[i][1], m, me, "m %d" % i)
+                assert_within(after[i][2], v, ve, "v %d" % i)
+                continue
+            u = oo.random_bits(n, i, seed)
+            for x, bits, part, code, scale in ((m, 7, u >> 16, t["state1"], t["scale1"]),
+                                               (np.sqrt(v), 8, u & 65535, t["state2"], t["scale2"])):
+                want, scales = oo.encode(x, bits, part / 65536)
+                assert_within(host(scale), scales, 1e-5 * np.abs(np.nan_to_num(scales)), "scale")
+                got = code.cpu().numpy().astype(np.int64)
+                sign = 0 if bits == 8 else 128
+                flip = (got & sign) != (want & sign)
+                assert (np.abs(x[flip]) <= me[flip]).all()
+                far = np.abs((got & ~sign) - (want & ~sign))
+                assert far.max(initial=0) <= 1 and (far > 0).sum() <= 1 + 1e-3 * n, (i, far.max(), (far > 0).sum())
+        self.check_margins()
+
+    def check_margins(self):
+        """Nothing around the tensors has been written."""
+        import torch
+        for t in self.tensors:
+            for name in ("param", "copy", "state1", "state2", "scale1", "scale2"):
+                v = t.get(name)
+                if v is None:
+                    continue
+                whole = torch.empty(0, dtype=v.dtype, device="cuda").set_(v.untyped_storage())
+                around = torch.cat([whole[:v.storage_offset()], whole[v.storage_offset() + v.numel():]])
+                assert bool((around == 0x6d).all()) if v.dtype == torch.uint8 else bool(around.isnan().all()), name
+
+
+SIZES = [1, 255, 256, 257, 4096, 0, 4097, 3, 10000, 8192, 2, 4, 5]
+TYPES = [(p, g, s) for p in ("f32", "bf16") for g in ("f32", "bf16") for s in ("f32", "8bit")]
+
+
+@pytest.mark.parametrize("param,grad,state", TYPES)
+@pytest.mark.parametrize("b", [[5], [3, 0, 1], [1] * 9])
+def test_types(dynb, param, grad, state, b):
+    c = Case(SIZES, b, param, grad, state)
+    for step in (1, 2, 1000):
+        c.check_step(step, seed=step)
+
+
+@pytest.mark.parametrize("param,grad,state", TYPES)
+@pytest.mark.parametrize("offset", [1, 2, 3])
+def test_any_start_and_stride(dynb, param, grad, state, offset):
+    Case([700, 1, 4099, 256], [2, 3], param, grad, state, offset=offset, odd_stride=True).check_step(3, seed=9)
+
+
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+@pytest.mark.parametrize("count", [127, 128, 129, 255, 256, 257, 600])
+def test_many_tensors(dynb, state, count):
+    Case([1 + (37 * i) % 300 for i in range(count)], [1, 2], state=state, copy=False).check_step(2, seed=4)
+
+
+@pytest.mark.parametrize("b", [[0, 4], [0] * 63 + [1], [1] * 64])
+def test_workers(dynb, b):
+    Case([1000, 3], b, state="8bit", grad="bf16").check_step(5)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_read_states(dynb, out):
+    import torch
+    sizes = [1 + (91 * i) % 700 for i in range(140)] + [0, 9000]
+    c = Case(sizes, [1], state="8bit")
+    o1, o2 = ([torch.full((n + 3,), -7.0, device="cuda").to(torch_type(out)) for n in sizes] for _ in range(2))
+    c.h.read_states(o1, o2, out)
+    torch.cuda.synchronize()
+    for (_, m, v), a, b, n in zip(c.read(), o1, o2, sizes):
+        for got, want in ((a, m), (b, v)):
+            assert_within(host(got)[:n], want, (8 * EPS + (2.0 ** -8 if out == "bf16" else 0)) * 1.01 * np.abs(want), "state")
+            assert got[n:].tolist() == [-7.0] * 3
+
+
+def test_zero_states_and_gradients(dynb):
+    """The first step from zero states; a tensor without gradients only decays; blocks of zeros stay zeros."""
+    import torch
+    for state in ("f32", "8bit"):
+        c = Case([600, 300], [1], state=state)
+        for t in c.tensors:
+            for name in ("state1", "state2", "scale1", "scale2"):
+                if t.get(name) is not None:
+                    t[name].zero_()
+        c.grads[0, c.starts[1]:c.starts[1] + 300] = 0
+        c.check_step(1)
+        _, m, v = c.read()[1]
+        assert not m.any() and not v.any()
+
+
+def test_infinities_and_nan_stay_in_their_element_or_block(dynb):
+    import torch
+    for state in ("f32", "8bit"):
+        c = Case([1024], [1], state=state)
+        c.grads[0, 300] = float("inf")
+        c.grads[0, 800] = float("nan")
+        g = [c.grads[0, s:] for s in c.starts]
+        c.h.step(g, [1], c.stride, step=2, **RULE)
+        c.grads.zero_()
+        c.h.step(g, [1], c.stride, step=3, **RULE)
+        torch.cuda.synchronize()
+        p, m, _ = c.read()[0]
+        hurt = np.zeros(1024, bool)
+        if state == "f32":
+            hurt[[300, 800]] = True
+        else:
+            hurt[256:512] = hurt[768:1024] = True
+        assert np.isnan(p[hurt]).all() and np.isfinite(p[~hurt]).all()
+        assert not np.isfinite(m[hurt]).any() and np.isfinite(m[~hurt]).all()
+
+
+def test_steps_repeat(dynb):
+    import torch
+    runs = []
+    for _ in range(2):
+        c = Case([5000, 77], [3, 1], state="8bit", grad="bf16")
+        for step in (1, 2, 3):
+            c.h.step([c.grads[0, s:] for s in c.starts], c.b, c.stride, step=step, seed=step, **RULE)
+        torch.cuda.synchronize()
+        runs.append([t[n].clone() for t in c.tensors for n in ("param", "state1", "state2", "scale1", "scale2")])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_graph(dynb):
+    """A step recorded into a graph and replayed does what the same steps do one by one."""
+    import torch
+    def build():
+        return Case([5000, 77], [3, 1], state="8bit", grad="bf16")
+    one, two = build(), build()
+    call = lambda c: c.h.step(binding.pointers([c.grads[0, s:] for s in c.starts]), c.b, c.stride, step=5, seed=3, **RULE)  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call(two)
+    for _ in range(3):
+        call(one)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(one.tensors, two.tensors):
+            assert torch.equal(a["param"], b["param"]) and torch.equal(a["state1"], b["state1"])
