@@ -29,6 +29,32 @@ template <int OUT> __device__ inline uint8_t eight_bits(float v, float inv) {
   return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(t, t, 0, false) & 0xff);
 }
 
+// 8 neighbouring values, the first n of them.
+template <int OUT>
+__device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE], float inv) {
+  u32x2 q;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = inv > 0.f ? f[4 * h + e] * inv : 0.f;
+    if (OUT == DYNB_OUT_FP8) {
+      q[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
+    } else {
+      q[h] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[h] |= ((uint32_t)(int)rintf(v[e]) & 0xffu) << (8 * e);
+    }
+  }
+  if (n >= GRANULE) {
+    ((Any8*)p)->v = q;
+  } else {
+#pragma unroll
+    for (int e = 0; e < GRANULE; ++e)
+      if (e < n) p[e] = (uint8_t)(q[e / 4] >> (8 * (e & 3)));
+  }
+}
+
 // 1 / sqrt(mean + eps) from the sum of squares; where that has overflowed, from the squares of the row times 2^-80,
 // which `scaled_sum` gives (eps is nothing beside them; a row with an infinity or NaN ends the same either way).
 template <typename F> __device__ inline float rstd_of(float ss, int cols, float eps, F scaled_sum) {
@@ -90,6 +116,101 @@ __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
   }
 }
 
+// Rows that fit in the registers of W waves, N granules per thread: one read, one write.  (W = 1: four rows per
+// workgroup, no barrier.)  A thread keeps its part of the gain over all rows of the workgroup.  group: lanes that share a
+// scale (a power of two), 0 where the whole row does.
+template <typename T, int OUT, int W, int N>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArgs p, int group) {
+  constexpr int PER = W == 1 ? 4 : 1;      // rows of a workgroup
+  constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
+  __shared__ float red[W];
+  __shared__ uint32_t redu[W];
+  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  int64_t r = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x >> 6 : 0);
+  Raw<T> x[N], res[N];
+  auto ask = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (t + i * 64 * W) * GRANULE;
+      x[i] = load_raw((const T*)p.x + row * p.ld_x + c, p.cols - c);
+      if (p.residual) res[i] = load_raw((const T*)p.residual + row * p.ld_residual + c, p.cols - c);
+    }
+  };
+  if (r < p.rows) ask(r);
+  Raw<float> gain[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (t + i * 64 * W) * GRANULE;
+    if (p.gain) gain[i] = load_raw(p.gain + c, p.cols - c);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) gain[i].a[e] = gain[i].b[e] = 0x3f800000u;
+  }
+  for (; r < p.rows; r += (int64_t)gridDim.x * PER) {
+    float s[N][GRANULE], ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      unpack(x[i], s[i]);
+      if (p.residual) {
+        float q[GRANULE];
+        unpack(res[i], q);
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) s[i][e] += q[e];
+      }
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) ss += s[i][e] * s[i][e];
+    }
+    ss = block_sum<W>(ss, red);
+    const float rstd = rstd_of(ss, p.cols, p.eps, [&]() {
+      float a = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) a += (s[i][e] * 0x1p-80f) * (s[i][e] * 0x1p-80f);
+      return block_sum<W>(a, red);
+    });
+    if (t == 0 && p.rstd) p.rstd[r] = rstd;
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (t + i * 64 * W) * GRANULE;
+      if (p.sum && c < p.cols) store_part((T*)p.sum + r * p.ld_sum + c, p.cols - c, s[i]);
+      float g[GRANULE];
+      unpack(gain[i], g);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) {
+        s[i][e] *= rstd * g[e];
+        if (c + e >= p.cols) s[i][e] = 0.f;
+      }
+      if (OUT == DYNB_OUT_SAME && c < p.cols) store_part((T*)p.y + r * p.ld_y + c, p.cols - c, s[i]);
+    }
+    const int64_t now = r;
+    if (r + (int64_t)gridDim.x * PER < p.rows) ask(r + (int64_t)gridDim.x * PER);
+    if (OUT == DYNB_OUT_SAME) continue;
+    Scale scale;
+    if (group == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) amax = max(amax, __float_as_uint(s[i][e]) & 0x7fffffffu);
+      scale = scale_of(block_max<W>(amax, redu), TOP);
+      if (t == 0) p.scales[now] = scale.scale;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (t + i * 64 * W) * GRANULE;
+      if (group) {
+        amax = 0;
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) amax = max(amax, __float_as_uint(s[i][e]) & 0x7fffffffu);
+        scale = scale_of(group_max(amax, group), TOP);
+        if ((t & (group - 1)) == 0 && c < p.cols) p.scales[now * p.n_blocks + c / p.scale_block] = scale.scale;
+      }
+      if (c < p.cols) store_eight<OUT>((uint8_t*)p.y + now * p.ld_y + c, p.cols - c, s[i], scale.inv);
+    }
+  }
+}
+
 struct NormGradArgs {
   const void* sum;
   const float *rstd, *gain;
@@ -129,14 +250,28 @@ __global__ __launch_bounds__(256) void rms_norm_gain_grad_kernel(NormGradArgs p,
   p.dgain[k * p.dgain_stride + c] = a;
 }
 
+// A thread takes 8 neighbouring values of a row at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void dequantise_kernel(NormArgs p, int out, T* to, int64_t ld_to) {
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x)
-    for (int c = threadIdx.x; c < p.cols; c += 256) {
-      const uint8_t q = ((const uint8_t*)p.y)[r * p.ld_y + c];
-      const float v = out == DYNB_OUT_INT8 ? (float)(int8_t)q : __builtin_amdgcn_cvt_f32_fp8(q, 0);
-      to[r * ld_to + c] = (T)(v * p.scales[r * p.n_blocks + (p.n_blocks == 1 ? 0 : c / p.scale_block)]);
+  const int granules = (p.cols + GRANULE - 1) / GRANULE;
+  const int64_t total = (int64_t)p.rows * granules;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = total < ((int64_t)1 << 32) ? (int64_t)((uint32_t)i / (uint32_t)granules) : i / granules;
+    const int c = (int)(i - r * granules) * GRANULE, n = p.cols - c;
+    const uint8_t* y = (const uint8_t*)p.y + r * p.ld_y + c;
+    const float scale = p.scales[r * p.n_blocks + (p.n_blocks == 1 ? 0 : c / p.scale_block)];
+    u32x2 q = {0, 0};
+    if (n >= GRANULE) q = ((const Any8*)y)->v;
+    else
+      for (int e = 0; e < n; ++e) q[e / 4] |= (uint32_t)y[e] << (8 * (e & 3));
+    float f[GRANULE];
+#pragma unroll
+    for (int e = 0; e < GRANULE; ++e) {
+      const uint32_t b = q[e / 4] >> (8 * (e & 3));
+      f[e] = (out == DYNB_OUT_INT8 ? (float)(int8_t)b : __builtin_amdgcn_cvt_f32_fp8(b, 0)) * scale;
     }
+    store_part(to + r * ld_to + c, n, f);
+  }
 }
 
 int grid_of_rows(int64_t rows) { return (int)(rows < (1 << 20) ? rows : 1 << 20); }
@@ -167,17 +302,237 @@ int describe(const dynb_rms_norm_desc* d, const char* who, NormArgs& a) {
   return DYNB_OK;
 }
 
-template <typename T> void launch_norm(const NormArgs& a, int out, hipStream_t st) {
-  const dim3 grid(grid_of_rows(a.rows)), block(256);
-  if (out == DYNB_OUT_SAME) hipLaunchKernelGGL((rms_norm_any_kernel<T, DYNB_OUT_SAME>), grid, block, 0, st, a);
-  else if (out == DYNB_OUT_FP8) hipLaunchKernelGGL((rms_norm_any_kernel<T, DYNB_OUT_FP8>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((rms_norm_any_kernel<T, DYNB_OUT_INT8>), grid, block, 0, st, a);
+// Workgroups for `units` of work where one has `threads` threads: what the chip holds at once, less if there is less.
+int resident(int64_t units, int threads) {
+  const int64_t most = 256 * (2048 / threads);
+  return (int)(units < most ? units : most);
 }
 
-template <typename T> void launch_norm_grad(const NormGradArgs& a, const Segs& seg, hipStream_t st) {
-  if (a.dgain)   // (first: dx may lie on dy)
-    hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((a.cols + 255) / 256, seg.K), dim3(256), 0, st, a, seg);
-  if (a.rows) hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
+template <typename T, int OUT, int W, int N> void launch_norm_as(const NormArgs& a, int group, hipStream_t st) {
+  constexpr int THREADS = W == 1 ? 256 : 64 * W, PER = W == 1 ? 4 : 1;
+  hipLaunchKernelGGL((rms_norm_kernel<T, OUT, W, N>), dim3(resident((a.rows + PER - 1) / PER, THREADS)), dim3(THREADS), 0,
+                     st, a, group);
+}
+
+template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream_t st) {
+  // lanes that share a scale: a power of two within a wave, or the whole row
+  const int granules = (a.cols + GRANULE - 1) / GRANULE, lanes = a.scale_block / GRANULE;
+  const bool whole = OUT == DYNB_OUT_SAME || a.n_blocks == 1;
+  const int group = whole ? 0 : lanes;
+  if (granules > 2048 || (!whole && (lanes > 64 || (lanes & (lanes - 1))))) {
+    hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
+    return;
+  }
+  if (granules <= 64) launch_norm_as<T, OUT, 1, 1>(a, group, st);
+  else if (granules <= 128) launch_norm_as<T, OUT, 1, 2>(a, group, st);
+  else if (granules <= 256) launch_norm_as<T, OUT, 4, 1>(a, group, st);
+  else if (granules <= 512) launch_norm_as<T, OUT, 4, 2>(a, group, st);
+  else if (granules <= 1024) launch_norm_as<T, OUT, 8, 2>(a, group, st);
+  else launch_norm_as<T, OUT, 16, 2>(a, group, st);
+}
+
+template <typename T> void launch_norm(const NormArgs& a, int out, hipStream_t st) {
+  if (out == DYNB_OUT_SAME) launch_norm_out<T, DYNB_OUT_SAME>(a, st);
+  else if (out == DYNB_OUT_FP8) launch_norm_out<T, DYNB_OUT_FP8>(a, st);
+  else launch_norm_out<T, DYNB_OUT_INT8>(a, st);
+}
+
+// Both gradients of rows that fit in the registers of W waves, N granules per thread, in one pass: the rows' gradient, and
+// the gain's summed over the rows of a chunk (of one worker) in registers, then over the chunks by sum_chunks_kernel.
+// (W = 1: each of four waves takes every fourth row of the chunk, and their sums are added in LDS.)  A row's loads are
+// issued while the row before it is reduced.
+struct Chunks {
+  int rows;                               // of a chunk, the last one of a worker may be shorter
+  int first[DYNB_MAX_WORKERS + 1];        // of each worker's chunks
+};
+template <typename T, int W, int N>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(NormGradArgs p, Segs seg, Chunks ch,
+                                                                             float* partial) {
+  constexpr int PER = W == 1 ? 4 : 1, COLS = 64 * W * N * GRANULE;
+  constexpr bool AHEAD = W < 16 || sizeof(T) == 2;   // (fp32 rows of 16 waves: the next row would spill)
+  __shared__ float red[W];
+  __shared__ float sums[W == 1 ? 3 * COLS : 1];
+  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x, wave = W == 1 ? threadIdx.x >> 6 : 0;
+  int k = 0;
+  while (k + 1 < seg.K && (int)blockIdx.x >= ch.first[k + 1]) ++k;
+  const int begin = seg.off[k] + ((int)blockIdx.x - ch.first[k]) * ch.rows, end = min(begin + ch.rows, seg.off[k + 1]);
+  Raw<T> s[N], dy[N], ds[N];
+  float rstd = 0.f;
+  auto ask = [&](int64_t r) {
+    rstd = p.rstd[r];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (t + i * 64 * W) * GRANULE;
+      s[i] = load_raw((const T*)p.sum + r * p.ld_sum + c, p.cols - c);
+      dy[i] = load_raw((const T*)p.dy + r * p.ld_dy + c, p.cols - c);
+      if (p.dsum) ds[i] = load_raw((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c);
+    }
+  };
+  int r = begin + wave;
+  if (AHEAD && r < end) ask(r);
+  float acc[N][GRANULE];
+  Raw<float> gain[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (t + i * 64 * W) * GRANULE;
+    if (p.gain) gain[i] = load_raw(p.gain + c, p.cols - c);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) gain[i].a[e] = gain[i].b[e] = 0x3f800000u;
+#pragma unroll
+    for (int e = 0; e < GRANULE; ++e) acc[i][e] = 0.f;
+  }
+  for (; r < end; r += PER) {
+    if (!AHEAD) ask(r);
+    float c1 = 0.f;
+    Raw<T> s0[N], dy0[N], ds0[N];
+    const float rstd0 = rstd;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s0[i] = s[i];
+      dy0[i] = dy[i];
+      if (p.dsum) ds0[i] = ds[i];
+    }
+    if (AHEAD && r + PER < end) ask(r + PER);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float a[GRANULE], d[GRANULE], g[GRANULE];
+      unpack(s0[i], a);
+      unpack(dy0[i], d);
+      unpack(gain[i], g);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) {
+        const float q = d[e] * (a[e] * rstd0);
+        acc[i][e] += q;
+        c1 += g[e] * q;
+      }
+    }
+    c1 = block_sum<W>(c1, red) / (float)p.cols;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (t + i * 64 * W) * GRANULE;
+      if (c >= p.cols) continue;
+      float a[GRANULE], d[GRANULE], g[GRANULE];
+      unpack(s0[i], a);
+      unpack(dy0[i], d);
+      unpack(gain[i], g);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) a[e] = rstd0 * (g[e] * d[e] - a[e] * rstd0 * c1);
+      if (p.dsum) {
+        unpack(ds0[i], d);
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
+      }
+      store_part((T*)p.dx + (int64_t)r * p.ld_dx + c, p.cols - c, a);
+    }
+  }
+  if (!p.dgain) return;
+  if (W == 1) {
+    if (wave > 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) sums[(wave - 1) * COLS + e * 64 * N + i * 64 + t] = acc[i][e];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) acc[i][e] += sums[w * COLS + e * 64 * N + i * 64 + t];
+  }
+  // a worker's only chunk is its sum
+  float* const to = ch.first[k + 1] - ch.first[k] == 1 ? p.dgain + k * p.dgain_stride : partial + (int64_t)blockIdx.x * p.cols;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (t + i * 64 * W) * GRANULE;
+    if (c < p.cols) store_part(to + c, p.cols - c, acc[i]);
+  }
+}
+
+// Sums of the workers' chunks, 64 columns per workgroup: 16 groups of threads take every 16th chunk, then the groups are
+// added in order.  Workers without rows get zeros; those with one chunk have their sum.
+__global__ __launch_bounds__(1024) void sum_chunks_kernel(const float* partial, Chunks ch, int cols, float* dgain,
+                                                          int64_t stride) {
+  __shared__ float sums[16][64];
+  const int k = blockIdx.y, n = ch.first[k + 1] - ch.first[k];
+  if (n == 1) return;
+  const int lane = threadIdx.x & 63, group = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  float a = 0.f;
+  if (c < cols) {
+    const float* from = partial + (int64_t)ch.first[k] * cols + c;
+#pragma unroll 8
+    for (int i = group; i < n; i += 16) a += from[(int64_t)i * cols];
+  }
+  sums[group][lane] = a;
+  __syncthreads();
+  if (group > 0 || c >= cols) return;
+#pragma unroll
+  for (int g = 1; g < 16; ++g) a += sums[g][lane];
+  dgain[k * stride + c] = a;
+}
+
+constexpr int GRAD_GRANULES = 2048;       // widest rows of rms_norm_grad_kernel
+
+// How the workers' rows are cut, and how many chunks: enough workgroups for the chip, and rows enough in each that the
+// chunks' sums are a small part of what is read.
+int chunks_of(const Segs& seg, int cols, Chunks& ch) {
+  const int granules = (cols + GRANULE - 1) / GRANULE, rows = seg.off[seg.K];
+  const int per = granules <= 128 ? 4 : 1;
+  ch.rows = (rows + 511) / 512;
+  const int least = granules <= 128 ? 8 : 4;
+  if (ch.rows < least) ch.rows = least;
+  ch.rows = (ch.rows + per - 1) / per * per;
+  int n = 0;
+  for (int k = 0; k < seg.K; ++k) {
+    ch.first[k] = n;
+    n += (seg.off[k + 1] - seg.off[k] + ch.rows - 1) / ch.rows;
+  }
+  ch.first[seg.K] = n;
+  return n;
+}
+
+template <typename T, int W, int N>
+void launch_norm_grad_as(const NormGradArgs& a, const Segs& seg, const Chunks& ch, float* partial, hipStream_t st) {
+  hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, N>), dim3(ch.first[seg.K]), dim3(W == 1 ? 256 : 64 * W), 0, st, a, seg,
+                     ch, partial);
+}
+
+template <typename T>
+void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hipStream_t st) {
+  const int granules = (a.cols + GRANULE - 1) / GRANULE;
+  if (granules > GRAD_GRANULES) {
+    if (a.dgain)   // (first: dx may lie on dy)
+      hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((a.cols + 255) / 256, seg.K), dim3(256), 0, st, a, seg);
+    if (a.rows) hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
+    return;
+  }
+  Chunks ch;
+  const int n = chunks_of(seg, a.cols, ch);
+  if (n > 0) {
+    if (granules <= 64) launch_norm_grad_as<T, 1, 1>(a, seg, ch, partial, st);
+    else if (granules <= 128) launch_norm_grad_as<T, 1, 2>(a, seg, ch, partial, st);
+    else if (granules <= 256) launch_norm_grad_as<T, 4, 1>(a, seg, ch, partial, st);
+    else if (granules <= 512) launch_norm_grad_as<T, 4, 2>(a, seg, ch, partial, st);
+    else if (granules <= 1024) launch_norm_grad_as<T, 8, 2>(a, seg, ch, partial, st);
+    else launch_norm_grad_as<T, 16, 2>(a, seg, ch, partial, st);
+  }
+  bool left = false;
+  for (int k = 0; k < seg.K; ++k) left |= ch.first[k + 1] - ch.first[k] != 1;
+  if (a.dgain && left)
+    hipLaunchKernelGGL(sum_chunks_kernel, dim3((a.cols + 63) / 64, seg.K), dim3(1024), 0, st, partial, ch, a.cols, a.dgain,
+                       a.dgain_stride);
+}
+
+// Bytes of the chunks' sums (none where every worker has one chunk at most).
+size_t partial_bytes(const Segs& seg, int cols) {
+  Chunks ch;
+  if ((cols + GRANULE - 1) / GRANULE > GRAD_GRANULES) return 0;
+  const int n = chunks_of(seg, cols, ch);
+  bool more = false;
+  for (int k = 0; k < seg.K; ++k) more |= ch.first[k + 1] - ch.first[k] > 1;
+  return more ? (size_t)n * cols * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -250,7 +605,7 @@ extern "C" int dynb_dequantise(const dynb_rms_norm_desc* d, int64_t rows, const 
   a.scales = const_cast<float*>(scales);
   a.rows = (int)rows;
   if (!ld_out) ld_out = d->cols;
-  const dim3 grid(grid_of_rows(rows)), block(256);
+  const dim3 grid(resident((rows * ((d->cols + GRANULE - 1) / GRANULE) + 255) / 256, 256)), block(256);
   Timed t(KC_NORM, stream, (double)rows * d->cols, (double)rows * d->cols * (out_dtype == DYNB_F32 ? 5 : 3));
   if (out_dtype == DYNB_F32)
     hipLaunchKernelGGL(dequantise_kernel<float>, grid, block, 0, (hipStream_t)stream, a, d->out, (float*)out, ld_out);
@@ -263,7 +618,7 @@ extern "C" size_t dynb_rms_norm_backward_workspace_bytes(const dynb_rms_norm_des
   NormArgs a;
   Segs seg;
   if (describe(d, "rms_norm_backward", a) || segments_of(b, K, "rms_norm_backward", seg)) return 0;
-  return 0;
+  return partial_bytes(seg, a.cols);
 }
 
 extern "C" int dynb_rms_norm_backward(const dynb_rms_norm_desc* d, const int32_t* b, int32_t K, const void* sum,
@@ -282,13 +637,14 @@ extern "C" int dynb_rms_norm_backward(const dynb_rms_norm_desc* d, const int32_t
   if (off_by(sum, size) || off_by(dy, size) || off_by(dsum, size) || off_by(dx, size) || off_by(rstd, 4) ||
       off_by(gain, 4) || off_by(dgain, 4))
     return fail(DYNB_ERR_BADARG, "rms_norm_backward: a pointer is not a multiple of its element's size");
-  (void)workspace;
-  (void)workspace_bytes;
+  const size_t need = dgain ? partial_bytes(seg, d->cols) : 0;
+  if (need && (!workspace || workspace_bytes < need || off_by(workspace, 16)))
+    return fail(DYNB_ERR_BADARG, "rms_norm_backward: workspace is null, too small or not 16-byte aligned");
   NormGradArgs a = {sum, rstd, gain, dy, dsum, dx, dgain, f.ld_sum, d->ld_dy ? d->ld_dy : d->cols,
                     d->ld_dsum ? d->ld_dsum : d->cols, d->ld_dx ? d->ld_dx : d->cols, dgain_stride, rows, d->cols};
   const double n = (double)rows * d->cols;
   Timed t(KC_NORM, stream, 12.0 * n, n * size * (3 + (dsum != nullptr)) + 4.0 * K * d->cols);
-  if (d->dtype == DYNB_F32) launch_norm_grad<float>(a, seg, (hipStream_t)stream);
-  else launch_norm_grad<bf16>(a, seg, (hipStream_t)stream);
+  if (d->dtype == DYNB_F32) launch_norm_grad<float>(a, seg, (float*)workspace, (hipStream_t)stream);
+  else launch_norm_grad<bf16>(a, seg, (float*)workspace, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "rms_norm_backward launch failed");
 }

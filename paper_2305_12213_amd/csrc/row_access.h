@@ -78,15 +78,84 @@ __device__ inline void store_part(T* p, int n, const float (&f)[GRANULE]) {
     if (e < n) p[e] = (T)f[e];
 }
 
-__device__ inline float wave_sum(float v) {
+// A granule as it is stored, 4 (bf16) or 8 (fp32) registers: what waits for its use between load and arithmetic.
+template <typename T> struct Raw;
+template <> struct Raw<bf16> { u32x4 a; };
+template <> struct Raw<float> { u32x4 a, b; };
+__device__ inline void unpack(const Raw<bf16>& r, float (&f)[GRANULE]) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = __uint_as_float(r.a[e] << 16);
+    f[2 * e + 1] = __uint_as_float(r.a[e] & 0xffff0000u);
+  }
+}
+__device__ inline void unpack(const Raw<float>& r, float (&f)[GRANULE]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = __uint_as_float(r.a[e]);
+    f[4 + e] = __uint_as_float(r.b[e]);
+  }
+}
+// ... of the first n elements (n <= 0: none), zeros behind them
+__device__ inline Raw<bf16> load_raw(const bf16* p, int n) {
+  Raw<bf16> r = {{0, 0, 0, 0}};
+  if (n >= GRANULE) {
+    r.a = ((const Any16*)p)->v;
+  } else if (n > 0) {
+    const unsigned short* h = (const unsigned short*)p;
+#pragma unroll
+    for (int e = 0; e < GRANULE; ++e)
+      if (e < n) r.a[e / 2] |= (uint32_t)h[e] << (16 * (e & 1));
+  }
+  return r;
+}
+__device__ inline Raw<float> load_raw(const float* p, int n) {
+  Raw<float> r = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  if (n >= GRANULE) {
+    r.a = ((const Any16*)p)[0].v;
+    r.b = ((const Any16*)p)[1].v;
+  } else if (n > 0) {
+    const uint32_t* w = (const uint32_t*)p;
+#pragma unroll
+    for (int e = 0; e < GRANULE; ++e)
+      if (e < n) (e < 4 ? r.a : r.b)[e & 3] = w[e];
+  }
+  return r;
+}
+
+// Exchanges between lanes that need no LDS: within 2, 4, 8 and 16 lanes (after the step every lane of the group has
+// the same value, so that a mirrored partner is as good as the xor-ed one).
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
+template <int CTRL> __device__ inline uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL> __device__ inline float from_lane(float v) { return __uint_as_float(from_lane<CTRL>(__float_as_uint(v))); }
+__device__ inline float of_lane(float v, int lane) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane));
+}
+__device__ inline float wave_sum(float v) {
+  v += from_lane<DPP_XOR1>(v);
+  v += from_lane<DPP_XOR2>(v);
+  v += from_lane<DPP_HALF_MIRROR>(v);
+  v += from_lane<DPP_MIRROR>(v);
+  return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
+}
+// Over groups of 2, 4, ... 64 neighbouring lanes (`lanes` the same in the whole wave).
+__device__ inline uint32_t group_max(uint32_t v, int lanes) {
+  if (lanes > 1) v = max(v, from_lane<DPP_XOR1>(v));
+  if (lanes > 2) v = max(v, from_lane<DPP_XOR2>(v));
+  if (lanes > 4) v = max(v, from_lane<DPP_HALF_MIRROR>(v));
+  if (lanes > 8) v = max(v, from_lane<DPP_MIRROR>(v));
+  if (lanes > 16) v = max(v, (uint32_t)__shfl_xor((int)v, 16));
+  if (lanes > 32) v = max(v, (uint32_t)__shfl_xor((int)v, 32));
   return v;
 }
 __device__ inline uint32_t wave_max(uint32_t v) {
+  v = group_max(v, 16);
+  uint32_t m = 0;
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-  return v;
+  for (int l = 0; l < 64; l += 16) m = max(m, (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+  return m;
 }
 
 // Over a workgroup of WAVES waves; every thread gets the result.  `red` is workgroup-shared and may be used again
