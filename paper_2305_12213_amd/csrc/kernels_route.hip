@@ -9,9 +9,12 @@ namespace dynb {
 namespace {
 
 // ---- the plan -----------------------------------------------------------------------------------------------
-// One workgroup of 16 waves, each with a stretch of the choices: the waves count their stretches, the counts are
-// summed in the order (expert, wave), and each wave goes over its stretch again and hands out the places in order.
-constexpr int PLAN_WAVES = 16;
+// A stable counting sort.  Every wave owns a stretch of the choices; it counts its experts, the counts are summed in the
+// order (expert, workgroup, wave), and the wave goes over its stretch again, 64 choices at a time, and hands out the
+// places in order.  Up to SMALL choices one workgroup does it all in one launch; beyond, a launch before it counts per
+// workgroup, and every workgroup sums those of the ones before it.
+constexpr int SMALL = 8192, SMALL_WAVES = 16, LARGE_WAVES = 4, AHEAD = 8;   // AHEAD: choices per lane that are loaded at once
+constexpr int MOST_BLOCKS = 128;          // whose counts a workgroup sums
 
 // Lanes of the wave with the same key as this one (all lanes take part; keys below 2^bits).
 __device__ inline uint64_t same_key(int key, int bits) {
@@ -29,68 +32,162 @@ __device__ inline void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-__global__ __launch_bounds__(PLAN_WAVES * 64) void plan_kernel(const int32_t* experts, int n, int n_experts,
-                                                               int bits, int32_t* offsets, int32_t* slot,
-                                                               int32_t* source) {
-  __shared__ int count[PLAN_WAVES * DYNB_MAX_EXPERTS];
-  __shared__ int first[DYNB_MAX_EXPERTS + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int* mine = count + wave * n_experts;
-  for (int i = threadIdx.x; i < PLAN_WAVES * n_experts; i += PLAN_WAVES * 64) count[i] = 0;
-  __syncthreads();
-  const int per = ((n + PLAN_WAVES - 1) / PLAN_WAVES + 63) / 64 * 64;
-  const int64_t begin = (int64_t)wave * per, end = begin + per < n ? begin + per : n;
-  for (int64_t i = begin + lane; i < end; i += 64) {
-    const int e = experts[i];
-    if ((uint32_t)e < (uint32_t)n_experts) atomicAdd(&mine[e], 1);
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    int at = 0;
-    for (int e = 0; e < n_experts; ++e) {
-      first[e] = at;
-      for (int w = 0; w < PLAN_WAVES; ++w) {
-        const int c = count[w * n_experts + e];
-        count[w * n_experts + e] = at;
-        at += c;
-      }
+// What one stretch counts: each lane's choices begin + lane + 64 i.
+__device__ inline void count_stretch(const int32_t* experts, int64_t begin, int64_t end, int n_experts, int* count) {
+  for (int64_t i0 = begin; i0 < end; i0 += 64 * AHEAD) {
+    int e[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t i = i0 + 64 * u + (threadIdx.x & 63);
+      e[u] = i < end ? experts[i] : -1;
     }
-    first[n_experts] = at;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if ((uint32_t)e[u] < (uint32_t)n_experts) atomicAdd(&count[e[u]], 1);   // (whole numbers: any order)
   }
-  __syncthreads();
-  for (int e = threadIdx.x; e <= n_experts; e += PLAN_WAVES * 64) offsets[e] = first[e];
-  for (int64_t i0 = begin; i0 < end; i0 += 64) {
-    const int64_t i = i0 + lane;
-    int e = i < end ? experts[i] : -1;
-    const bool kept = (uint32_t)e < (uint32_t)n_experts;
-    if (!kept) e = n_experts;
-    const uint64_t same = same_key(e, bits);
-    const int before = __popcll(same & ((1ull << lane) - 1));
-    int place = -1;
-    if (kept) place = mine[e] + before;
-    wave_fence();                        // every lane has read its expert's place before the first of them moves it on
-    if (kept && before == 0) mine[e] += __popcll(same);
-    wave_fence();
-    if (i < end) slot[i] = place;
-    if (kept) source[place] = (int)i;
-  }
-  for (int64_t r = first[n_experts] + (int64_t)threadIdx.x; r < n; r += PLAN_WAVES * 64) source[r] = -1;
 }
 
-// segments[e][k]: the first of expert e's rows whose choice is at or behind worker k's first (choices ascend there).
+__global__ __launch_bounds__(LARGE_WAVES * 64) void plan_count_kernel(const int32_t* experts, int64_t n, int64_t per_block,
+                                                                      int n_experts, int32_t* counts) {
+  __shared__ int count[DYNB_MAX_EXPERTS];
+  for (int e = threadIdx.x; e < n_experts; e += LARGE_WAVES * 64) count[e] = 0;
+  __syncthreads();
+  const int64_t per = per_block / LARGE_WAVES, begin = blockIdx.x * per_block + (threadIdx.x >> 6) * per;
+  count_stretch(experts, begin, begin + per < n ? begin + per : n, n_experts, count);
+  __syncthreads();
+  for (int e = threadIdx.x; e < n_experts; e += LARGE_WAVES * 64) counts[(int64_t)blockIdx.x * n_experts + e] = count[e];
+}
+
+// counts: [gridDim.x][n_experts] of plan_count_kernel (not read by a single workgroup)
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void plan_kernel(const int32_t* experts, int64_t n, int64_t per_block,
+                                                          int n_experts, int bits, const int32_t* counts,
+                                                          int32_t* offsets, int32_t* slot, int32_t* source) {
+  constexpr int THREADS = WAVES * 64, EACH = (DYNB_MAX_EXPERTS + THREADS - 1) / THREADS;
+  __shared__ int place[WAVES * DYNB_MAX_EXPERTS];     // [wave][expert]: counts, then the next place
+  __shared__ int all[DYNB_MAX_EXPERTS];               // of every expert, then its first place
+  __shared__ int wave_total[WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int* const mine = place + wave * n_experts;
+  for (int i = threadIdx.x; i < WAVES * n_experts; i += THREADS) place[i] = 0;
+  __syncthreads();
+  const int64_t per = per_block / WAVES, begin = blockIdx.x * per_block + wave * per;
+  const int64_t end = begin + per < n ? begin + per : n;
+  count_stretch(experts, begin, end, n_experts, mine);
+  __syncthreads();
+  // each expert: first places of the waves relative to the workgroup's, choices of the workgroups before, of all
+  int before[EACH];
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int e = threadIdx.x + u * THREADS;
+    before[u] = 0;
+    if (e >= n_experts) continue;
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int c = place[w * n_experts + e];
+      place[w * n_experts + e] = total;
+      total += c;
+    }
+    if (gridDim.x > 1) {
+      total = 0;
+#pragma unroll 16
+      for (int b = 0; b < (int)gridDim.x; ++b) {
+        const int c = counts[(int64_t)b * n_experts + e];
+        before[u] += b < (int)blockIdx.x ? c : 0;
+        total += c;
+      }
+    }
+    all[e] = total;
+  }
+  __syncthreads();
+  // first places: each thread EACH neighbouring experts, lanes by shuffles, waves through LDS
+  int sum = 0;
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int e = threadIdx.x * EACH + u;
+    sum += e < n_experts ? all[e] : 0;
+  }
+  int upto = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d);
+    upto += lane >= d ? v : 0;
+  }
+  if (lane == 63) wave_total[wave] = upto;
+  __syncthreads();
+  int at = upto - sum, kept = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    at += w < wave ? wave_total[w] : 0;
+    kept += wave_total[w];
+  }
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int e = threadIdx.x * EACH + u;
+    if (e >= n_experts) continue;
+    const int c = all[e];
+    all[e] = at;
+    if (blockIdx.x == 0) offsets[e] = at;
+    at += c;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) offsets[n_experts] = kept;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int e = threadIdx.x + u * THREADS;
+    if (e >= n_experts) continue;
+    const int from = all[e] + before[u];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) place[w * n_experts + e] += from;
+  }
+  __syncthreads();
+  for (int64_t i0 = begin; i0 < end; i0 += 64 * AHEAD) {
+    int next[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t i = i0 + 64 * u + lane;
+      next[u] = i < end ? experts[i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (i0 + 64 * u >= end) break;
+      const int64_t i = i0 + 64 * u + lane;
+      const bool is = (uint32_t)next[u] < (uint32_t)n_experts;
+      const int e = is ? next[u] : n_experts;
+      const uint64_t same = same_key(e, bits);
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      const int to = is ? mine[e] + rank : -1;
+      wave_fence();                      // every lane has read its expert's place before the first of them moves it on
+      if (is && rank == 0) mine[e] += __popcll(same);
+      wave_fence();
+      if (i < end) slot[i] = to;
+      if (is) source[to] = (int)i;
+    }
+  }
+  for (int64_t r = kept + (int64_t)blockIdx.x * THREADS + threadIdx.x; r < n; r += (int64_t)gridDim.x * THREADS)
+    source[r] = -1;
+}
+
+// segments[e][k]: the first of expert e's rows whose choice is at or behind worker k's first (choices ascend there).  A wave
+// per pair looks at 64 places at a time: two rounds up to 4096 rows, where halving takes twelve.
 __global__ __launch_bounds__(256) void segments_kernel(const int32_t* offsets, const int32_t* source, Segs seg,
                                                        int top_k, int n_experts, int32_t* segments) {
-  const int i = blockIdx.x * 256 + threadIdx.x, e = i / (seg.K + 1), k = i - e * (seg.K + 1);
+  const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6), e = i / (seg.K + 1), k = i - e * (seg.K + 1);
   if (e >= n_experts) return;
   int lo = offsets[e], hi = offsets[e + 1];
   if (k == seg.K) lo = hi;
   const int from = k < seg.K ? seg.off[k] * top_k : 0;
   while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    if (source[mid] < from) lo = mid + 1;
-    else hi = mid;
+    const int step = (hi - lo + 63) / 64;
+    const int64_t at = lo + (int64_t)lane * step;
+    const int below = __popcll(__ballot(at < hi && source[at < hi ? at : lo] < from));   // (a prefix of the lanes)
+    if (below == 0) break;
+    const int64_t behind = lo + (int64_t)below * step;
+    lo = (int)(behind - step) + 1;
+    if (behind < hi) hi = (int)behind;
   }
-  segments[i] = lo;
+  if (lane == 0) segments[i] = lo;
 }
 
 // ---- rows ---------------------------------------------------------------------------------------------------
@@ -216,9 +313,16 @@ int launched(const char* what) {
 
 using namespace dynb;
 
+// Choices of a workgroup of the large plan: whole rounds of all its waves, and no more than MOST_BLOCKS workgroups.
+static int64_t choices_per_block(int64_t n) {
+  constexpr int64_t ROUND = LARGE_WAVES * 64 * AHEAD;
+  return round_up((n + MOST_BLOCKS - 1) / MOST_BLOCKS, ROUND);
+}
+
 extern "C" size_t dynb_route_workspace_bytes(const dynb_route_desc* d) {
   if (describe(d, "route_workspace_bytes")) return 0;
-  return 0;
+  const int64_t n = d->tokens * d->top_k, per = choices_per_block(n);
+  return n <= SMALL ? 0 : (size_t)((n + per - 1) / per * d->n_experts) * sizeof(int32_t);
 }
 
 extern "C" int dynb_route_plan(const dynb_route_desc* d, const int32_t* experts, int32_t* offsets, int32_t* slot,
@@ -228,13 +332,24 @@ extern "C" int dynb_route_plan(const dynb_route_desc* d, const int32_t* experts,
   if (!offsets || (n > 0 && (!experts || !slot || !source))) return fail(DYNB_ERR_BADARG, "route_plan: null pointer");
   if (off_by(experts, 4) || off_by(offsets, 4) || off_by(slot, 4) || off_by(source, 4))
     return fail(DYNB_ERR_BADARG, "route_plan: a pointer is not a multiple of its element's size");
-  (void)workspace;
-  (void)workspace_bytes;
+  const size_t need = dynb_route_workspace_bytes(d);
+  if (need && (!workspace || workspace_bytes < need || off_by(workspace, 16)))
+    return fail(DYNB_ERR_BADARG, "route_plan: workspace is null, too small or not 16-byte aligned");
   int bits = 0;
   while ((1 << bits) <= d->n_experts) ++bits;      // (keys 0 .. n_experts: the last one stands for a dropped choice)
+  const hipStream_t st = (hipStream_t)stream;
   Timed t(KC_ROUTE, stream, 0.0, 12.0 * n);
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_WAVES * 64), 0, (hipStream_t)stream, experts, n, d->n_experts,
-                     bits, offsets, slot, source);
+  if (n <= SMALL) {
+    hipLaunchKernelGGL(plan_kernel<SMALL_WAVES>, dim3(1), dim3(SMALL_WAVES * 64), 0, st, experts, (int64_t)n,
+                       round_up((n + SMALL_WAVES - 1) / SMALL_WAVES, 64) * SMALL_WAVES, d->n_experts, bits,
+                       (const int32_t*)nullptr, offsets, slot, source);
+  } else {
+    const int64_t per = choices_per_block(n);
+    const dim3 grid((unsigned)((n + per - 1) / per)), block(LARGE_WAVES * 64);
+    hipLaunchKernelGGL(plan_count_kernel, grid, block, 0, st, experts, (int64_t)n, per, d->n_experts, (int32_t*)workspace);
+    hipLaunchKernelGGL(plan_kernel<LARGE_WAVES>, grid, block, 0, st, experts, (int64_t)n, per, d->n_experts, bits,
+                       (const int32_t*)workspace, offsets, slot, source);
+  }
   return launched("route_plan");
 }
 
@@ -248,7 +363,7 @@ extern "C" int dynb_route_segments(const dynb_route_desc* d, const int32_t* offs
   if (off_by(offsets, 4) || off_by(source, 4) || off_by(segments, 4))
     return fail(DYNB_ERR_BADARG, "route_segments: a pointer is not a multiple of its element's size");
   Timed t(KC_ROUTE, stream, 0.0, 4.0 * d->n_experts * (K + 1));
-  hipLaunchKernelGGL(segments_kernel, dim3((d->n_experts * (K + 1) + 255) / 256), dim3(256), 0, (hipStream_t)stream,
+  hipLaunchKernelGGL(segments_kernel, dim3((d->n_experts * (K + 1) + 3) / 4), dim3(256), 0, (hipStream_t)stream,
                      offsets, source, seg, d->top_k, d->n_experts, segments);
   return launched("route_segments");
 }
