@@ -203,54 +203,75 @@ struct RowArgs {
   int cols, granules, top_k, n_experts;
 };
 
-// Sorted rows that no choice has: zeros.
-template <typename T> __device__ void clear_rows(const RowArgs& p, int64_t block, int64_t blocks) {
+// Sorted rows from `from` on, which no choice has: zeros.
+template <typename T> __device__ void clear_rows(const RowArgs& p, int64_t from, int64_t block, int64_t blocks) {
   const float zeros[GRANULE] = {};
-  for (int64_t r = p.offsets[p.n_experts] + block; r < p.choices; r += blocks)
+  for (int64_t r = from + block; r < p.choices; r += blocks)
     for (int c = threadIdx.x * GRANULE; c < p.cols; c += 256 * GRANULE)
       store_part((T*)p.out + r * p.ld_out + c, p.cols - c, zeros);
 }
 
+// The choices of a token are taken JS at a time: their slots and weights are asked for together, then their rows.
+constexpr int JS = 8;
+
 // A thread takes a granule of a token: one load, top_k stores.
 template <typename T> __global__ __launch_bounds__(256) void gather_kernel(RowArgs p) {
   const int64_t total = p.tokens * p.granules;
+  const int kept = p.offsets[p.n_experts];
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / p.granules;
-    const int c = (int)(i - t * p.granules) * GRANULE;
+    const int64_t t = total < ((int64_t)1 << 32) ? (int64_t)((uint32_t)i / (uint32_t)p.granules) : i / p.granules;
+    const int c = (int)(i - t * p.granules) * GRANULE, n = p.cols - c;
     float v[GRANULE];
-    load_part((const T*)p.in + t * p.ld_in + c, p.cols - c, v);
-    for (int j = 0; j < p.top_k; ++j) {
-      const int s = p.slot[t * p.top_k + j];
-      if (s >= 0) store_part((T*)p.out + (int64_t)s * p.ld_out + c, p.cols - c, v);
+    load_part((const T*)p.in + t * p.ld_in + c, n, v);
+    for (int j0 = 0; j0 < p.top_k; j0 += JS) {
+      int s[JS];
+#pragma unroll
+      for (int u = 0; u < JS; ++u) s[u] = j0 + u < p.top_k ? p.slot[t * p.top_k + j0 + u] : -1;
+#pragma unroll
+      for (int u = 0; u < JS; ++u)
+        if (s[u] >= 0) store_part((T*)p.out + (int64_t)s[u] * p.ld_out + c, n, v);
     }
   }
-  clear_rows<T>(p, blockIdx.x, gridDim.x);
+  clear_rows<T>(p, kept, blockIdx.x, gridDim.x);
 }
 
 // A thread takes a granule of a token: the sum over its choices, j ascending, in fp32.
 template <typename T> __global__ __launch_bounds__(256) void combine_kernel(RowArgs p) {
   const int64_t total = p.tokens * p.granules;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / p.granules;
-    const int c = (int)(i - t * p.granules) * GRANULE;
+    const int64_t t = total < ((int64_t)1 << 32) ? (int64_t)((uint32_t)i / (uint32_t)p.granules) : i / p.granules;
+    const int c = (int)(i - t * p.granules) * GRANULE, n = p.cols - c;
     float a[GRANULE] = {};
-    if (p.addend) load_part((const T*)p.addend + t * p.ld_addend + c, p.cols - c, a);
-    for (int j = 0; j < p.top_k; ++j) {
-      const int s = p.slot[t * p.top_k + j];
-      if (s < 0) continue;
-      const float w = p.weights ? p.weights[t * p.top_k + j] : 1.f;
-      float v[GRANULE];
-      load_part((const T*)p.in + (int64_t)s * p.ld_in + c, p.cols - c, v);
+    if (p.addend) load_part((const T*)p.addend + t * p.ld_addend + c, n, a);
+    for (int j0 = 0; j0 < p.top_k; j0 += JS) {
+      int s[JS];
+      float w[JS];
+      Raw<T> row[JS];
 #pragma unroll
-      for (int e = 0; e < GRANULE; ++e) a[e] += w * v[e];
+      for (int u = 0; u < JS; ++u) {
+        const bool is = j0 + u < p.top_k;
+        s[u] = is ? p.slot[t * p.top_k + j0 + u] : -1;
+        w[u] = is && p.weights ? p.weights[t * p.top_k + j0 + u] : 1.f;
+      }
+#pragma unroll
+      for (int u = 0; u < JS; ++u) row[u] = load_raw((const T*)p.in + (int64_t)s[u] * p.ld_in + c, s[u] >= 0 ? n : 0);
+#pragma unroll
+      for (int u = 0; u < JS; ++u) {
+        if (s[u] < 0) continue;
+        float v[GRANULE];
+        unpack(row[u], v);
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) a[e] += w[u] * v[e];
+      }
     }
-    store_part((T*)p.out + t * p.ld_out + c, p.cols - c, a);
+    store_part((T*)p.out + t * p.ld_out + c, n, a);
   }
 }
 
 // A wave takes a choice: its row of dsorted, and the product of the two rows.
 template <typename T> __global__ __launch_bounds__(256) void combine_grad_kernel(RowArgs p) {
   const int lane = threadIdx.x & 63;
+  const int kept = p.offsets[p.n_experts];
   for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < p.choices; i += (int64_t)gridDim.x * 4) {
     const int64_t t = i / p.top_k, s = p.slot[i];
     float dot = 0.f;
@@ -271,7 +292,7 @@ template <typename T> __global__ __launch_bounds__(256) void combine_grad_kernel
     }
     if (lane == 0) p.dweights[i] = dot;
   }
-  clear_rows<T>(p, blockIdx.x, gridDim.x);
+  clear_rows<T>(p, kept, blockIdx.x, gridDim.x);
 }
 
 int grid_for(int64_t threads) {
