@@ -13,7 +13,8 @@ namespace dynb {
 namespace {
 
 constexpr int BLOCK = DYNB_STATE_BLOCK;   // elements that share a scale: a wave, 4 neighbouring ones per lane
-constexpr int CHUNK = 4096;               // elements of a workgroup
+constexpr int U = 2;                      // blocks of a wave
+constexpr int CHUNK = 4 * U * BLOCK;      // elements of a workgroup
 
 struct Tensor {
   void *param, *copy, *s1, *s2;
@@ -43,23 +44,25 @@ struct Rule {
 };
 
 // ---- 4 neighbouring elements, of which the first n exist ------------------------------------------------------
-struct __attribute__((packed, aligned(4))) Float4 { float v[4]; };
-struct __attribute__((packed, aligned(2))) Half4 { u32x2 v; };
-struct __attribute__((packed, aligned(1))) Byte4 { uint32_t v; };
+// Every byte is used once a step: accesses pass the caches by.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+#define GLOBAL __attribute__((address_space(1)))
 
-__device__ inline void load4(const float* p, int n, float (&f)[4]) {
+__device__ inline void load4(const GLOBAL float* p, int n, float (&f)[4]) {
   if (n >= 4) {
-    const Float4 q = *(const Float4*)p;
+    const f32x4_any q = __builtin_nontemporal_load((const GLOBAL f32x4_any*)p);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = q.v[e];
+    for (int e = 0; e < 4; ++e) f[e] = q[e];
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[e] = e < n ? p[e] : 0.f;
   }
 }
-__device__ inline void load4(const bf16* p, int n, float (&f)[4]) {
+__device__ inline void load4(const GLOBAL bf16* p, int n, float (&f)[4]) {
   if (n >= 4) {
-    const u32x2 q = ((const Half4*)p)->v;
+    const u32x2_any q = __builtin_nontemporal_load((const GLOBAL u32x2_any*)p);
     f[0] = __uint_as_float(q[0] << 16);
     f[1] = __uint_as_float(q[0] & 0xffff0000u);
     f[2] = __uint_as_float(q[1] << 16);
@@ -69,38 +72,37 @@ __device__ inline void load4(const bf16* p, int n, float (&f)[4]) {
     for (int e = 0; e < 4; ++e) f[e] = e < n ? (float)p[e] : 0.f;
   }
 }
-__device__ inline void store4(float* p, int n, const float (&f)[4]) {
+__device__ inline void store4(GLOBAL float* p, int n, const float (&f)[4]) {
   if (n >= 4) {
-    Float4 q;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) q.v[e] = f[e];
-    *(Float4*)p = q;
+    const f32x4_any q = {f[0], f[1], f[2], f[3]};
+    __builtin_nontemporal_store(q, (GLOBAL f32x4_any*)p);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (e < n) p[e] = f[e];
   }
 }
-__device__ inline void store4(bf16* p, int n, const float (&f)[4]) {
+__device__ inline void store4(GLOBAL bf16* p, int n, const float (&f)[4]) {
   if (n >= 4) {
-    ((Half4*)p)->v = u32x2{two_bf16(f[0], f[1]), two_bf16(f[2], f[3])};
+    const u32x2_any q = {two_bf16(f[0], f[1]), two_bf16(f[2], f[3])};
+    __builtin_nontemporal_store(q, (GLOBAL u32x2_any*)p);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (e < n) p[e] = (bf16)f[e];
   }
 }
-__device__ inline uint32_t load_codes(const uint8_t* p, int n) {
-  if (n >= 4) return ((const Byte4*)p)->v;
+__device__ inline uint32_t load_codes(const GLOBAL uint8_t* p, int n) {
+  if (n >= 4) return __builtin_nontemporal_load((const GLOBAL u32_any*)p);
   uint32_t q = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (e < n) q |= (uint32_t)p[e] << (8 * e);
   return q;
 }
-__device__ inline void store_codes(uint8_t* p, int n, uint32_t q) {
+__device__ inline void store_codes(GLOBAL uint8_t* p, int n, uint32_t q) {
   if (n >= 4) {
-    ((Byte4*)p)->v = q;
+    __builtin_nontemporal_store(q, (GLOBAL u32_any*)p);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -134,76 +136,103 @@ __device__ inline uint32_t random_bits(uint32_t x) {
   return x ^ (x >> 16);
 }
 
+// A wave takes U blocks; all it reads is asked for before anything is used.
 template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const Chunk* chunks, Pointers grads,
                                                     int first_tensor, int64_t worker_stride, Workers workers,
                                                     Rule rule) {
   const Chunk chunk = chunks[blockIdx.x];
   const Tensor t = tensors[chunk.tensor];
-  const G* const grad = (const G*)grads.p[chunk.tensor - first_tensor];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const GLOBAL G* const grad = (const GLOBAL G*)grads.p[chunk.tensor - first_tensor];
+  GLOBAL P* const param = (GLOBAL P*)t.param;
+  GLOBAL uint8_t *const codes1 = (GLOBAL uint8_t*)t.s1, *const codes2 = (GLOBAL uint8_t*)t.s2;
+  GLOBAL float *const state1 = (GLOBAL float*)t.s1, *const state2 = (GLOBAL float*)t.s2;
+  GLOBAL float *const scale1 = (GLOBAL float*)t.c1, *const scale2 = (GLOBAL float*)t.c2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float keep = 1.f - rule.lr * t.decay;
-  for (int b = wave; b < CHUNK / BLOCK; b += 4) {
-    const int64_t begin = (int64_t)chunk.at * CHUNK + b * BLOCK;
-    if (begin >= t.n) break;
-    const int64_t i = begin + 4 * lane, left = t.n - i;
-    const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-    float p[4], m[4], v[4], g[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < workers.n; ++k) {
-      float d[4];
-      load4(grad + workers.index[k] * worker_stride + i, n, d);
+  float p[U][4], m[U][4], v[U][4], g[U][4], c1[U], c2[U];
+  uint32_t q1[U], q2[U];
+  int64_t at[U];
+  int n[U];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) g[e] += workers.w[k] * d[e];
-    }
-    load4((const P*)t.param + i, n, p);
+  for (int u = 0; u < U; ++u) {
+    const int64_t begin = (int64_t)chunk.at * CHUNK + (wave * U + u) * BLOCK, left = t.n - begin - 4 * lane;
+    at[u] = begin + 4 * lane;
+    n[u] = left >= 4 ? 4 : left > 0 ? (int)left : 0;
+    load4(param + at[u], n[u], p[u]);
     if (EIGHT) {
-      const float s1 = t.c1[begin / BLOCK], s2 = t.c2[begin / BLOCK];
-      const uint32_t q1 = load_codes((const uint8_t*)t.s1 + i, n), q2 = load_codes((const uint8_t*)t.s2 + i, n);
+      c1[u] = begin < t.n ? scale1[begin / BLOCK] : 0.f;
+      c2[u] = begin < t.n ? scale2[begin / BLOCK] : 0.f;
+      q1[u] = load_codes(codes1 + at[u], n[u]);
+      q2[u] = load_codes(codes2 + at[u], n[u]);
+    } else {
+      load4(state1 + at[u], n[u], m[u]);
+      load4(state2 + at[u], n[u], v[u]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[u][e] = 0.f;
+  }
+  constexpr int KS = 4;                   // workers whose gradients are asked for together
+  for (int k0 = 0; k0 < workers.n; k0 += KS) {
+    float d[KS][U][4];
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      if (k0 + k < workers.n)
+#pragma unroll
+        for (int u = 0; u < U; ++u) load4(grad + workers.index[k0 + k] * worker_stride + at[u], n[u], d[k][u]);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      if (k0 + k < workers.n)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) g[u][e] += workers.w[k0 + k] * d[k][u][e];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (EIGHT) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float a = decode<7>(q1 >> (8 * e) & 0x7f) * s1, r = decode<8>(q2 >> (8 * e) & 0xff) * s2;
-        m[e] = q1 >> (8 * e) & 0x80 ? -a : a;
-        v[e] = r * r;
+        const float a = decode<7>(q1[u] >> (8 * e) & 0x7f) * c1[u], r = decode<8>(q2[u] >> (8 * e) & 0xff) * c2[u];
+        m[u][e] = q1[u] >> (8 * e) & 0x80 ? -a : a;
+        v[u][e] = r * r;
       }
-    } else {
-      load4((const float*)t.s1 + i, n, m);
-      load4((const float*)t.s2 + i, n, v);
     }
     float root[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      m[e] = rule.beta1 * m[e] + rule.omb1 * g[e];
-      v[e] = rule.beta2 * v[e] + rule.omb2 * g[e] * g[e];
-      root[e] = sqrtf(v[e]);
-      p[e] = p[e] * keep - rule.lr * (m[e] * rule.inv_c1) / (root[e] * rule.inv_c2 + rule.eps);
+      m[u][e] = rule.beta1 * m[u][e] + rule.omb1 * g[u][e];
+      v[u][e] = rule.beta2 * v[u][e] + rule.omb2 * g[u][e] * g[u][e];
+      root[e] = sqrtf(v[u][e]);
+      p[u][e] = p[u][e] * keep - rule.lr * (m[u][e] * rule.inv_c1) / (root[e] * rule.inv_c2 + rule.eps);
     }
-    store4((P*)t.param + i, n, p);
-    if (t.copy) store4((bf16*)t.copy + i, n, p);
+    store4(param + at[u], n[u], p[u]);
+    if (t.copy) store4((GLOBAL bf16*)t.copy + at[u], n[u], p[u]);
     if (!EIGHT) {
-      store4((float*)t.s1 + i, n, m);
-      store4((float*)t.s2 + i, n, v);
+      store4(state1 + at[u], n[u], m[u]);
+      store4(state2 + at[u], n[u], v[u]);
       continue;
     }
     uint32_t a1 = 0, a2 = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (e >= n) m[e] = root[e] = 0.f;
-      a1 = max(a1, __float_as_uint(m[e]) & 0x7fffffffu);
+      if (e >= n[u]) m[u][e] = root[e] = 0.f;
+      a1 = max(a1, __float_as_uint(m[u][e]) & 0x7fffffffu);
       a2 = max(a2, __float_as_uint(root[e]) & 0x7fffffffu);
     }
     const Scale s1 = state_scale(wave_max(a1), Code<7>::TOP), s2 = state_scale(wave_max(a2), Code<8>::TOP);
-    uint32_t q1 = 0, q2 = 0;
+    uint32_t to1 = 0, to2 = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t u = random_bits((uint32_t)(i + e) * 0x9E3779B1u + t.ordinal * 0x7F4A7C15u + rule.seed);
-      q1 |= (encode<7>(fabsf(m[e]), s1.inv, u >> 16) | (m[e] < 0.f ? 0x80u : 0u)) << (8 * e);
-      q2 |= encode<8>(root[e], s2.inv, u & 0xffffu) << (8 * e);
+      const uint32_t r = random_bits((uint32_t)(at[u] + e) * 0x9E3779B1u + t.ordinal * 0x7F4A7C15u + rule.seed);
+      to1 |= (encode<7>(fabsf(m[u][e]), s1.inv, r >> 16) | (m[u][e] < 0.f ? 0x80u : 0u)) << (8 * e);
+      to2 |= encode<8>(root[e], s2.inv, r & 0xffffu) << (8 * e);
     }
-    store_codes((uint8_t*)t.s1 + i, n, q1);
-    store_codes((uint8_t*)t.s2 + i, n, q2);
-    if (lane == 0) {
-      t.c1[begin / BLOCK] = s1.scale;
-      t.c2[begin / BLOCK] = s2.scale;
+    store_codes(codes1 + at[u], n[u], to1);
+    store_codes(codes2 + at[u], n[u], to2);
+    if (lane == 0 && n[u] > 0) {
+      scale1[at[u] / BLOCK] = s1.scale;
+      scale2[at[u] / BLOCK] = s2.scale;
     }
   }
 }
@@ -213,24 +242,33 @@ __global__ __launch_bounds__(256) void read_states_kernel(const Tensor* tensors,
                                                           int first_tensor) {
   const Chunk chunk = chunks[blockIdx.x];
   const Tensor t = tensors[chunk.tensor];
-  T *const to1 = (T*)out.a[chunk.tensor - first_tensor], *const to2 = (T*)out.b[chunk.tensor - first_tensor];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = wave; b < CHUNK / BLOCK; b += 4) {
-    const int64_t begin = (int64_t)chunk.at * CHUNK + b * BLOCK;
-    if (begin >= t.n) break;
-    const int64_t i = begin + 4 * lane, left = t.n - i;
-    const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-    const float s1 = t.c1[begin / BLOCK], s2 = t.c2[begin / BLOCK];
-    const uint32_t q1 = load_codes((const uint8_t*)t.s1 + i, n), q2 = load_codes((const uint8_t*)t.s2 + i, n);
+  GLOBAL T *const to1 = (GLOBAL T*)out.a[chunk.tensor - first_tensor], *const to2 = (GLOBAL T*)out.b[chunk.tensor - first_tensor];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t q1[U], q2[U];
+  float c1[U], c2[U];
+  int64_t at[U];
+  int n[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t begin = (int64_t)chunk.at * CHUNK + (wave * U + u) * BLOCK, left = t.n - begin - 4 * lane;
+    at[u] = begin + 4 * lane;
+    n[u] = left >= 4 ? 4 : left > 0 ? (int)left : 0;
+    c1[u] = begin < t.n ? ((const GLOBAL float*)t.c1)[begin / BLOCK] : 0.f;
+    c2[u] = begin < t.n ? ((const GLOBAL float*)t.c2)[begin / BLOCK] : 0.f;
+    q1[u] = load_codes((const GLOBAL uint8_t*)t.s1 + at[u], n[u]);
+    q2[u] = load_codes((const GLOBAL uint8_t*)t.s2 + at[u], n[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
     float m[4], v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = decode<7>(q1 >> (8 * e) & 0x7f) * s1, r = decode<8>(q2 >> (8 * e) & 0xff) * s2;
-      m[e] = q1 >> (8 * e) & 0x80 ? -a : a;
+      const float a = decode<7>(q1[u] >> (8 * e) & 0x7f) * c1[u], r = decode<8>(q2[u] >> (8 * e) & 0xff) * c2[u];
+      m[e] = q1[u] >> (8 * e) & 0x80 ? -a : a;
       v[e] = r * r;
     }
-    store4(to1 + i, n, m);
-    store4(to2 + i, n, v);
+    store4(to1 + at[u], n[u], m);
+    store4(to2 + at[u], n[u], v);
   }
 }
 
