@@ -276,9 +276,9 @@ typedef struct {
  *   residual: rows, or NULL (s = x);  gain: fp32 [cols], or NULL (ones);  sum: receives s, or NULL;
  *   y: rows of dtype or of 8 bits;  rstd: receives fp32 [rows], or NULL;
  *   scales: fp32 [rows][ceil(cols / scale_block)], 8-bit outputs only: with a = max |y| of the block and
- *   q = 448 or 127, scale = a / q and y is stored as round(y / scale) (nearest-even).  A block of zeros
- *   has scale 0; a block with an infinity or NaN has scale NaN and stored zeros, so that what it stands
- *   for is NaN.
+ *   q = 448 or 127, scale = a / q and y is stored as round(y / scale) (nearest-even).  A block whose
+ *   a is below 2^-100 has scale 0 and stored zeros; one with an infinity or NaN has scale NaN, so that all
+ *   of it stands for NaN.
  * sum and a y of dtype may be x's or residual's memory (same pointer, same ld).  rows >= 0.
  * DYNB_ERR_BADARG: null pointers, unknown type, cols, scale_block, eps (negative or not finite), an ld
  * below cols, a pointer that is not a multiple of its element's size, rows beyond 2^31 - 1. */

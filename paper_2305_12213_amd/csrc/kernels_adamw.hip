@@ -118,17 +118,21 @@ template <int MAG> struct Code {
   static constexpr int SHIFT = MAG == 7 ? 20 : 19;
   static constexpr float TOP = MAG == 7 ? 1.875f : 1.9375f;
 };
-template <int MAG> __device__ inline float decode(uint32_t code) {
-  return __uint_as_float((code << Code<MAG>::SHIFT) + LOW_BITS) - 0x1p-15f;
+// byte `e` of q; low = 2^-15 * scale (a power of two times it, so that the product below rounds once)
+template <int MAG> __device__ inline float decode(uint32_t q, int e, float scale, float low) {
+  constexpr int SHIFT = Code<MAG>::SHIFT;
+  constexpr uint32_t MASK = ((1u << MAG) - 1) << SHIFT;
+  const uint32_t bits = (8 * e > SHIFT ? q >> (8 * e - SHIFT) : q << (SHIFT - 8 * e)) & MASK;
+  return __builtin_fmaf(__uint_as_float(bits + LOW_BITS), scale, -low);
 }
-// u16: 16 random bits, 65536ths of a step
+__device__ inline float signed_as(float magnitude, uint32_t q, int e) {       // bit 7 of byte `e`
+  return __uint_as_float(__float_as_uint(magnitude) ^ (q << (24 - 8 * e) & 0x80000000u));
+}
+// u16: 16 random bits, 65536ths of a step.  (A factor of 0 gives code 0; of a block with an infinity or NaN it does not
+// matter which code: its scale is NaN.)
 template <int MAG> __device__ inline uint32_t encode(float magnitude, float inv, uint32_t u16) {
-  const uint32_t bits = __float_as_uint(magnitude * inv + 0x1p-15f) - LOW_BITS + (u16 << (Code<MAG>::SHIFT - 16));
-  return inv > 0.f ? min(bits >> Code<MAG>::SHIFT, (1u << MAG) - 1) : 0u;
-}
-__device__ inline Scale state_scale(uint32_t amax_bits, float top) {
-  if (amax_bits < (27u << 23)) return {0.f, 0.f};   // below 2^-100
-  return scale_of(amax_bits, top);
+  const uint32_t bits = __float_as_uint(__builtin_fmaf(magnitude, inv, 0x1p-15f)) - LOW_BITS + (u16 << (Code<MAG>::SHIFT - 16));
+  return min(bits >> Code<MAG>::SHIFT, (1u << MAG) - 1);
 }
 __device__ inline uint32_t random_bits(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x6A09E667u;
@@ -136,6 +140,8 @@ __device__ inline uint32_t random_bits(uint32_t x) {
   return x ^ (x >> 16);
 }
 
+// The root and the reciprocal are the hardware's (off by a unit in the last place of a term that is small beside the
+// parameter; a v below 2^-126 counts as zero): with the correctly rounded ones the 8-bit step is bound by its arithmetic.
 // A wave takes U blocks; all it reads is asked for before anything is used.
 template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const Chunk* chunks, Pointers grads,
@@ -193,8 +199,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
     if (EIGHT) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float a = decode<7>(q1[u] >> (8 * e) & 0x7f) * c1[u], r = decode<8>(q2[u] >> (8 * e) & 0xff) * c2[u];
-        m[u][e] = q1[u] >> (8 * e) & 0x80 ? -a : a;
+        const float r = decode<8>(q2[u], e, c2[u], c2[u] * 0x1p-15f);
+        m[u][e] = signed_as(decode<7>(q1[u], e, c1[u], c1[u] * 0x1p-15f), q1[u], e);
         v[u][e] = r * r;
       }
     }
@@ -203,8 +209,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
     for (int e = 0; e < 4; ++e) {
       m[u][e] = rule.beta1 * m[u][e] + rule.omb1 * g[u][e];
       v[u][e] = rule.beta2 * v[u][e] + rule.omb2 * g[u][e] * g[u][e];
-      root[e] = sqrtf(v[u][e]);
-      p[u][e] = p[u][e] * keep - rule.lr * (m[u][e] * rule.inv_c1) / (root[e] * rule.inv_c2 + rule.eps);
+      root[e] = __builtin_amdgcn_sqrtf(v[u][e]);
+      const float by = __builtin_amdgcn_rcpf(root[e] * rule.inv_c2 + rule.eps);
+      p[u][e] = p[u][e] * keep - (rule.lr * rule.inv_c1) * (m[u][e] * by);
     }
     store4(param + at[u], n[u], p[u]);
     if (t.copy) store4((GLOBAL bf16*)t.copy + at[u], n[u], p[u]);
@@ -213,19 +220,18 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
       store4(state2 + at[u], n[u], v[u]);
       continue;
     }
-    uint32_t a1 = 0, a2 = 0;
+    uint32_t a1 = 0, a2 = 0;               // (elements that do not exist are zeros)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (e >= n[u]) m[u][e] = root[e] = 0.f;
       a1 = max(a1, __float_as_uint(m[u][e]) & 0x7fffffffu);
-      a2 = max(a2, __float_as_uint(root[e]) & 0x7fffffffu);
+      a2 = max(a2, __float_as_uint(root[e]));
     }
-    const Scale s1 = state_scale(wave_max(a1), Code<7>::TOP), s2 = state_scale(wave_max(a2), Code<8>::TOP);
+    const Scale s1 = scale_of(wave_max(a1), Code<7>::TOP), s2 = scale_of(wave_max(a2), Code<8>::TOP);
     uint32_t to1 = 0, to2 = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t r = random_bits((uint32_t)(at[u] + e) * 0x9E3779B1u + t.ordinal * 0x7F4A7C15u + rule.seed);
-      to1 |= (encode<7>(fabsf(m[u][e]), s1.inv, r >> 16) | (m[u][e] < 0.f ? 0x80u : 0u)) << (8 * e);
+      to1 |= (encode<7>(fabsf(m[u][e]), s1.inv, r >> 16) | (__float_as_uint(m[u][e]) >> 24 & 0x80u)) << (8 * e);
       to2 |= encode<8>(root[e], s2.inv, r & 0xffffu) << (8 * e);
     }
     store_codes(codes1 + at[u], n[u], to1);
@@ -263,8 +269,8 @@ __global__ __launch_bounds__(256) void read_states_kernel(const Tensor* tensors,
     float m[4], v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = decode<7>(q1[u] >> (8 * e) & 0x7f) * c1[u], r = decode<8>(q2[u] >> (8 * e) & 0xff) * c2[u];
-      m[e] = q1[u] >> (8 * e) & 0x80 ? -a : a;
+      const float r = decode<8>(q2[u], e, c2[u], c2[u] * 0x1p-15f);
+      m[e] = signed_as(decode<7>(q1[u], e, c1[u], c1[u] * 0x1p-15f), q1[u], e);
       v[e] = r * r;
     }
     store4(to1 + at[u], n[u], m);

@@ -22,9 +22,9 @@ struct NormArgs {
   float eps;
 };
 
-// One value in 8 bits.  (An 8-bit block that holds an infinity or NaN has factor 0: 0 * inf is kept out.)
+// One value in 8 bits.  (Of a block with an infinity or NaN it does not matter which: its scale is NaN.)
 template <int OUT> __device__ inline uint8_t eight_bits(float v, float inv) {
-  const float t = inv > 0.f ? v * inv : 0.f;
+  const float t = v * inv;
   if (OUT == DYNB_OUT_INT8) return (uint8_t)(int8_t)rintf(t);
   return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(t, t, 0, false) & 0xff);
 }
@@ -37,7 +37,7 @@ __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE],
   for (int h = 0; h < 2; ++h) {
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = inv > 0.f ? f[4 * h + e] * inv : 0.f;
+    for (int e = 0; e < 4; ++e) v[e] = f[4 * h + e] * inv;
     if (OUT == DYNB_OUT_FP8) {
       q[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
     } else {

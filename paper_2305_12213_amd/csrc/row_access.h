@@ -186,13 +186,15 @@ __device__ inline uint32_t block_max(uint32_t v, uint32_t* red) {
 }
 
 // Values of 8 bits with a scale: the largest magnitude's bits (a NaN's are above an infinity's) give scale and factor.
+// Below 2^-100 a block counts as zeros: the factor could overflow.
 struct Scale {
   float scale, inv;
 };
 __device__ inline Scale scale_of(uint32_t amax_bits, float top) {
   if (amax_bits >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.f};
-  const float a = __uint_as_float(amax_bits), s = a / top;
-  return {s, s > 0.f ? top / a : 0.f};
+  if (amax_bits < (27u << 23)) return {0.f, 0.f};
+  const float a = __uint_as_float(amax_bits);
+  return {a * (1.f / top), top * __builtin_amdgcn_rcpf(a)};
 }
 
 }  // namespace dynb
