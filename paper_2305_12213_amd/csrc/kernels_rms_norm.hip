@@ -20,6 +20,7 @@ struct NormArgs {
   int64_t ld_x, ld_residual, ld_sum, ld_y;
   int rows, cols, scale_block, n_blocks;
   float eps;
+  double bytes;                            // of the call
 };
 
 // One value in 8 bits.  (Of a block with an infinity or NaN it does not matter which: its scale is NaN.)
@@ -30,7 +31,7 @@ template <int OUT> __device__ inline uint8_t eight_bits(float v, float inv) {
 }
 
 // 8 neighbouring values, the first n of them.
-template <int OUT>
+template <int OUT, bool PAST>
 __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE], float inv) {
   u32x2 q;
 #pragma unroll
@@ -47,7 +48,8 @@ __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE],
     }
   }
   if (n >= GRANULE) {
-    ((Any8*)p)->v = q;
+    if (PAST) __builtin_nontemporal_store((u32x2_any)q, (u32x2_any*)p);
+    else *(u32x2_any*)p = q;
   } else {
 #pragma unroll
     for (int e = 0; e < GRANULE; ++e)
@@ -119,7 +121,7 @@ __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
 // Rows that fit in the registers of W waves, N granules per thread: one read, one write.  (W = 1: four rows per
 // workgroup, no barrier.)  A thread keeps its part of the gain over all rows of the workgroup.  group: lanes that share a
 // scale (a power of two), 0 where the whole row does.
-template <typename T, int OUT, int W, int N>
+template <typename T, int OUT, int W, int N, bool PAST>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArgs p, int group) {
   constexpr int PER = W == 1 ? 4 : 1;      // rows of a workgroup
   constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
@@ -132,8 +134,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (t + i * 64 * W) * GRANULE;
-      x[i] = load_raw((const T*)p.x + row * p.ld_x + c, p.cols - c);
-      if (p.residual) res[i] = load_raw((const T*)p.residual + row * p.ld_residual + c, p.cols - c);
+      x[i] = load_raw<PAST>((const T*)p.x + row * p.ld_x + c, p.cols - c);
+      if (p.residual) res[i] = load_raw<PAST>((const T*)p.residual + row * p.ld_residual + c, p.cols - c);
     }
   };
   if (r < p.rows) ask(r);
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (t + i * 64 * W) * GRANULE;
-      if (p.sum && c < p.cols) store_part((T*)p.sum + r * p.ld_sum + c, p.cols - c, s[i]);
+      if (p.sum && c < p.cols) store_part<PAST>((T*)p.sum + r * p.ld_sum + c, p.cols - c, s[i]);
       float g[GRANULE];
       unpack(gain[i], g);
 #pragma unroll
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
         s[i][e] *= rstd * g[e];
         if (c + e >= p.cols) s[i][e] = 0.f;
       }
-      if (OUT == DYNB_OUT_SAME && c < p.cols) store_part((T*)p.y + r * p.ld_y + c, p.cols - c, s[i]);
+      if (OUT == DYNB_OUT_SAME && c < p.cols) store_part<PAST>((T*)p.y + r * p.ld_y + c, p.cols - c, s[i]);
     }
     const int64_t now = r;
     if (r + (int64_t)gridDim.x * PER < p.rows) ask(r + (int64_t)gridDim.x * PER);
@@ -206,7 +208,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
         scale = scale_of(group_max(amax, group), TOP);
         if ((t & (group - 1)) == 0 && c < p.cols) p.scales[now * p.n_blocks + c / p.scale_block] = scale.scale;
       }
-      if (c < p.cols) store_eight<OUT>((uint8_t*)p.y + now * p.ld_y + c, p.cols - c, s[i], scale.inv);
+      if (c < p.cols) store_eight<OUT, PAST>((uint8_t*)p.y + now * p.ld_y + c, p.cols - c, s[i], scale.inv);
     }
   }
 }
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(256) void rms_norm_gain_grad_kernel(NormGradArgs p,
 }
 
 // A thread takes 8 neighbouring values of a row at a time.
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void dequantise_kernel(NormArgs p, int out, T* to, int64_t ld_to) {
   const int granules = (p.cols + GRANULE - 1) / GRANULE;
   const int64_t total = (int64_t)p.rows * granules;
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(256) void dequantise_kernel(NormArgs p, int out, T*
     const uint8_t* y = (const uint8_t*)p.y + r * p.ld_y + c;
     const float scale = p.scales[r * p.n_blocks + (p.n_blocks == 1 ? 0 : c / p.scale_block)];
     u32x2 q = {0, 0};
-    if (n >= GRANULE) q = ((const Any8*)y)->v;
+    if (n >= GRANULE) q = PAST ? (u32x2)__builtin_nontemporal_load((const u32x2_any*)y) : (u32x2)*(const u32x2_any*)y;
     else
       for (int e = 0; e < n; ++e) q[e / 4] |= (uint32_t)y[e] << (8 * (e & 3));
     float f[GRANULE];
@@ -270,7 +272,7 @@ __global__ __launch_bounds__(256) void dequantise_kernel(NormArgs p, int out, T*
       const uint32_t b = q[e / 4] >> (8 * (e & 3));
       f[e] = (out == DYNB_OUT_INT8 ? (float)(int8_t)b : __builtin_amdgcn_cvt_f32_fp8(b, 0)) * scale;
     }
-    store_part(to + r * ld_to + c, n, f);
+    store_part<PAST>(to + r * ld_to + c, n, f);
   }
 }
 
@@ -308,10 +310,13 @@ int resident(int64_t units, int threads) {
   return (int)(units < most ? units : most);
 }
 
+bool past_caches(const NormArgs& a) { return a.bytes > 64e6; }
+
 template <typename T, int OUT, int W, int N> void launch_norm_as(const NormArgs& a, int group, hipStream_t st) {
   constexpr int THREADS = W == 1 ? 256 : 64 * W, PER = W == 1 ? 4 : 1;
-  hipLaunchKernelGGL((rms_norm_kernel<T, OUT, W, N>), dim3(resident((a.rows + PER - 1) / PER, THREADS)), dim3(THREADS), 0,
-                     st, a, group);
+  const dim3 grid(resident((a.rows + PER - 1) / PER, THREADS)), block(THREADS);
+  if (past_caches(a)) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, W, N, true>), grid, block, 0, st, a, group);
+  else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, W, N, false>), grid, block, 0, st, a, group);
 }
 
 template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream_t st) {
@@ -345,7 +350,7 @@ struct Chunks {
   int rows;                               // of a chunk, the last one of a worker may be shorter
   int first[DYNB_MAX_WORKERS + 1];        // of each worker's chunks
 };
-template <typename T, int W, int N>
+template <typename T, int W, int N, bool PAST>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(NormGradArgs p, Segs seg, Chunks ch,
                                                                              float* partial) {
   constexpr int PER = W == 1 ? 4 : 1, COLS = 64 * W * N * GRANULE;
@@ -363,9 +368,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (t + i * 64 * W) * GRANULE;
-      s[i] = load_raw((const T*)p.sum + r * p.ld_sum + c, p.cols - c);
-      dy[i] = load_raw((const T*)p.dy + r * p.ld_dy + c, p.cols - c);
-      if (p.dsum) ds[i] = load_raw((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c);
+      s[i] = load_raw<PAST>((const T*)p.sum + r * p.ld_sum + c, p.cols - c);
+      dy[i] = load_raw<PAST>((const T*)p.dy + r * p.ld_dy + c, p.cols - c);
+      if (p.dsum) ds[i] = load_raw<PAST>((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c);
     }
   };
   int r = begin + wave;
@@ -423,7 +428,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
       }
-      store_part((T*)p.dx + (int64_t)r * p.ld_dx + c, p.cols - c, a);
+      store_part<PAST>((T*)p.dx + (int64_t)r * p.ld_dx + c, p.cols - c, a);
     }
   }
   if (!p.dgain) return;
@@ -495,8 +500,11 @@ int chunks_of(const Segs& seg, int cols, Chunks& ch) {
 
 template <typename T, int W, int N>
 void launch_norm_grad_as(const NormGradArgs& a, const Segs& seg, const Chunks& ch, float* partial, hipStream_t st) {
-  hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, N>), dim3(ch.first[seg.K]), dim3(W == 1 ? 256 : 64 * W), 0, st, a, seg,
-                     ch, partial);
+  const dim3 grid(ch.first[seg.K]), block(W == 1 ? 256 : 64 * W);
+  if ((double)a.rows * a.cols * sizeof(T) * (3 + (a.dsum != nullptr)) > 64e6)
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, N, true>), grid, block, 0, st, a, seg, ch, partial);
+  else
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, N, false>), grid, block, 0, st, a, seg, ch, partial);
 }
 
 template <typename T>
@@ -577,8 +585,8 @@ extern "C" int dynb_rms_norm(const dynb_rms_norm_desc* d, int64_t rows, const vo
   a.rstd = rstd;
   a.rows = (int)rows;
   const double n = (double)rows * d->cols;
-  Timed t(KC_NORM, stream, 8.0 * n,
-          n * (size * (1 + (residual != nullptr) + (sum != nullptr)) + (d->out == DYNB_OUT_SAME ? size : 1)));
+  a.bytes = n * (size * (1 + (residual != nullptr) + (sum != nullptr)) + (d->out == DYNB_OUT_SAME ? size : 1));
+  Timed t(KC_NORM, stream, 8.0 * n, a.bytes);
   if (d->dtype == DYNB_F32) launch_norm<float>(a, d->out, (hipStream_t)stream);
   else launch_norm<bf16>(a, d->out, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "rms_norm launch failed");
@@ -606,11 +614,16 @@ extern "C" int dynb_dequantise(const dynb_rms_norm_desc* d, int64_t rows, const 
   a.rows = (int)rows;
   if (!ld_out) ld_out = d->cols;
   const dim3 grid(resident((rows * ((d->cols + GRANULE - 1) / GRANULE) + 255) / 256, 256)), block(256);
-  Timed t(KC_NORM, stream, (double)rows * d->cols, (double)rows * d->cols * (out_dtype == DYNB_F32 ? 5 : 3));
-  if (out_dtype == DYNB_F32)
-    hipLaunchKernelGGL(dequantise_kernel<float>, grid, block, 0, (hipStream_t)stream, a, d->out, (float*)out, ld_out);
-  else
-    hipLaunchKernelGGL(dequantise_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a, d->out, (bf16*)out, ld_out);
+  const hipStream_t st = (hipStream_t)stream;
+  a.bytes = (double)rows * d->cols * (out_dtype == DYNB_F32 ? 5 : 3);
+  Timed t(KC_NORM, stream, (double)rows * d->cols, a.bytes);
+  if (out_dtype == DYNB_F32) {
+    if (past_caches(a)) hipLaunchKernelGGL((dequantise_kernel<float, true>), grid, block, 0, st, a, d->out, (float*)out, ld_out);
+    else hipLaunchKernelGGL((dequantise_kernel<float, false>), grid, block, 0, st, a, d->out, (float*)out, ld_out);
+  } else {
+    if (past_caches(a)) hipLaunchKernelGGL((dequantise_kernel<bf16, true>), grid, block, 0, st, a, d->out, (bf16*)out, ld_out);
+    else hipLaunchKernelGGL((dequantise_kernel<bf16, false>), grid, block, 0, st, a, d->out, (bf16*)out, ld_out);
+  }
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "dequantise launch failed");
 }
 

@@ -204,75 +204,96 @@ struct RowArgs {
 };
 
 // Sorted rows from `from` on, which no choice has: zeros.
-template <typename T> __device__ void clear_rows(const RowArgs& p, int64_t from, int64_t block, int64_t blocks) {
+template <typename T> __device__ void clear_rows(const RowArgs& p, int64_t from) {
   const float zeros[GRANULE] = {};
-  for (int64_t r = from + block; r < p.choices; r += blocks)
+  for (int64_t r = from + blockIdx.x; r < p.choices; r += gridDim.x)
     for (int c = threadIdx.x * GRANULE; c < p.cols; c += 256 * GRANULE)
       store_part((T*)p.out + r * p.ld_out + c, p.cols - c, zeros);
+}
+
+// L lanes take a row, a granule each and another one L granules on; 256 / L rows per workgroup.  From 64 lanes on a row
+// is the same in the whole wave, and what belongs to it (slots, weights) is read by scalar instructions.
+template <int L> __device__ inline int64_t row_of_thread() {
+  const int64_t r = (int64_t)blockIdx.x * (256 / L);
+  return r + (L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L);
 }
 
 // The choices of a token are taken JS at a time: their slots and weights are asked for together, then their rows.
 constexpr int JS = 8;
 
-// A thread takes a granule of a token: one load, top_k stores.
-template <typename T> __global__ __launch_bounds__(256) void gather_kernel(RowArgs p) {
-  const int64_t total = p.tokens * p.granules;
+// One load and top_k stores.
+template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void gather_kernel(RowArgs p) {
   const int kept = p.offsets[p.n_experts];
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = total < ((int64_t)1 << 32) ? (int64_t)((uint32_t)i / (uint32_t)p.granules) : i / p.granules;
-    const int c = (int)(i - t * p.granules) * GRANULE, n = p.cols - c;
-    float v[GRANULE];
-    load_part((const T*)p.in + t * p.ld_in + c, n, v);
-    for (int j0 = 0; j0 < p.top_k; j0 += JS) {
-      int s[JS];
+  for (int64_t t = row_of_thread<L>(); t < p.tokens; t += (int64_t)gridDim.x * (256 / L))
+    for (int c = threadIdx.x % L * GRANULE; c < p.cols; c += L * GRANULE) {
+      const int n = p.cols - c;
+      float v[GRANULE];
+      unpack(load_raw<PAST>((const T*)p.in + t * p.ld_in + c, n), v);
+      for (int j0 = 0; j0 < p.top_k; j0 += JS) {
+        int s[JS];
 #pragma unroll
-      for (int u = 0; u < JS; ++u) s[u] = j0 + u < p.top_k ? p.slot[t * p.top_k + j0 + u] : -1;
+        for (int u = 0; u < JS; ++u) s[u] = j0 + u < p.top_k ? p.slot[t * p.top_k + j0 + u] : -1;
 #pragma unroll
-      for (int u = 0; u < JS; ++u)
-        if (s[u] >= 0) store_part((T*)p.out + (int64_t)s[u] * p.ld_out + c, n, v);
-    }
-  }
-  clear_rows<T>(p, kept, blockIdx.x, gridDim.x);
-}
-
-// A thread takes a granule of a token: the sum over its choices, j ascending, in fp32.
-template <typename T> __global__ __launch_bounds__(256) void combine_kernel(RowArgs p) {
-  const int64_t total = p.tokens * p.granules;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = total < ((int64_t)1 << 32) ? (int64_t)((uint32_t)i / (uint32_t)p.granules) : i / p.granules;
-    const int c = (int)(i - t * p.granules) * GRANULE, n = p.cols - c;
-    float a[GRANULE] = {};
-    if (p.addend) load_part((const T*)p.addend + t * p.ld_addend + c, n, a);
-    for (int j0 = 0; j0 < p.top_k; j0 += JS) {
-      int s[JS];
-      float w[JS];
-      Raw<T> row[JS];
-#pragma unroll
-      for (int u = 0; u < JS; ++u) {
-        const bool is = j0 + u < p.top_k;
-        s[u] = is ? p.slot[t * p.top_k + j0 + u] : -1;
-        w[u] = is && p.weights ? p.weights[t * p.top_k + j0 + u] : 1.f;
-      }
-#pragma unroll
-      for (int u = 0; u < JS; ++u) row[u] = load_raw((const T*)p.in + (int64_t)s[u] * p.ld_in + c, s[u] >= 0 ? n : 0);
-#pragma unroll
-      for (int u = 0; u < JS; ++u) {
-        if (s[u] < 0) continue;
-        float v[GRANULE];
-        unpack(row[u], v);
-#pragma unroll
-        for (int e = 0; e < GRANULE; ++e) a[e] += w[u] * v[e];
+        for (int u = 0; u < JS; ++u)
+          if (s[u] >= 0) store_part<PAST>((T*)p.out + (int64_t)s[u] * p.ld_out + c, n, v);
       }
     }
-    store_part((T*)p.out + t * p.ld_out + c, n, a);
-  }
+  clear_rows<T>(p, kept);
 }
 
-// A wave takes a choice: its row of dsorted, and the product of the two rows.
-template <typename T> __global__ __launch_bounds__(256) void combine_grad_kernel(RowArgs p) {
+// The sum over a token's choices, j ascending, in fp32.
+template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void combine_kernel(RowArgs p) {
+  for (int64_t t = row_of_thread<L>(); t < p.tokens; t += (int64_t)gridDim.x * (256 / L))
+    for (int c = threadIdx.x % L * GRANULE; c < p.cols; c += L * GRANULE) {
+      const int n = p.cols - c;
+      float a[GRANULE] = {};
+      Raw<T> add;
+      if (p.addend) add = load_raw<PAST>((const T*)p.addend + t * p.ld_addend + c, n);
+      for (int j0 = 0; j0 < p.top_k; j0 += JS) {
+        int s[JS];
+        float w[JS];
+        Raw<T> row[JS];
+#pragma unroll
+        for (int u = 0; u < JS; ++u) {
+          const bool is = j0 + u < p.top_k;
+          s[u] = is ? p.slot[t * p.top_k + j0 + u] : -1;
+          w[u] = is && p.weights ? p.weights[t * p.top_k + j0 + u] : 1.f;
+        }
+#pragma unroll
+        for (int u = 0; u < JS; ++u)
+          if (s[u] >= 0) row[u] = load_raw<PAST>((const T*)p.in + (int64_t)s[u] * p.ld_in + c, n);
+        if (j0 == 0 && p.addend) unpack(add, a);
+#pragma unroll
+        for (int u = 0; u < JS; ++u) {
+          if (s[u] < 0) continue;
+          float v[GRANULE];
+          unpack(row[u], v);
+#pragma unroll
+          for (int e = 0; e < GRANULE; ++e) a[e] += w[u] * v[e];
+        }
+      }
+      store_part<PAST>((T*)p.out + t * p.ld_out + c, n, a);
+    }
+}
+
+// Sum over L neighbouring lanes (L <= 64), the same in all of them.
+template <int L> __device__ inline float lanes_sum(float v) {
+  if (L == 64) return wave_sum(v);
+  v += from_lane<DPP_XOR1>(v);
+  v += from_lane<DPP_XOR2>(v);
+  v += from_lane<DPP_HALF_MIRROR>(v);
+  v += from_lane<DPP_MIRROR>(v);
+  if (L == 32) v += __shfl_xor(v, 16);
+  return v;
+}
+
+// A wave takes a choice: its row of dsorted, and the product of the two rows.  For calls that the caches hold, where more and
+// shorter chains count (the gradient is read again for each choice): 1024 tokens of 4 choices of 2048 bf16 columns and the
+// combination of the rows' gradient behind it 13.8 us, by tokens 16.2.
+template <typename T> __global__ __launch_bounds__(256) void choice_grad_kernel(RowArgs p) {
   const int lane = threadIdx.x & 63;
   const int kept = p.offsets[p.n_experts];
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < p.choices; i += (int64_t)gridDim.x * 4) {
+  for (int64_t i = row_of_thread<64>(); i < p.choices; i += (int64_t)gridDim.x * 4) {
     const int64_t t = i / p.top_k, s = p.slot[i];
     float dot = 0.f;
     if (s >= 0) {
@@ -292,12 +313,113 @@ template <typename T> __global__ __launch_bounds__(256) void combine_grad_kernel
     }
     if (lane == 0) p.dweights[i] = dot;
   }
-  clear_rows<T>(p, kept, blockIdx.x, gridDim.x);
+  clear_rows<T>(p, kept);
 }
 
-int grid_for(int64_t threads) {
-  const int64_t blocks = (threads + 255) / 256;
-  return (int)(blocks < 1 ? 1 : blocks < (1 << 20) ? blocks : 1 << 20);
+// A token's rows of dsorted, and the product of its gradient with each of its choices' rows: the gradient is read once for
+// JS choices.  For calls beyond the caches: 8192 tokens of 2 choices of 4096 bf16 columns 60 us (5.6 TB/s), by choices 68.
+template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void combine_grad_kernel(RowArgs p) {
+  constexpr int WAVES = L > 64 ? L / 64 : 1;          // of a row
+  __shared__ float part[4][JS];
+  const int kept = p.offsets[p.n_experts];
+  const int64_t mine = row_of_thread<L>() - (int64_t)blockIdx.x * (256 / L);
+  for (int64_t first = (int64_t)blockIdx.x * (256 / L); first < p.tokens; first += (int64_t)gridDim.x * (256 / L)) {
+    const int64_t t = first + mine;
+    const bool live = t < p.tokens;
+    for (int j0 = 0; j0 < p.top_k; j0 += JS) {
+      int s[JS];
+      float w[JS], dot[JS];
+#pragma unroll
+      for (int u = 0; u < JS; ++u) {
+        s[u] = live && j0 + u < p.top_k ? p.slot[t * p.top_k + j0 + u] : -1;
+        w[u] = s[u] >= 0 ? p.weights[t * p.top_k + j0 + u] : 0.f;
+        dot[u] = 0.f;
+      }
+      for (int c = threadIdx.x % L * GRANULE; live && c < p.cols; c += L * GRANULE) {
+        const int n = p.cols - c;
+        Raw<T> row[JS];
+        float g[GRANULE];
+        const Raw<T> dout = load_raw((const T*)p.in + t * p.ld_in + c, n);
+#pragma unroll
+        for (int u = 0; u < JS; ++u)
+          if (s[u] >= 0) row[u] = load_raw<PAST>((const T*)p.sorted + (int64_t)s[u] * p.ld_sorted + c, n);
+        unpack(dout, g);
+#pragma unroll
+        for (int u = 0; u < JS; ++u) {
+          if (s[u] < 0) continue;
+          float y[GRANULE];
+          unpack(row[u], y);
+#pragma unroll
+          for (int e = 0; e < GRANULE; ++e) {
+            dot[u] += g[e] * y[e];
+            y[e] = w[u] * g[e];
+          }
+          store_part<PAST>((T*)p.out + (int64_t)s[u] * p.ld_out + c, n, y);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < JS; ++u)
+        if (j0 + u < p.top_k) dot[u] = lanes_sum<(L < 64 ? L : 64)>(dot[u]);
+      if (WAVES > 1) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+          for (int u = 0; u < JS; ++u) part[wave][u] = dot[u];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < JS; ++u) {
+          dot[u] = part[wave / WAVES * WAVES][u];
+#pragma unroll
+          for (int v = 1; v < WAVES; ++v) dot[u] += part[wave / WAVES * WAVES + v][u];
+        }
+        __syncthreads();
+      }
+      if (threadIdx.x % L == 0 && live)
+#pragma unroll
+        for (int u = 0; u < JS; ++u)
+          if (j0 + u < p.top_k) p.dweights[t * p.top_k + j0 + u] = dot[u];
+    }
+  }
+  clear_rows<T>(p, kept);
+}
+
+// Workgroups for rows of L lanes.
+int grid_of(int64_t rows, int lanes) {
+  const int64_t per = 256 / lanes, blocks = (rows + per - 1) / per;
+  return (int)(blocks < (1 << 20) ? blocks : 1 << 20);
+}
+
+// Lanes of a row (of 8 elements each): as few as hold it up to 32, else the one of 64, 128 and 256 that leaves the fewest idle in the last round.
+int lanes_of(int granules) {
+  if (granules <= 32) return granules <= 16 ? 16 : 32;
+  int best = 256;
+  for (int l : {128, 64})
+    if ((granules + l - 1) / l * l < (granules + best - 1) / best * best) best = l;
+  return best;
+}
+
+// Calls of more bytes than the caches keep until the next one reads them pass them by.  Sorting and combination of 2048
+// columns in bf16, 8 choices: 1024 tokens (38 and 42 MB) 30.2 us either way, 2048 tokens 46 us past the caches and 55 through
+// them, 16384 tokens 245 and 279; gradients of 4 choices: 1024 tokens (38 and 21 MB) 15.8 and 13.8, 2048 27.0 and 30.2.
+bool past_caches(double bytes) { return bytes > 64e6; }
+
+#define ROUTE_LAUNCH(name, L) \
+  hipLaunchKernelGGL((name##_kernel<T, L, PAST>), dim3(grid_of(a.tokens, L)), dim3(256), 0, st, a)
+#define ROUTE_LAUNCHES(name)                                                 \
+  template <typename T, bool PAST> void launch_##name(const RowArgs& a, hipStream_t st) { \
+    switch (lanes_of(a.granules)) {                                          \
+      case 16: ROUTE_LAUNCH(name, 16); break;                                \
+      case 32: ROUTE_LAUNCH(name, 32); break;                                \
+      case 64: ROUTE_LAUNCH(name, 64); break;                                \
+      case 128: ROUTE_LAUNCH(name, 128); break;                              \
+      default: ROUTE_LAUNCH(name, 256);                                      \
+    }                                                                        \
+  }
+ROUTE_LAUNCHES(gather)
+ROUTE_LAUNCHES(combine)
+ROUTE_LAUNCHES(combine_grad)
+template <typename T> void launch_choice_grad(const RowArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(choice_grad_kernel<T>, dim3(grid_of(a.choices, 64)), dim3(256), 0, st, a);
 }
 
 bool off_by(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }
@@ -404,10 +526,12 @@ extern "C" int dynb_route_gather(const dynb_route_desc* d, const void* x, const 
   a.ld_out = pitch(d, d->ld_sorted);
   a.offsets = offsets;
   a.slot = slot;
-  const dim3 grid(grid_for(a.tokens * a.granules)), block(256);
-  Timed t(KC_ROUTE, stream, 0.0, (double)size * d->cols * (a.tokens + a.choices));
-  if (d->dtype == DYNB_F32) hipLaunchKernelGGL(gather_kernel<float>, grid, block, 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(gather_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a);
+  const double bytes = (double)size * d->cols * (a.tokens + a.choices);
+  const bool past = past_caches(bytes);
+  Timed t(KC_ROUTE, stream, 0.0, bytes);
+  const hipStream_t st = (hipStream_t)stream;
+  if (d->dtype == DYNB_F32) past ? launch_gather<float, true>(a, st) : launch_gather<float, false>(a, st);
+  else past ? launch_gather<bf16, true>(a, st) : launch_gather<bf16, false>(a, st);
   return launched("route_gather");
 }
 
@@ -428,11 +552,12 @@ extern "C" int dynb_route_combine(const dynb_route_desc* d, const void* sorted, 
   a.ld_addend = pitch(d, d->ld_addend);
   a.out = out;
   a.ld_out = pitch(d, d->ld_out);
-  const dim3 grid(grid_for(a.tokens * a.granules)), block(256);
-  Timed t(KC_ROUTE, stream, 2.0 * a.choices * d->cols,
-          (double)size * d->cols * (a.choices + a.tokens * (1 + (addend != nullptr))));
-  if (d->dtype == DYNB_F32) hipLaunchKernelGGL(combine_kernel<float>, grid, block, 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(combine_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a);
+  const double bytes = (double)size * d->cols * (a.choices + a.tokens * (1 + (addend != nullptr)));
+  const bool past = past_caches(bytes);
+  Timed t(KC_ROUTE, stream, 2.0 * a.choices * d->cols, bytes);
+  const hipStream_t st = (hipStream_t)stream;
+  if (d->dtype == DYNB_F32) past ? launch_combine<float, true>(a, st) : launch_combine<float, false>(a, st);
+  else past ? launch_combine<bf16, true>(a, st) : launch_combine<bf16, false>(a, st);
   return launched("route_combine");
 }
 
@@ -457,9 +582,11 @@ extern "C" int dynb_route_combine_backward(const dynb_route_desc* d, const void*
   a.slot = slot;
   a.weights = weights;
   a.dweights = dweights;
-  const dim3 grid(grid_for(a.choices * 64)), block(256);
-  Timed t(KC_ROUTE, stream, 3.0 * a.choices * d->cols, (double)size * d->cols * (a.tokens + 2 * a.choices));
-  if (d->dtype == DYNB_F32) hipLaunchKernelGGL(combine_grad_kernel<float>, grid, block, 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(combine_grad_kernel<bf16>, grid, block, 0, (hipStream_t)stream, a);
+  const double bytes = (double)size * d->cols * (a.tokens + 2 * a.choices);
+  const bool past = past_caches(bytes);
+  Timed t(KC_ROUTE, stream, 3.0 * a.choices * d->cols, bytes);
+  const hipStream_t st = (hipStream_t)stream;
+  if (d->dtype == DYNB_F32) past ? launch_combine_grad<float, true>(a, st) : launch_choice_grad<float>(a, st);
+  else past ? launch_combine_grad<bf16, true>(a, st) : launch_choice_grad<bf16>(a, st);
   return launched("route_combine_backward");
 }

@@ -14,14 +14,24 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // A granule is 8 neighbouring elements of a row.  Vector accesses need no alignment beyond the element's on this
 // target: the memory pipeline splits what crosses a line.
 constexpr int GRANULE = 8;
-struct __attribute__((packed, aligned(2))) Any16 { u32x4 v; };
-struct __attribute__((packed, aligned(1))) Any8 { u32x2 v; };
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+// PAST: the access passes the caches by (data that is used once and is more than they hold).
+template <bool PAST = false> __device__ inline u32x4 load16(const void* p) {
+  if (PAST) return __builtin_nontemporal_load((const u32x4_any*)p);
+  return *(const u32x4_any*)p;
+}
+template <bool PAST = false> __device__ inline void store16(void* p, const u32x4& v) {
+  if (PAST) __builtin_nontemporal_store((u32x4_any)v, (u32x4_any*)p);
+  else *(u32x4_any*)p = v;
+}
 
 __device__ inline float to_float(float v) { return v; }
 __device__ inline float to_float(bf16 v) { return (float)v; }
 
 __device__ inline void load_granule(const float* p, float (&f)[GRANULE]) {
-  const u32x4 a = ((const Any16*)p)[0].v, b = ((const Any16*)p)[1].v;
+  const u32x4 a = load16(p), b = load16(p + 4);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     f[e] = __uint_as_float(a[e]);
@@ -29,32 +39,32 @@ __device__ inline void load_granule(const float* p, float (&f)[GRANULE]) {
   }
 }
 __device__ inline void load_granule(const bf16* p, float (&f)[GRANULE]) {
-  const u32x4 a = ((const Any16*)p)->v;
+  const u32x4 a = load16(p);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     f[2 * e] = __uint_as_float(a[e] << 16);
     f[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
   }
 }
-__device__ inline void store_granule(float* p, const float (&f)[GRANULE]) {
+template <bool PAST = false> __device__ inline void store_granule(float* p, const float (&f)[GRANULE]) {
   u32x4 a, b;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     a[e] = __float_as_uint(f[e]);
     b[e] = __float_as_uint(f[4 + e]);
   }
-  ((Any16*)p)[0].v = a;
-  ((Any16*)p)[1].v = b;
+  store16<PAST>(p, a);
+  store16<PAST>(p + 4, b);
 }
 __device__ inline uint32_t two_bf16(float a, float b) {   // round to nearest even
   return (uint32_t)__builtin_bit_cast(unsigned short, (bf16)a) |
          ((uint32_t)__builtin_bit_cast(unsigned short, (bf16)b) << 16);
 }
-__device__ inline void store_granule(bf16* p, const float (&f)[GRANULE]) {
+template <bool PAST = false> __device__ inline void store_granule(bf16* p, const float (&f)[GRANULE]) {
   u32x4 a;
 #pragma unroll
   for (int e = 0; e < 4; ++e) a[e] = two_bf16(f[2 * e], f[2 * e + 1]);
-  ((Any16*)p)->v = a;
+  store16<PAST>(p, a);
 }
 
 // The first n of 8 elements (n >= 8: all), zeros behind them; nothing past the n-th is touched.
@@ -67,10 +77,10 @@ __device__ inline void load_part(const T* p, int n, float (&f)[GRANULE]) {
 #pragma unroll
   for (int e = 0; e < GRANULE; ++e) f[e] = e < n ? to_float(p[e]) : 0.f;
 }
-template <typename T>
+template <bool PAST = false, typename T>
 __device__ inline void store_part(T* p, int n, const float (&f)[GRANULE]) {
   if (n >= GRANULE) {
-    store_granule(p, f);
+    store_granule<PAST>(p, f);
     return;
   }
 #pragma unroll
@@ -97,10 +107,10 @@ __device__ inline void unpack(const Raw<float>& r, float (&f)[GRANULE]) {
   }
 }
 // ... of the first n elements (n <= 0: none), zeros behind them
-__device__ inline Raw<bf16> load_raw(const bf16* p, int n) {
+template <bool PAST = false> __device__ inline Raw<bf16> load_raw(const bf16* p, int n) {
   Raw<bf16> r = {{0, 0, 0, 0}};
   if (n >= GRANULE) {
-    r.a = ((const Any16*)p)->v;
+    r.a = load16<PAST>(p);
   } else if (n > 0) {
     const unsigned short* h = (const unsigned short*)p;
 #pragma unroll
@@ -109,11 +119,11 @@ __device__ inline Raw<bf16> load_raw(const bf16* p, int n) {
   }
   return r;
 }
-__device__ inline Raw<float> load_raw(const float* p, int n) {
+template <bool PAST = false> __device__ inline Raw<float> load_raw(const float* p, int n) {
   Raw<float> r = {{0, 0, 0, 0}, {0, 0, 0, 0}};
   if (n >= GRANULE) {
-    r.a = ((const Any16*)p)[0].v;
-    r.b = ((const Any16*)p)[1].v;
+    r.a = load16<PAST>(p);
+    r.b = load16<PAST>(p + 4);
   } else if (n > 0) {
     const uint32_t* w = (const uint32_t*)p;
 #pragma unroll

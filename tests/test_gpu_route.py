@@ -192,6 +192,14 @@ def test_pitches_and_starts(dynb, dtype, pads, offset, cols):
     rows_case(19, 4, 6, cols, dtype, "holes", pads=pads, offset=offset)
 
 
+@pytest.mark.parametrize("cols,dtype,tokens,k", [(100, "f32", 36000, 4), (201, "bf16", 58000, 2), (500, "bf16", 8000, 9),
+                                                 (1001, "f32", 4500, 3), (2000, "bf16", 5600, 2), (2051, "bf16", 9000, 1)])
+def test_calls_beyond_the_caches(dynb, cols, dtype, tokens, k):
+    """More than 64 MB per call, where rows pass the caches by and gradients go token by token."""
+    assert (1 + k) * tokens * cols * (4 if dtype == "f32" else 2) > 64e6
+    rows_case(tokens, k, 37, cols, dtype, "holes", pads=(1, 0, 3, 0))
+
+
 @pytest.mark.parametrize("kind", ["none", "one"])
 def test_nothing_kept_and_all_to_one(dynb, kind):
     rows_case(40, 2, 9, 520, "bf16", kind)
