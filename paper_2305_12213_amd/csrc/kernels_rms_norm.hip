@@ -11,6 +11,10 @@ namespace {
 
 constexpr float FP8_TOP = 448.f, INT8_TOP = 127.f;
 constexpr int MAX_COLS = 1 << 20;
+constexpr int WIDEST = 2 * 64 * MOST_WAVES;   // granules of the widest rows that stay in registers
+// Rows of up to so many waves take one granule per thread, wider ones two (4096 bf16 columns: one row 3.2 us, with two granules
+// 3.8, 4096 rows 25.2 and 26.1; 8192 columns: 53.3 us with one, 49.9 with two).
+constexpr int ONE_GRANULE = 8;
 
 struct NormArgs {
   const void *x, *residual;
@@ -67,10 +71,11 @@ template <typename F> __device__ inline float rstd_of(float ss, int cols, float 
 // Rows of any width, a workgroup per row that reads it two or three times.
 template <typename T, int OUT>
 __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
-  __shared__ float red[4];
-  __shared__ uint32_t redu[4];
+  __shared__ float red[3][MOST_WAVES];
+  __shared__ uint32_t redu[MOST_WAVES];
   constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
     const T* x = (const T*)p.x + r * p.ld_x;
     const T* res = p.residual ? (const T*)p.residual + r * p.ld_residual : nullptr;
     T* sum = p.sum ? (T*)p.sum + r * p.ld_sum : nullptr;
@@ -80,14 +85,14 @@ __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
       const float s = value(c);
       ss += s * s;
     }
-    ss = block_sum<4>(ss, red);
+    ss = block_sum(ss, 4, red[turn]);
     const float rstd = rstd_of(ss, p.cols, p.eps, [&]() {
       float a = 0.f;
       for (int c = threadIdx.x; c < p.cols; c += 256) {
         const float s = value(c) * 0x1p-80f;
         a += s * s;
       }
-      return block_sum<4>(a, red);
+      return block_sum(a, 4, red[2]);
     });
     if (threadIdx.x == 0 && p.rstd) p.rstd[r] = rstd;
     auto result = [&](float s, int c) { return s * rstd * (p.gain ? p.gain[c] : 1.f); };
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
       const int c0 = b * p.scale_block, c1 = min(c0 + p.scale_block, p.cols);
       uint32_t a = 0;
       for (int c = c0 + lane; c < c1; c += lanes) a = max(a, __float_as_uint(result(value(c), c)) & 0x7fffffffu);
-      a = whole ? block_max<4>(a, redu) : wave_max(a);
+      a = whole ? block_max(a, 4, redu) : wave_max(a);
       const Scale s = scale_of(a, TOP);
       if (lane == 0) p.scales[r * p.n_blocks + b] = s.scale;
       for (int c = c0 + lane; c < c1; c += lanes) {
@@ -118,22 +123,24 @@ __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
   }
 }
 
-// Rows that fit in the registers of W waves, N granules per thread: one read, one write.  (W = 1: four rows per
-// workgroup, no barrier.)  A thread keeps its part of the gain over all rows of the workgroup.  group: lanes that share a
+// Rows that fit in registers, N granules per thread: one read, one write.  WIDE: a workgroup of as many waves as a row needs
+// takes a row at a time; else each of its four waves does.  A thread keeps its part of the gain over all rows of the workgroup.  group: lanes that share a
 // scale (a power of two), 0 where the whole row does.
-template <typename T, int OUT, int W, int N, bool PAST>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArgs p, int group) {
-  constexpr int PER = W == 1 ? 4 : 1;      // rows of a workgroup
+template <typename T, int OUT, bool WIDE, int N, bool PAST>
+__global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(NormArgs p, int group) {
+  constexpr int PER = WIDE ? 1 : 4;        // rows of a workgroup
   constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
-  __shared__ float red[W];
-  __shared__ uint32_t redu[W];
-  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-  int64_t r = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x >> 6 : 0);
+  __shared__ float red[3][MOST_WAVES];
+  __shared__ uint32_t redu[2][MOST_WAVES];
+  const int waves = WIDE ? blockDim.x >> 6 : 1;
+  const int t = WIDE ? threadIdx.x : threadIdx.x & 63;
+  int64_t r = (int64_t)blockIdx.x * PER + (WIDE ? 0 : threadIdx.x >> 6);
+  int turn = 0;
   Raw<T> x[N], res[N];
   auto ask = [&](int64_t row) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * W) * GRANULE;
+      const int c = (t + i * 64 * waves) * GRANULE;
       x[i] = load_raw<PAST>((const T*)p.x + row * p.ld_x + c, p.cols - c);
       if (p.residual) res[i] = load_raw<PAST>((const T*)p.residual + row * p.ld_residual + c, p.cols - c);
     }
@@ -142,13 +149,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
   Raw<float> gain[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int c = (t + i * 64 * W) * GRANULE;
+    const int c = (t + i * 64 * waves) * GRANULE;
     if (p.gain) gain[i] = load_raw(p.gain + c, p.cols - c);
     else
 #pragma unroll
       for (int e = 0; e < 4; ++e) gain[i].a[e] = gain[i].b[e] = 0x3f800000u;
   }
-  for (; r < p.rows; r += (int64_t)gridDim.x * PER) {
+  for (; r < p.rows; r += (int64_t)gridDim.x * PER, turn ^= 1) {
     float s[N][GRANULE], ss = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -162,20 +169,20 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
 #pragma unroll
       for (int e = 0; e < GRANULE; ++e) ss += s[i][e] * s[i][e];
     }
-    ss = block_sum<W>(ss, red);
+    ss = block_sum(ss, waves, red[turn]);
     const float rstd = rstd_of(ss, p.cols, p.eps, [&]() {
       float a = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) a += (s[i][e] * 0x1p-80f) * (s[i][e] * 0x1p-80f);
-      return block_sum<W>(a, red);
+      return block_sum(a, waves, red[2]);
     });
     if (t == 0 && p.rstd) p.rstd[r] = rstd;
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * W) * GRANULE;
+      const int c = (t + i * 64 * waves) * GRANULE;
       if (p.sum && c < p.cols) store_part<PAST>((T*)p.sum + r * p.ld_sum + c, p.cols - c, s[i]);
       float g[GRANULE];
       unpack(gain[i], g);
@@ -195,12 +202,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_kernel(NormArg
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) amax = max(amax, __float_as_uint(s[i][e]) & 0x7fffffffu);
-      scale = scale_of(block_max<W>(amax, redu), TOP);
+      scale = scale_of(block_max(amax, waves, redu[turn]), TOP);
       if (t == 0) p.scales[now] = scale.scale;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * W) * GRANULE;
+      const int c = (t + i * 64 * waves) * GRANULE;
       if (group) {
         amax = 0;
 #pragma unroll
@@ -225,8 +232,9 @@ struct NormGradArgs {
 
 template <typename T>
 __global__ __launch_bounds__(256) void rms_norm_grad_any_kernel(NormGradArgs p) {
-  __shared__ float red[4];
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+  __shared__ float red[2][MOST_WAVES];
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
     const T *s = (const T*)p.sum + r * p.ld_sum, *dy = (const T*)p.dy + r * p.ld_dy;
     const T* dsum = p.dsum ? (const T*)p.dsum + r * p.ld_dsum : nullptr;
     T* dx = (T*)p.dx + r * p.ld_dx;
@@ -234,7 +242,7 @@ __global__ __launch_bounds__(256) void rms_norm_grad_any_kernel(NormGradArgs p) 
     float c1 = 0.f;
     for (int c = threadIdx.x; c < p.cols; c += 256)
       c1 += (p.gain ? p.gain[c] : 1.f) * to_float(dy[c]) * (to_float(s[c]) * rstd);
-    c1 = block_sum<4>(c1, red) / (float)p.cols;
+    c1 = block_sum(c1, 4, red[turn]) / (float)p.cols;
     for (int c = threadIdx.x; c < p.cols; c += 256) {
       const float g = (p.gain ? p.gain[c] : 1.f) * to_float(dy[c]);
       dx[c] = (T)(rstd * (g - to_float(s[c]) * rstd * c1) + (dsum ? to_float(dsum[c]) : 0.f));
@@ -304,19 +312,21 @@ int describe(const dynb_rms_norm_desc* d, const char* who, NormArgs& a) {
   return DYNB_OK;
 }
 
-// Workgroups for `units` of work where one has `threads` threads: what the chip holds at once, less if there is less.
+// Workgroups for `units` of work where one has `threads` threads: four times what the chip holds at once, less if there is
+// less.
 int resident(int64_t units, int threads) {
-  const int64_t most = 256 * (2048 / threads);
+  const int64_t most = 1024 * (2048 / threads);
   return (int)(units < most ? units : most);
 }
 
-bool past_caches(const NormArgs& a) { return a.bytes > 64e6; }
+// Calls of more bytes than the caches keep until the next one reads them pass them by (16384 x 8192 bf16 to fp8: 165 us, 185
+// through the caches).
+bool past_caches(double bytes) { return bytes > 64e6; }
 
-template <typename T, int OUT, int W, int N> void launch_norm_as(const NormArgs& a, int group, hipStream_t st) {
-  constexpr int THREADS = W == 1 ? 256 : 64 * W, PER = W == 1 ? 4 : 1;
-  const dim3 grid(resident((a.rows + PER - 1) / PER, THREADS)), block(THREADS);
-  if (past_caches(a)) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, W, N, true>), grid, block, 0, st, a, group);
-  else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, W, N, false>), grid, block, 0, st, a, group);
+template <typename T, int OUT, bool WIDE, int N> void launch_norm_as(const NormArgs& a, int waves, int group, hipStream_t st) {
+  const dim3 block(64 * waves), grid(resident(WIDE ? a.rows : (a.rows + 3) / 4, 64 * waves));
+  if (past_caches(a.bytes)) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, WIDE, N, true>), grid, block, 0, st, a, group);
+  else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, WIDE, N, false>), grid, block, 0, st, a, group);
 }
 
 template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream_t st) {
@@ -324,16 +334,15 @@ template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream
   const int granules = (a.cols + GRANULE - 1) / GRANULE, lanes = a.scale_block / GRANULE;
   const bool whole = OUT == DYNB_OUT_SAME || a.n_blocks == 1;
   const int group = whole ? 0 : lanes;
-  if (granules > 2048 || (!whole && (lanes > 64 || (lanes & (lanes - 1))))) {
+  if (granules > WIDEST || (!whole && (lanes > 64 || (lanes & (lanes - 1))))) {
     hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
     return;
   }
-  if (granules <= 64) launch_norm_as<T, OUT, 1, 1>(a, group, st);
-  else if (granules <= 128) launch_norm_as<T, OUT, 1, 2>(a, group, st);
-  else if (granules <= 256) launch_norm_as<T, OUT, 4, 1>(a, group, st);
-  else if (granules <= 512) launch_norm_as<T, OUT, 4, 2>(a, group, st);
-  else if (granules <= 1024) launch_norm_as<T, OUT, 8, 2>(a, group, st);
-  else launch_norm_as<T, OUT, 16, 2>(a, group, st);
+  const int waves = (granules + 63) / 64;
+  if (granules <= 64) launch_norm_as<T, OUT, false, 1>(a, 4, group, st);
+  else if (granules <= 128) launch_norm_as<T, OUT, false, 2>(a, 4, group, st);
+  else if (waves <= ONE_GRANULE) launch_norm_as<T, OUT, true, 1>(a, waves, group, st);
+  else launch_norm_as<T, OUT, true, 2>(a, (waves + 1) / 2, group, st);
 }
 
 template <typename T> void launch_norm(const NormArgs& a, int out, hipStream_t st) {
@@ -342,22 +351,24 @@ template <typename T> void launch_norm(const NormArgs& a, int out, hipStream_t s
   else launch_norm_out<T, DYNB_OUT_INT8>(a, st);
 }
 
-// Both gradients of rows that fit in the registers of W waves, N granules per thread, in one pass: the rows' gradient, and
+// Both gradients of rows that fit in registers, N granules per thread, in one pass: the rows' gradient, and
 // the gain's summed over the rows of a chunk (of one worker) in registers, then over the chunks by sum_chunks_kernel.
-// (W = 1: each of four waves takes every fourth row of the chunk, and their sums are added in LDS.)  A row's loads are
-// issued while the row before it is reduced.
+// WIDE: a workgroup of as many waves as a row needs takes a row at a time; else each of its four waves takes every fourth row
+// of the chunk, and their sums are added in LDS.  A row's loads are issued while the row before it is reduced.
 struct Chunks {
   int rows;                               // of a chunk, the last one of a worker may be shorter
   int first[DYNB_MAX_WORKERS + 1];        // of each worker's chunks
 };
-template <typename T, int W, int N, bool PAST>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(NormGradArgs p, Segs seg, Chunks ch,
+template <typename T, bool WIDE, int N, bool PAST>
+__global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_kernel(NormGradArgs p, Segs seg, Chunks ch,
                                                                              float* partial) {
-  constexpr int PER = W == 1 ? 4 : 1, COLS = 64 * W * N * GRANULE;
-  constexpr bool AHEAD = W < 16 || sizeof(T) == 2;   // (fp32 rows of 16 waves: the next row would spill)
-  __shared__ float red[W];
-  __shared__ float sums[W == 1 ? 3 * COLS : 1];
-  const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x, wave = W == 1 ? threadIdx.x >> 6 : 0;
+  constexpr int PER = WIDE ? 1 : 4, COLS = 64 * N * GRANULE;
+  constexpr bool AHEAD = !WIDE || N == 1 || sizeof(T) == 2;   // (fp32, two granules, up to 16 waves: the next row would spill)
+  __shared__ float red[2][MOST_WAVES];
+  __shared__ float sums[WIDE ? 1 : 3 * COLS];
+  const int waves = WIDE ? blockDim.x >> 6 : 1;
+  const int t = WIDE ? threadIdx.x : threadIdx.x & 63, wave = WIDE ? 0 : threadIdx.x >> 6;
+  int turn = 0;
   int k = 0;
   while (k + 1 < seg.K && (int)blockIdx.x >= ch.first[k + 1]) ++k;
   const int begin = seg.off[k] + ((int)blockIdx.x - ch.first[k]) * ch.rows, end = min(begin + ch.rows, seg.off[k + 1]);
@@ -367,7 +378,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
     rstd = p.rstd[r];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * W) * GRANULE;
+      const int c = (t + i * 64 * waves) * GRANULE;
       s[i] = load_raw<PAST>((const T*)p.sum + r * p.ld_sum + c, p.cols - c);
       dy[i] = load_raw<PAST>((const T*)p.dy + r * p.ld_dy + c, p.cols - c);
       if (p.dsum) ds[i] = load_raw<PAST>((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c);
@@ -379,7 +390,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
   Raw<float> gain[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int c = (t + i * 64 * W) * GRANULE;
+    const int c = (t + i * 64 * waves) * GRANULE;
     if (p.gain) gain[i] = load_raw(p.gain + c, p.cols - c);
     else
 #pragma unroll
@@ -387,7 +398,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
 #pragma unroll
     for (int e = 0; e < GRANULE; ++e) acc[i][e] = 0.f;
   }
-  for (; r < end; r += PER) {
+  for (; r < end; r += PER, turn ^= 1) {
     if (!AHEAD) ask(r);
     float c1 = 0.f;
     Raw<T> s0[N], dy0[N], ds0[N];
@@ -412,10 +423,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
         c1 += g[e] * q;
       }
     }
-    c1 = block_sum<W>(c1, red) / (float)p.cols;
+    c1 = block_sum(c1, waves, red[turn]) / (float)p.cols;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * W) * GRANULE;
+      const int c = (t + i * 64 * waves) * GRANULE;
       if (c >= p.cols) continue;
       float a[GRANULE], d[GRANULE], g[GRANULE];
       unpack(s0[i], a);
@@ -432,7 +443,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
     }
   }
   if (!p.dgain) return;
-  if (W == 1) {
+  if (!WIDE) {
     if (wave > 0)
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -451,34 +462,33 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_grad_kernel(No
   float* const to = ch.first[k + 1] - ch.first[k] == 1 ? p.dgain + k * p.dgain_stride : partial + (int64_t)blockIdx.x * p.cols;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int c = (t + i * 64 * W) * GRANULE;
+    const int c = (t + i * 64 * waves) * GRANULE;
     if (c < p.cols) store_part(to + c, p.cols - c, acc[i]);
   }
 }
 
-// Sums of the workers' chunks, 64 columns per workgroup: 16 groups of threads take every 16th chunk, then the groups are
-// added in order.  Workers without rows get zeros; those with one chunk have their sum.
-__global__ __launch_bounds__(1024) void sum_chunks_kernel(const float* partial, Chunks ch, int cols, float* dgain,
+// Sums of the workers' chunks, COLS columns per workgroup: GROUPS groups of threads take every GROUPS-th chunk, then the
+// groups are added in order.  Workers without rows get zeros; those with one chunk have their sum.
+template <int COLS, int GROUPS>
+__global__ __launch_bounds__(COLS * GROUPS) void sum_chunks_kernel(const float* partial, Chunks ch, int cols, float* dgain,
                                                           int64_t stride) {
-  __shared__ float sums[16][64];
+  __shared__ float sums[GROUPS][COLS];
   const int k = blockIdx.y, n = ch.first[k + 1] - ch.first[k];
   if (n == 1) return;
-  const int lane = threadIdx.x & 63, group = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const int lane = threadIdx.x % COLS, group = threadIdx.x / COLS, c = blockIdx.x * COLS + lane;
   float a = 0.f;
   if (c < cols) {
     const float* from = partial + (int64_t)ch.first[k] * cols + c;
 #pragma unroll 8
-    for (int i = group; i < n; i += 16) a += from[(int64_t)i * cols];
+    for (int i = group; i < n; i += GROUPS) a += from[(int64_t)i * cols];
   }
   sums[group][lane] = a;
   __syncthreads();
   if (group > 0 || c >= cols) return;
 #pragma unroll
-  for (int g = 1; g < 16; ++g) a += sums[g][lane];
+  for (int g = 1; g < GROUPS; ++g) a += sums[g][lane];
   dgain[k * stride + c] = a;
 }
-
-constexpr int GRAD_GRANULES = 2048;       // widest rows of rms_norm_grad_kernel
 
 // How the workers' rows are cut, and how many chunks: enough workgroups for the chip, and rows enough in each that the
 // chunks' sums are a small part of what is read.
@@ -498,19 +508,19 @@ int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   return n;
 }
 
-template <typename T, int W, int N>
-void launch_norm_grad_as(const NormGradArgs& a, const Segs& seg, const Chunks& ch, float* partial, hipStream_t st) {
-  const dim3 grid(ch.first[seg.K]), block(W == 1 ? 256 : 64 * W);
-  if ((double)a.rows * a.cols * sizeof(T) * (3 + (a.dsum != nullptr)) > 64e6)
-    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, N, true>), grid, block, 0, st, a, seg, ch, partial);
+template <typename T, bool WIDE, int N>
+void launch_norm_grad_as(const NormGradArgs& a, const Segs& seg, const Chunks& ch, int waves, float* partial, hipStream_t st) {
+  const dim3 grid(ch.first[seg.K]), block(64 * waves);
+  if (past_caches((double)a.rows * a.cols * sizeof(T) * (3 + (a.dsum != nullptr))))
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, WIDE, N, true>), grid, block, 0, st, a, seg, ch, partial);
   else
-    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, N, false>), grid, block, 0, st, a, seg, ch, partial);
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, WIDE, N, false>), grid, block, 0, st, a, seg, ch, partial);
 }
 
 template <typename T>
 void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hipStream_t st) {
   const int granules = (a.cols + GRANULE - 1) / GRANULE;
-  if (granules > GRAD_GRANULES) {
+  if (granules > WIDEST) {
     if (a.dgain)   // (first: dx may lie on dy)
       hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((a.cols + 255) / 256, seg.K), dim3(256), 0, st, a, seg);
     if (a.rows) hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
@@ -519,24 +529,34 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
   Chunks ch;
   const int n = chunks_of(seg, a.cols, ch);
   if (n > 0) {
-    if (granules <= 64) launch_norm_grad_as<T, 1, 1>(a, seg, ch, partial, st);
-    else if (granules <= 128) launch_norm_grad_as<T, 1, 2>(a, seg, ch, partial, st);
-    else if (granules <= 256) launch_norm_grad_as<T, 4, 1>(a, seg, ch, partial, st);
-    else if (granules <= 512) launch_norm_grad_as<T, 4, 2>(a, seg, ch, partial, st);
-    else if (granules <= 1024) launch_norm_grad_as<T, 8, 2>(a, seg, ch, partial, st);
-    else launch_norm_grad_as<T, 16, 2>(a, seg, ch, partial, st);
+    const int waves = (granules + 63) / 64;
+    if (granules <= 64) launch_norm_grad_as<T, false, 1>(a, seg, ch, 4, partial, st);
+    else if (granules <= 128) launch_norm_grad_as<T, false, 2>(a, seg, ch, 4, partial, st);
+    else if (waves <= ONE_GRANULE) launch_norm_grad_as<T, true, 1>(a, seg, ch, waves, partial, st);
+    else launch_norm_grad_as<T, true, 2>(a, seg, ch, (waves + 1) / 2, partial, st);
   }
   bool left = false;
-  for (int k = 0; k < seg.K; ++k) left |= ch.first[k + 1] - ch.first[k] != 1;
-  if (a.dgain && left)
-    hipLaunchKernelGGL(sum_chunks_kernel, dim3((a.cols + 63) / 64, seg.K), dim3(1024), 0, st, partial, ch, a.cols, a.dgain,
-                       a.dgain_stride);
+  int most = 0;
+  for (int k = 0; k < seg.K; ++k) {
+    const int c = ch.first[k + 1] - ch.first[k];
+    left |= c != 1;
+    most = c > most ? c : most;
+  }
+  if (!a.dgain || !left) return;
+  // Many groups where a worker has many chunks, few threads where none does: 4096 columns of one worker with 512 chunks 4.6
+  // us, with four groups 7.1; of 16 workers with 9 to 80 chunks 4.7 us, with 32 groups 6.4.
+  if (most > 128)
+    hipLaunchKernelGGL((sum_chunks_kernel<32, 32>), dim3((a.cols + 31) / 32, seg.K), dim3(1024), 0, st, partial, ch, a.cols,
+                       a.dgain, a.dgain_stride);
+  else
+    hipLaunchKernelGGL((sum_chunks_kernel<64, 4>), dim3((a.cols + 63) / 64, seg.K), dim3(256), 0, st, partial, ch, a.cols,
+                       a.dgain, a.dgain_stride);
 }
 
 // Bytes of the chunks' sums (none where every worker has one chunk at most).
 size_t partial_bytes(const Segs& seg, int cols) {
   Chunks ch;
-  if ((cols + GRANULE - 1) / GRANULE > GRAD_GRANULES) return 0;
+  if ((cols + GRANULE - 1) / GRANULE > WIDEST) return 0;
   const int n = chunks_of(seg, cols, ch);
   bool more = false;
   for (int k = 0; k < seg.K; ++k) more |= ch.first[k + 1] - ch.first[k] > 1;
@@ -618,10 +638,10 @@ extern "C" int dynb_dequantise(const dynb_rms_norm_desc* d, int64_t rows, const 
   a.bytes = (double)rows * d->cols * (out_dtype == DYNB_F32 ? 5 : 3);
   Timed t(KC_NORM, stream, (double)rows * d->cols, a.bytes);
   if (out_dtype == DYNB_F32) {
-    if (past_caches(a)) hipLaunchKernelGGL((dequantise_kernel<float, true>), grid, block, 0, st, a, d->out, (float*)out, ld_out);
+    if (past_caches(a.bytes)) hipLaunchKernelGGL((dequantise_kernel<float, true>), grid, block, 0, st, a, d->out, (float*)out, ld_out);
     else hipLaunchKernelGGL((dequantise_kernel<float, false>), grid, block, 0, st, a, d->out, (float*)out, ld_out);
   } else {
-    if (past_caches(a)) hipLaunchKernelGGL((dequantise_kernel<bf16, true>), grid, block, 0, st, a, d->out, (bf16*)out, ld_out);
+    if (past_caches(a.bytes)) hipLaunchKernelGGL((dequantise_kernel<bf16, true>), grid, block, 0, st, a, d->out, (bf16*)out, ld_out);
     else hipLaunchKernelGGL((dequantise_kernel<bf16, false>), grid, block, 0, st, a, d->out, (bf16*)out, ld_out);
   }
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "dequantise launch failed");

@@ -168,31 +168,28 @@ __device__ inline uint32_t wave_max(uint32_t v) {
   return m;
 }
 
-// Over a workgroup of WAVES waves; every thread gets the result.  `red` is workgroup-shared and may be used again
-// right away.
-template <int WAVES>
-__device__ inline float block_sum(float v, float* red) {
+// Over a workgroup of `waves` <= 16 waves; every thread gets the result.  `red` is workgroup-shared and must not be that of the
+// reduction before (the barrier of one is what protects the other).
+constexpr int MOST_WAVES = 16;
+__device__ inline float block_sum(float v, int waves, float* red) {
   v = wave_sum(v);
-  if (WAVES == 1) return v;
+  if (waves == 1) return v;
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  float s = red[0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) s += red[w];
-  __syncthreads();
-  return s;
+  const int w = threadIdx.x & (MOST_WAVES - 1);
+  v = w < waves ? red[w] : 0.f;
+  v += from_lane<DPP_XOR1>(v);
+  v += from_lane<DPP_XOR2>(v);
+  v += from_lane<DPP_HALF_MIRROR>(v);
+  return of_lane(v + from_lane<DPP_MIRROR>(v), 0);
 }
-template <int WAVES>
-__device__ inline uint32_t block_max(uint32_t v, uint32_t* red) {
+__device__ inline uint32_t block_max(uint32_t v, int waves, uint32_t* red) {
   v = wave_max(v);
-  if (WAVES == 1) return v;
+  if (waves == 1) return v;
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  uint32_t s = red[0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) s = max(s, red[w]);
-  __syncthreads();
-  return s;
+  const int w = threadIdx.x & (MOST_WAVES - 1);
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)group_max(w < waves ? red[w] : 0u, 16));
 }
 
 // Values of 8 bits with a scale: the largest magnitude's bits (a NaN's are above an infinity's) give scale and factor.

@@ -133,6 +133,15 @@ def test_zeros_infinities_and_nan(dynb, out, block, cols):
     forward(6, cols, "f32", out, block, residual=True, gain=False, x=x, res=res, stats=cols != 200)
 
 
+@pytest.mark.parametrize("rows,cols,dtype,out,block", [(40000, 96, "bf16", "same", 0), (40000, 250, "f32", "fp8", 64),
+                                                       (34000, 1001, "bf16", "int8", 0), (9000, 2050, "bf16", "fp8", 128),
+                                                       (9000, 2051, "bf16", "same", 0), (6000, 5001, "bf16", "fp8", 0),
+                                                       (4200, 5000, "f32", "same", 0)])
+def test_calls_beyond_the_caches(dynb, rows, cols, dtype, out, block):
+    """More rows than workgroups, and beyond 64 MB rows pass the caches by."""
+    forward(rows, cols, dtype, out, block, residual=True, gain=True, pads=(1, 0, 3, 0))
+
+
 def test_no_rows(dynb):
     d = binding.rms_norm_desc("bf16", 64)
     binding.rms_norm(d, 0, None, None, None, None, None)
@@ -202,6 +211,12 @@ def test_gradient_workers(dynb, b, cols, dtype):
 @pytest.mark.parametrize("cols", [7, 250, 1032, 5001, 20003])
 def test_gradient_pitches_and_starts(dynb, dtype, pads, offset, cols):
     backward([4, 0, 7], cols, dtype, dsum=True, gain=True, pads=pads, offset=offset, stride=cols + 3)
+
+
+@pytest.mark.parametrize("b,cols,dtype", [([30000, 0, 17, 20001], 250, "f32"), ([34000], 1001, "bf16"), ([5000, 4000], 2050, "bf16"),
+                                          ([3, 6000], 5001, "bf16"), ([2500, 1700], 5000, "f32")])
+def test_gradients_beyond_the_caches(dynb, b, cols, dtype):
+    backward(b, cols, dtype, dsum=True, gain=True, pads=(1, 0, 3, 0))
 
 
 @pytest.mark.parametrize("alias", ["dy", "dsum"])
