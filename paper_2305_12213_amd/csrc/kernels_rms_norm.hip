@@ -13,8 +13,9 @@ constexpr float FP8_TOP = 448.f, INT8_TOP = 127.f;
 constexpr int MAX_COLS = 1 << 20;
 constexpr int WIDEST = 2 * 64 * MOST_WAVES;   // granules of the widest rows that stay in registers
 // Rows of up to so many waves take one granule per thread, wider ones two (4096 bf16 columns: one row 3.2 us, with two granules
-// 3.8, 4096 rows 25.2 and 26.1; 8192 columns: 53.3 us with one, 49.9 with two).
-constexpr int ONE_GRANULE = 8;
+// 3.8, 4096 rows 25.2 and 26.1; 8192 columns: 53.3 us with one, 49.9 with two).  Gradients: one as far as the waves go (4096
+// x 8192: 58.2 us, with two 60.4).
+constexpr int ONE_GRANULE = 8, ONE_GRANULE_GRAD = MOST_WAVES;
 
 struct NormArgs {
   const void *x, *residual;
@@ -23,7 +24,7 @@ struct NormArgs {
   float *scales, *rstd;
   int64_t ld_x, ld_residual, ld_sum, ld_y;
   int rows, cols, scale_block, n_blocks;
-  float eps;
+  float eps, inv_cols;
   double bytes;                            // of the call
 };
 
@@ -40,15 +41,16 @@ __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE],
   u32x2 q;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    float v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = f[4 * h + e] * inv;
+    const float *v = f + 4 * h;
     if (OUT == DYNB_OUT_FP8) {
-      q[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), true);
-    } else {
-      q[h] = 0;
+      q[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv,
+                                                       __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false), true);
+    } else {                               // the lowest byte of 1.5 * 2^23 + value is the value, rounded to nearest-even
+      uint32_t b[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q[h] |= ((uint32_t)(int)rintf(v[e]) & 0xffu) << (8 * e);
+      for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(__builtin_fmaf(v[e], inv, 12582912.f));
+      q[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u),
+                                   0x05040100u);
     }
   }
   if (n >= GRANULE) {
@@ -61,11 +63,14 @@ __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE],
   }
 }
 
-// 1 / sqrt(mean + eps) from the sum of squares; where that has overflowed, from the squares of the row times 2^-80,
-// which `scaled_sum` gives (eps is nothing beside them; a row with an infinity or NaN ends the same either way).
-template <typename F> __device__ inline float rstd_of(float ss, int cols, float eps, F scaled_sum) {
-  if (ss <= 3.4e38f) return 1.f / sqrtf(ss / (float)cols + eps);
-  return 0x1p-80f / sqrtf(scaled_sum() / (float)cols);
+// 1 / sqrt(mean + eps) from the sum of squares, by the hardware's root (one unit in the last place).  Where the sum has
+// overflowed, from the squares of the row times 2^-80, which `scaled_sum` gives (eps is nothing beside them; a row with an
+// infinity or NaN ends the same either way); where it is too small for the hardware's root, by the library's.
+template <typename F> __device__ inline float rstd_of(float ss, float inv_cols, float eps, F scaled_sum) {
+  const float m = __builtin_fmaf(ss, inv_cols, eps);
+  if (m >= 0x1p-126f && m <= 3e38f) return __builtin_amdgcn_rsqf(m);
+  if (m < 1.f) return 1.f / sqrtf(m);
+  return 0x1p-80f / sqrtf(scaled_sum() * inv_cols);
 }
 
 // Rows of any width, a workgroup per row that reads it two or three times.
@@ -86,7 +91,7 @@ __global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
       ss += s * s;
     }
     ss = block_sum(ss, 4, red[turn]);
-    const float rstd = rstd_of(ss, p.cols, p.eps, [&]() {
+    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() {
       float a = 0.f;
       for (int c = threadIdx.x; c < p.cols; c += 256) {
         const float s = value(c) * 0x1p-80f;
@@ -132,25 +137,25 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
   constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
   __shared__ float red[3][MOST_WAVES];
   __shared__ uint32_t redu[2][MOST_WAVES];
-  const int waves = WIDE ? blockDim.x >> 6 : 1;
-  const int t = WIDE ? threadIdx.x : threadIdx.x & 63;
-  int64_t r = (int64_t)blockIdx.x * PER + (WIDE ? 0 : threadIdx.x >> 6);
+  const uint32_t waves = WIDE ? blockDim.x >> 6 : 1;
+  const uint32_t t = WIDE ? threadIdx.x : threadIdx.x & 63;
+  int64_t r = (int64_t)blockIdx.x * PER + (WIDE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   int turn = 0;
   Raw<T> x[N], res[N];
   auto ask = [&](int64_t row) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * waves) * GRANULE;
-      x[i] = load_raw<PAST>((const T*)p.x + row * p.ld_x + c, p.cols - c);
-      if (p.residual) res[i] = load_raw<PAST>((const T*)p.residual + row * p.ld_residual + c, p.cols - c);
+      const uint32_t c = (t + i * 64 * waves) * GRANULE;
+      x[i] = load_raw<PAST>((const T*)p.x + row * p.ld_x + c, (int)(p.cols - c));
+      if (p.residual) res[i] = load_raw<PAST>((const T*)p.residual + row * p.ld_residual + c, (int)(p.cols - c));
     }
   };
   if (r < p.rows) ask(r);
   Raw<float> gain[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int c = (t + i * 64 * waves) * GRANULE;
-    if (p.gain) gain[i] = load_raw(p.gain + c, p.cols - c);
+    const uint32_t c = (t + i * 64 * waves) * GRANULE;
+    if (p.gain) gain[i] = load_raw(p.gain + c, (int)(p.cols - c));
     else
 #pragma unroll
       for (int e = 0; e < 4; ++e) gain[i].a[e] = gain[i].b[e] = 0x3f800000u;
@@ -170,7 +175,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
       for (int e = 0; e < GRANULE; ++e) ss += s[i][e] * s[i][e];
     }
     ss = block_sum(ss, waves, red[turn]);
-    const float rstd = rstd_of(ss, p.cols, p.eps, [&]() {
+    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() {
       float a = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -182,16 +187,13 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * waves) * GRANULE;
-      if (p.sum && c < p.cols) store_part<PAST>((T*)p.sum + r * p.ld_sum + c, p.cols - c, s[i]);
+      const uint32_t c = (t + i * 64 * waves) * GRANULE;
+      if (p.sum && c < (uint32_t)p.cols) store_part<PAST>((T*)p.sum + r * p.ld_sum + c, (int)(p.cols - c), s[i]);
       float g[GRANULE];
       unpack(gain[i], g);
 #pragma unroll
-      for (int e = 0; e < GRANULE; ++e) {
-        s[i][e] *= rstd * g[e];
-        if (c + e >= p.cols) s[i][e] = 0.f;
-      }
-      if (OUT == DYNB_OUT_SAME && c < p.cols) store_part<PAST>((T*)p.y + r * p.ld_y + c, p.cols - c, s[i]);
+      for (int e = 0; e < GRANULE; ++e) s[i][e] *= rstd * g[e];     // (elements that do not exist are zeros)
+      if (OUT == DYNB_OUT_SAME && c < (uint32_t)p.cols) store_part<PAST>((T*)p.y + r * p.ld_y + c, (int)(p.cols - c), s[i]);
     }
     const int64_t now = r;
     if (r + (int64_t)gridDim.x * PER < p.rows) ask(r + (int64_t)gridDim.x * PER);
@@ -207,15 +209,15 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * waves) * GRANULE;
+      const uint32_t c = (t + i * 64 * waves) * GRANULE;
       if (group) {
         amax = 0;
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) amax = max(amax, __float_as_uint(s[i][e]) & 0x7fffffffu);
         scale = scale_of(group_max(amax, group), TOP);
-        if ((t & (group - 1)) == 0 && c < p.cols) p.scales[now * p.n_blocks + c / p.scale_block] = scale.scale;
+        if ((t & (group - 1)) == 0 && c < (uint32_t)p.cols) p.scales[now * p.n_blocks + c / p.scale_block] = scale.scale;
       }
-      if (c < p.cols) store_eight<OUT, PAST>((uint8_t*)p.y + now * p.ld_y + c, p.cols - c, s[i], scale.inv);
+      if (c < (uint32_t)p.cols) store_eight<OUT, PAST>((uint8_t*)p.y + now * p.ld_y + c, (int)(p.cols - c), s[i], scale.inv);
     }
   }
 }
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(256) void rms_norm_grad_any_kernel(NormGradArgs p) 
 template <typename T>
 __global__ __launch_bounds__(256) void rms_norm_gain_grad_kernel(NormGradArgs p, Segs seg) {
   const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
-  if (c >= p.cols) return;
+  if (c >= (uint32_t)p.cols) return;
   float a = 0.f;
   for (int64_t r = seg.off[k]; r < seg.off[k + 1]; ++r)
     a += to_float(((const T*)p.dy)[r * p.ld_dy + c]) * (to_float(((const T*)p.sum)[r * p.ld_sum + c]) * p.rstd[r]);
@@ -307,6 +309,7 @@ int describe(const dynb_rms_norm_desc* d, const char* who, NormArgs& a) {
   a.ld_y = pitch(d->ld_y);
   a.cols = d->cols;
   a.eps = d->eps;
+  a.inv_cols = 1.f / (float)d->cols;
   a.scale_block = d->scale_block && d->scale_block < d->cols ? d->scale_block : d->cols;
   a.n_blocks = d->out == DYNB_OUT_SAME ? 0 : (d->cols + a.scale_block - 1) / a.scale_block;
   return DYNB_OK;
@@ -366,8 +369,8 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
   constexpr bool AHEAD = !WIDE || N == 1 || sizeof(T) == 2;   // (fp32, two granules, up to 16 waves: the next row would spill)
   __shared__ float red[2][MOST_WAVES];
   __shared__ float sums[WIDE ? 1 : 3 * COLS];
-  const int waves = WIDE ? blockDim.x >> 6 : 1;
-  const int t = WIDE ? threadIdx.x : threadIdx.x & 63, wave = WIDE ? 0 : threadIdx.x >> 6;
+  const uint32_t waves = WIDE ? blockDim.x >> 6 : 1;
+  const uint32_t t = WIDE ? threadIdx.x : threadIdx.x & 63, wave = WIDE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int turn = 0;
   int k = 0;
   while (k + 1 < seg.K && (int)blockIdx.x >= ch.first[k + 1]) ++k;
@@ -378,10 +381,10 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
     rstd = p.rstd[r];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * waves) * GRANULE;
-      s[i] = load_raw<PAST>((const T*)p.sum + r * p.ld_sum + c, p.cols - c);
-      dy[i] = load_raw<PAST>((const T*)p.dy + r * p.ld_dy + c, p.cols - c);
-      if (p.dsum) ds[i] = load_raw<PAST>((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c);
+      const uint32_t c = (t + i * 64 * waves) * GRANULE;
+      s[i] = load_raw<PAST>((const T*)p.sum + r * p.ld_sum + c, (int)(p.cols - c));
+      dy[i] = load_raw<PAST>((const T*)p.dy + r * p.ld_dy + c, (int)(p.cols - c));
+      if (p.dsum) ds[i] = load_raw<PAST>((const T*)p.dsum + r * p.ld_dsum + c, (int)(p.cols - c));
     }
   };
   int r = begin + wave;
@@ -390,8 +393,8 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
   Raw<float> gain[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int c = (t + i * 64 * waves) * GRANULE;
-    if (p.gain) gain[i] = load_raw(p.gain + c, p.cols - c);
+    const uint32_t c = (t + i * 64 * waves) * GRANULE;
+    if (p.gain) gain[i] = load_raw(p.gain + c, (int)(p.cols - c));
     else
 #pragma unroll
       for (int e = 0; e < 4; ++e) gain[i].a[e] = gain[i].b[e] = 0x3f800000u;
@@ -426,8 +429,8 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
     c1 = block_sum(c1, waves, red[turn]) / (float)p.cols;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (t + i * 64 * waves) * GRANULE;
-      if (c >= p.cols) continue;
+      const uint32_t c = (t + i * 64 * waves) * GRANULE;
+      if (c >= (uint32_t)p.cols) continue;
       float a[GRANULE], d[GRANULE], g[GRANULE];
       unpack(s0[i], a);
       unpack(dy0[i], d);
@@ -439,7 +442,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
       }
-      store_part<PAST>((T*)p.dx + (int64_t)r * p.ld_dx + c, p.cols - c, a);
+      store_part<PAST>((T*)p.dx + (int64_t)r * p.ld_dx + c, (int)(p.cols - c), a);
     }
   }
   if (!p.dgain) return;
@@ -462,8 +465,8 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
   float* const to = ch.first[k + 1] - ch.first[k] == 1 ? p.dgain + k * p.dgain_stride : partial + (int64_t)blockIdx.x * p.cols;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int c = (t + i * 64 * waves) * GRANULE;
-    if (c < p.cols) store_part(to + c, p.cols - c, acc[i]);
+    const uint32_t c = (t + i * 64 * waves) * GRANULE;
+    if (c < (uint32_t)p.cols) store_part(to + c, (int)(p.cols - c), acc[i]);
   }
 }
 
@@ -496,7 +499,7 @@ int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   const int granules = (cols + GRANULE - 1) / GRANULE, rows = seg.off[seg.K];
   const int per = granules <= 128 ? 4 : 1;
   ch.rows = (rows + 511) / 512;
-  const int least = granules <= 128 ? 8 : 4;
+  const int least = granules <= 128 ? 4 : 2;
   if (ch.rows < least) ch.rows = least;
   ch.rows = (ch.rows + per - 1) / per * per;
   int n = 0;
@@ -532,7 +535,7 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
     const int waves = (granules + 63) / 64;
     if (granules <= 64) launch_norm_grad_as<T, false, 1>(a, seg, ch, 4, partial, st);
     else if (granules <= 128) launch_norm_grad_as<T, false, 2>(a, seg, ch, 4, partial, st);
-    else if (waves <= ONE_GRANULE) launch_norm_grad_as<T, true, 1>(a, seg, ch, waves, partial, st);
+    else if (waves <= ONE_GRANULE_GRAD) launch_norm_grad_as<T, true, 1>(a, seg, ch, waves, partial, st);
     else launch_norm_grad_as<T, true, 2>(a, seg, ch, (waves + 1) / 2, partial, st);
   }
   bool left = false;
