@@ -12,18 +12,23 @@ namespace {
 // A stable counting sort.  Every wave owns a stretch of the choices; it counts its experts, the counts are summed in the
 // order (expert, workgroup, wave), and the wave goes over its stretch again, 64 choices at a time, and hands out the
 // places in order.  Up to SMALL choices one workgroup does it all in one launch; beyond, a launch before it counts per
-// workgroup, and every workgroup sums those of the ones before it.
-constexpr int SMALL = 8192, SMALL_WAVES = 16, LARGE_WAVES = 4, AHEAD = 8;   // AHEAD: choices per lane that are loaded at once
+// workgroup, and every workgroup sums those of all of them.  What bounds it are chains: loads, barriers, a round of 64.
+constexpr int WAVES = 16, THREADS = WAVES * 64, AHEAD = 2;   // AHEAD: choices per lane that are loaded at once
+constexpr int ROUND = THREADS * AHEAD;    // of a workgroup
+// Choices of one workgroup alone (128 experts: 4096 choices 7.3 us, in two launches 8.2; 8192 choices 10.4 and 8.3).
+constexpr int SMALL = 4096;
 constexpr int MOST_BLOCKS = 128;          // whose counts a workgroup sums
 
 // Lanes of the wave with the same key as this one (all lanes take part; keys below 2^bits).
 __device__ inline uint64_t same_key(int key, int bits) {
-  uint64_t same = ~0ull;
+  uint32_t low = ~0u, high = ~0u;
   for (int b = 0; b < bits; ++b) {
-    const uint64_t set = __ballot((key >> b) & 1);
-    same &= ((key >> b) & 1) ? set : ~set;
+    const int mine = -((key >> b) & 1);
+    const uint64_t set = __ballot(mine);
+    low &= ~((uint32_t)set ^ (uint32_t)mine);
+    high &= ~((uint32_t)(set >> 32) ^ (uint32_t)mine);
   }
-  return same;
+  return (uint64_t)high << 32 | low;
 }
 
 // LDS written by some lanes of a wave and read by others: in order, with nothing moved across.
@@ -47,41 +52,54 @@ __device__ inline void count_stretch(const int32_t* experts, int64_t begin, int6
   }
 }
 
-__global__ __launch_bounds__(LARGE_WAVES * 64) void plan_count_kernel(const int32_t* experts, int64_t n, int64_t per_block,
+__global__ __launch_bounds__(THREADS) void plan_count_kernel(const int32_t* experts, int64_t n, int64_t per_block,
                                                                       int n_experts, int32_t* counts) {
   __shared__ int count[DYNB_MAX_EXPERTS];
-  for (int e = threadIdx.x; e < n_experts; e += LARGE_WAVES * 64) count[e] = 0;
+  for (int e = threadIdx.x; e < n_experts; e += THREADS) count[e] = 0;
   __syncthreads();
-  const int64_t per = per_block / LARGE_WAVES, begin = blockIdx.x * per_block + (threadIdx.x >> 6) * per;
+  const int64_t per = per_block / WAVES, begin = blockIdx.x * per_block + (threadIdx.x >> 6) * per;
   count_stretch(experts, begin, begin + per < n ? begin + per : n, n_experts, count);
   __syncthreads();
-  for (int e = threadIdx.x; e < n_experts; e += LARGE_WAVES * 64) counts[(int64_t)blockIdx.x * n_experts + e] = count[e];
+  for (int e = threadIdx.x; e < n_experts; e += THREADS) counts[(int64_t)blockIdx.x * n_experts + e] = count[e];
 }
 
 // counts: [gridDim.x][n_experts] of plan_count_kernel (not read by a single workgroup)
-template <int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void plan_kernel(const int32_t* experts, int64_t n, int64_t per_block,
+__global__ __launch_bounds__(THREADS) void plan_kernel(const int32_t* experts, int64_t n, int64_t per_block,
                                                           int n_experts, int bits, const int32_t* counts,
                                                           int32_t* offsets, int32_t* slot, int32_t* source) {
-  constexpr int THREADS = WAVES * 64, EACH = (DYNB_MAX_EXPERTS + THREADS - 1) / THREADS;
   __shared__ int place[WAVES * DYNB_MAX_EXPERTS];     // [wave][expert]: counts, then the next place
-  __shared__ int all[DYNB_MAX_EXPERTS];               // of every expert, then its first place
+  __shared__ int all[DYNB_MAX_EXPERTS];               // choices of an expert, then its first place
+  __shared__ int before[DYNB_MAX_EXPERTS];            // ... of the workgroups before this one
   __shared__ int wave_total[WAVES];
+  static_assert(DYNB_MAX_EXPERTS <= THREADS, "a thread per expert");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int* const mine = place + wave * n_experts;
   for (int i = threadIdx.x; i < WAVES * n_experts; i += THREADS) place[i] = 0;
+  for (int i = threadIdx.x; i < n_experts; i += THREADS) all[i] = before[i] = 0;
   __syncthreads();
+  if (gridDim.x > 1) {                   // every thread an expert and some of the workgroups
+    int width = 64;
+    while (width < n_experts) width *= 2;
+    const int e = threadIdx.x % width;
+    int total = 0, ahead = 0;
+    if (e < n_experts) {
+#pragma unroll 8
+      for (int b = threadIdx.x / width; b < (int)gridDim.x; b += THREADS / width) {
+        const int c = counts[(int64_t)b * n_experts + e];
+        ahead += b < (int)blockIdx.x ? c : 0;
+        total += c;
+      }
+      atomicAdd(&all[e], total);
+      atomicAdd(&before[e], ahead);
+    }
+  }
   const int64_t per = per_block / WAVES, begin = blockIdx.x * per_block + wave * per;
   const int64_t end = begin + per < n ? begin + per : n;
   count_stretch(experts, begin, end, n_experts, mine);
   __syncthreads();
-  // each expert: first places of the waves relative to the workgroup's, choices of the workgroups before, of all
-  int before[EACH];
-#pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    const int e = threadIdx.x + u * THREADS;
-    before[u] = 0;
-    if (e >= n_experts) continue;
+  // first places of the waves relative to the workgroup's
+  if ((int)threadIdx.x < n_experts) {
+    const int e = threadIdx.x;
     int total = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
@@ -89,25 +107,11 @@ __global__ __launch_bounds__(WAVES * 64) void plan_kernel(const int32_t* experts
       place[w * n_experts + e] = total;
       total += c;
     }
-    if (gridDim.x > 1) {
-      total = 0;
-#pragma unroll 16
-      for (int b = 0; b < (int)gridDim.x; ++b) {
-        const int c = counts[(int64_t)b * n_experts + e];
-        before[u] += b < (int)blockIdx.x ? c : 0;
-        total += c;
-      }
-    }
-    all[e] = total;
+    if (gridDim.x == 1) all[e] = total;
   }
   __syncthreads();
-  // first places: each thread EACH neighbouring experts, lanes by shuffles, waves through LDS
-  int sum = 0;
-#pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    const int e = threadIdx.x * EACH + u;
-    sum += e < n_experts ? all[e] : 0;
-  }
+  // first places of the experts: lanes by shuffles, waves through LDS
+  const int e0 = threadIdx.x, sum = e0 < n_experts ? all[e0] : 0;
   int upto = sum;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -122,25 +126,13 @@ __global__ __launch_bounds__(WAVES * 64) void plan_kernel(const int32_t* experts
     at += w < wave ? wave_total[w] : 0;
     kept += wave_total[w];
   }
+  if (e0 < n_experts) {
+    if (blockIdx.x == 0) offsets[e0] = at;
+    const int from = at + before[e0];
 #pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    const int e = threadIdx.x * EACH + u;
-    if (e >= n_experts) continue;
-    const int c = all[e];
-    all[e] = at;
-    if (blockIdx.x == 0) offsets[e] = at;
-    at += c;
+    for (int w = 0; w < WAVES; ++w) place[w * n_experts + e0] += from;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) offsets[n_experts] = kept;
-  __syncthreads();
-#pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    const int e = threadIdx.x + u * THREADS;
-    if (e >= n_experts) continue;
-    const int from = all[e] + before[u];
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) place[w * n_experts + e] += from;
-  }
   __syncthreads();
   for (int64_t i0 = begin; i0 < end; i0 += 64 * AHEAD) {
     int next[AHEAD];
@@ -458,7 +450,6 @@ using namespace dynb;
 
 // Choices of a workgroup of the large plan: whole rounds of all its waves, and no more than MOST_BLOCKS workgroups.
 static int64_t choices_per_block(int64_t n) {
-  constexpr int64_t ROUND = LARGE_WAVES * 64 * AHEAD;
   return round_up((n + MOST_BLOCKS - 1) / MOST_BLOCKS, ROUND);
 }
 
@@ -483,14 +474,14 @@ extern "C" int dynb_route_plan(const dynb_route_desc* d, const int32_t* experts,
   const hipStream_t st = (hipStream_t)stream;
   Timed t(KC_ROUTE, stream, 0.0, 12.0 * n);
   if (n <= SMALL) {
-    hipLaunchKernelGGL(plan_kernel<SMALL_WAVES>, dim3(1), dim3(SMALL_WAVES * 64), 0, st, experts, (int64_t)n,
-                       round_up((n + SMALL_WAVES - 1) / SMALL_WAVES, 64) * SMALL_WAVES, d->n_experts, bits,
+    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(THREADS), 0, st, experts, (int64_t)n,
+                       round_up((n + WAVES - 1) / WAVES, 64) * WAVES, d->n_experts, bits,
                        (const int32_t*)nullptr, offsets, slot, source);
   } else {
     const int64_t per = choices_per_block(n);
-    const dim3 grid((unsigned)((n + per - 1) / per)), block(LARGE_WAVES * 64);
+    const dim3 grid((unsigned)((n + per - 1) / per)), block(THREADS);
     hipLaunchKernelGGL(plan_count_kernel, grid, block, 0, st, experts, (int64_t)n, per, d->n_experts, (int32_t*)workspace);
-    hipLaunchKernelGGL(plan_kernel<LARGE_WAVES>, grid, block, 0, st, experts, (int64_t)n, per, d->n_experts, bits,
+    hipLaunchKernelGGL(plan_kernel, grid, block, 0, st, experts, (int64_t)n, per, d->n_experts, bits,
                        (const int32_t*)workspace, offsets, slot, source);
   }
   return launched("route_plan");
