@@ -46,7 +46,6 @@ struct Rule {
 // ---- 4 neighbouring elements, of which the first n exist ------------------------------------------------------
 // Every byte is used once a step: accesses pass the caches by.
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32_any __attribute__((aligned(1)));
 #define GLOBAL __attribute__((address_space(1)))
 
 __device__ inline void load4(const GLOBAL float* p, int n, float (&f)[4]) {

@@ -279,18 +279,19 @@ template <int L> __device__ inline float lanes_sum(float v) {
   return v;
 }
 
-// A wave takes a choice: its row of dsorted, and the product of the two rows.  For calls that the caches hold, where more and
+// L lanes take a choice: its row of dsorted, and the product of the two rows.  For calls that the caches hold, where more and
 // shorter chains count (the gradient is read again for each choice): 1024 tokens of 4 choices of 2048 bf16 columns and the
 // combination of the rows' gradient behind it 13.8 us, by tokens 16.2.
-template <typename T> __global__ __launch_bounds__(256) void choice_grad_kernel(RowArgs p) {
-  const int lane = threadIdx.x & 63;
+template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_kernel(RowArgs p) {
+  __shared__ float red[2][MOST_WAVES];
   const int kept = p.offsets[p.n_experts];
-  for (int64_t i = row_of_thread<64>(); i < p.choices; i += (int64_t)gridDim.x * 4) {
+  int turn = 0;
+  for (int64_t i = row_of_thread<L>(); i < p.choices; i += (int64_t)gridDim.x * (256 / L), turn ^= 1) {
     const int64_t t = i / p.top_k, s = p.slot[i];
     float dot = 0.f;
     if (s >= 0) {
       const float w = p.weights[i];
-      for (int c = lane * GRANULE; c < p.cols; c += 64 * GRANULE) {
+      for (int c = threadIdx.x % L * GRANULE; c < p.cols; c += L * GRANULE) {
         float g[GRANULE], y[GRANULE];
         load_part((const T*)p.in + t * p.ld_in + c, p.cols - c, g);
         load_part((const T*)p.sorted + s * p.ld_sorted + c, p.cols - c, y);
@@ -301,9 +302,9 @@ template <typename T> __global__ __launch_bounds__(256) void choice_grad_kernel(
         }
         store_part((T*)p.out + s * p.ld_out + c, p.cols - c, g);
       }
-      dot = wave_sum(dot);
+      dot = L > 64 ? block_sum(dot, L / 64, red[turn]) : lanes_sum<(L < 64 ? L : 64)>(dot);
     }
-    if (lane == 0) p.dweights[i] = dot;
+    if (threadIdx.x % L == 0) p.dweights[i] = dot;
   }
   clear_rows<T>(p, kept);
 }
@@ -381,13 +382,16 @@ int grid_of(int64_t rows, int lanes) {
   return (int)(blocks < (1 << 20) ? blocks : 1 << 20);
 }
 
-// Lanes of a row (of 8 elements each): as few as hold it up to 32, else the one of 64, 128 and 256 that leaves the fewest idle in the last round.
-int lanes_of(int granules) {
+// Lanes of a row (of 8 elements each): as few as hold it up to 32; else the most of 64, 128 and 256 that leave no more than a
+// fifth idle over the rounds, or, where rows are too few to fill the chip with waves, those of the fewest rounds.  (70 tokens
+// of 8 choices of 3136 bf16 columns, gradients: 256 lanes 10.6 us, 64 20.0; 2000 of 2 of 5300, forward: 256 lanes 43 us, 64 53;
+// 3000 of 4 of 1400 fp32: 64 lanes 55.6 us, 256 61.4.)
+int lanes_of(int granules, int64_t rows) {
   if (granules <= 32) return granules <= 16 ? 16 : 32;
-  int best = 256;
-  for (int l : {128, 64})
-    if ((granules + l - 1) / l * l < (granules + best - 1) / best * best) best = l;
-  return best;
+  if (rows < 1024) return granules <= 64 ? 64 : granules <= 128 ? 128 : 256;
+  for (int l : {256, 128})
+    if ((granules + l - 1) / l * l * 4 <= granules * 5) return l;
+  return 64;
 }
 
 // Calls of more bytes than the caches keep until the next one reads them pass them by.  Sorting and combination of 2048
@@ -399,7 +403,7 @@ bool past_caches(double bytes) { return bytes > 64e6; }
   hipLaunchKernelGGL((name##_kernel<T, L, PAST>), dim3(grid_of(a.tokens, L)), dim3(256), 0, st, a)
 #define ROUTE_LAUNCHES(name)                                                 \
   template <typename T, bool PAST> void launch_##name(const RowArgs& a, hipStream_t st) { \
-    switch (lanes_of(a.granules)) {                                          \
+    switch (lanes_of(a.granules, a.tokens)) {                                \
       case 16: ROUTE_LAUNCH(name, 16); break;                                \
       case 32: ROUTE_LAUNCH(name, 32); break;                                \
       case 64: ROUTE_LAUNCH(name, 64); break;                                \
@@ -411,7 +415,13 @@ ROUTE_LAUNCHES(gather)
 ROUTE_LAUNCHES(combine)
 ROUTE_LAUNCHES(combine_grad)
 template <typename T> void launch_choice_grad(const RowArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(choice_grad_kernel<T>, dim3(grid_of(a.choices, 64)), dim3(256), 0, st, a);
+  const dim3 block(256);
+  if (a.granules <= 16) hipLaunchKernelGGL((choice_grad_kernel<T, 16>), dim3(grid_of(a.choices, 16)), block, 0, st, a);
+  else if (a.granules <= 32) hipLaunchKernelGGL((choice_grad_kernel<T, 32>), dim3(grid_of(a.choices, 32)), block, 0, st, a);
+  else if (a.granules <= 128 || a.choices >= 1024)
+    hipLaunchKernelGGL((choice_grad_kernel<T, 64>), dim3(grid_of(a.choices, 64)), block, 0, st, a);
+  else
+    hipLaunchKernelGGL((choice_grad_kernel<T, 256>), dim3(grid_of(a.choices, 256)), block, 0, st, a);
 }
 
 bool off_by(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }

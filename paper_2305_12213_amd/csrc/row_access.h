@@ -16,6 +16,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int GRANULE = 8;
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
 
 // PAST: the access passes the caches by (data that is used once and is more than they hold).
 template <bool PAST = false> __device__ inline u32x4 load16(const void* p) {
@@ -29,63 +31,9 @@ template <bool PAST = false> __device__ inline void store16(void* p, const u32x4
 
 __device__ inline float to_float(float v) { return v; }
 __device__ inline float to_float(bf16 v) { return (float)v; }
-
-__device__ inline void load_granule(const float* p, float (&f)[GRANULE]) {
-  const u32x4 a = load16(p), b = load16(p + 4);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[e] = __uint_as_float(a[e]);
-    f[4 + e] = __uint_as_float(b[e]);
-  }
-}
-__device__ inline void load_granule(const bf16* p, float (&f)[GRANULE]) {
-  const u32x4 a = load16(p);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = __uint_as_float(a[e] << 16);
-    f[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
-  }
-}
-template <bool PAST = false> __device__ inline void store_granule(float* p, const float (&f)[GRANULE]) {
-  u32x4 a, b;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    a[e] = __float_as_uint(f[e]);
-    b[e] = __float_as_uint(f[4 + e]);
-  }
-  store16<PAST>(p, a);
-  store16<PAST>(p + 4, b);
-}
 __device__ inline uint32_t two_bf16(float a, float b) {   // round to nearest even
   return (uint32_t)__builtin_bit_cast(unsigned short, (bf16)a) |
          ((uint32_t)__builtin_bit_cast(unsigned short, (bf16)b) << 16);
-}
-template <bool PAST = false> __device__ inline void store_granule(bf16* p, const float (&f)[GRANULE]) {
-  u32x4 a;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) a[e] = two_bf16(f[2 * e], f[2 * e + 1]);
-  store16<PAST>(p, a);
-}
-
-// The first n of 8 elements (n >= 8: all), zeros behind them; nothing past the n-th is touched.
-template <typename T>
-__device__ inline void load_part(const T* p, int n, float (&f)[GRANULE]) {
-  if (n >= GRANULE) {
-    load_granule(p, f);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < GRANULE; ++e) f[e] = e < n ? to_float(p[e]) : 0.f;
-}
-template <bool PAST = false, typename T>
-__device__ inline void store_part(T* p, int n, const float (&f)[GRANULE]) {
-  if (n >= GRANULE) {
-    store_granule<PAST>(p, f);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < GRANULE; ++e)
-    if (e < n) p[e] = (T)f[e];
 }
 
 // A granule as it is stored, 4 (bf16) or 8 (fp32) registers: what waits for its use between load and arithmetic.
@@ -106,16 +54,23 @@ __device__ inline void unpack(const Raw<float>& r, float (&f)[GRANULE]) {
     f[4 + e] = __uint_as_float(r.b[e]);
   }
 }
-// ... of the first n elements (n <= 0: none), zeros behind them
+
+// The first n of 8 elements (n >= 8: all, n <= 0: none); zeros behind them, and nothing past the n-th is touched.  What is
+// left of a row's last granule is 4, 2 and 1 elements, as the bits of n say: three accesses at most.
 template <bool PAST = false> __device__ inline Raw<bf16> load_raw(const bf16* p, int n) {
   Raw<bf16> r = {{0, 0, 0, 0}};
   if (n >= GRANULE) {
     r.a = load16<PAST>(p);
   } else if (n > 0) {
-    const unsigned short* h = (const unsigned short*)p;
-#pragma unroll
-    for (int e = 0; e < GRANULE; ++e)
-      if (e < n) r.a[e / 2] |= (uint32_t)h[e] << (16 * (e & 1));
+    u32x2 four = {0, 0};
+    uint32_t two = 0, one = 0;
+    if (n & 4) four = *(const u32x2_any*)p;
+    if (n & 2) two = *(const u32_any*)(p + (n & 4));
+    if (n & 1) one = *(const u16_any*)(p + n - 1);
+    r.a[0] = n & 4 ? four[0] : n & 2 ? two : one;
+    r.a[1] = n & 4 ? four[1] : n & 2 ? one : 0;
+    r.a[2] = n & 4 ? (n & 2 ? two : one) : 0;
+    r.a[3] = (n & 6) == 6 ? one : 0;
   }
   return r;
 }
@@ -125,13 +80,49 @@ template <bool PAST = false> __device__ inline Raw<float> load_raw(const float* 
     r.a = load16<PAST>(p);
     r.b = load16<PAST>(p + 4);
   } else if (n > 0) {
-    const uint32_t* w = (const uint32_t*)p;
-#pragma unroll
-    for (int e = 0; e < GRANULE; ++e)
-      if (e < n) (e < 4 ? r.a : r.b)[e & 3] = w[e];
+    u32x4 four = {0, 0, 0, 0};
+    u32x2 two = {0, 0};
+    uint32_t one = 0;
+    if (n & 4) four = load16(p);
+    if (n & 2) two = *(const u32x2_any*)(p + (n & 4));
+    if (n & 1) one = *(const uint32_t*)(p + n - 1);
+    const u32x4 rest = {n & 2 ? two[0] : one, two[1], n & 2 ? one : 0, 0};
+    r.a = n & 4 ? four : rest;
+    r.b = n & 4 ? rest : r.b;
   }
   return r;
 }
+template <bool PAST = false> __device__ inline void store_part(bf16* p, int n, const float (&f)[GRANULE]) {
+  u32x4 a;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) a[e] = two_bf16(f[2 * e], f[2 * e + 1]);
+  if (n >= GRANULE) {
+    store16<PAST>(p, a);
+  } else if (n > 0) {
+    if (n & 4) *(u32x2_any*)p = u32x2{a[0], a[1]};
+    const uint32_t low = n & 4 ? a[2] : a[0], high = n & 4 ? a[3] : a[1];
+    if (n & 2) *(u32_any*)(p + (n & 4)) = low;
+    if (n & 1) *(u16_any*)(p + n - 1) = (uint16_t)(n & 2 ? high : low);
+  }
+}
+template <bool PAST = false> __device__ inline void store_part(float* p, int n, const float (&f)[GRANULE]) {
+  u32x4 a, b;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    a[e] = __float_as_uint(f[e]);
+    b[e] = __float_as_uint(f[4 + e]);
+  }
+  if (n >= GRANULE) {
+    store16<PAST>(p, a);
+    store16<PAST>(p + 4, b);
+  } else if (n > 0) {
+    if (n & 4) store16(p, a);
+    const u32x4 rest = n & 4 ? b : a;
+    if (n & 2) *(u32x2_any*)(p + (n & 4)) = u32x2{rest[0], rest[1]};
+    if (n & 1) *(uint32_t*)(p + n - 1) = n & 2 ? rest[2] : rest[0];
+  }
+}
+template <typename T> __device__ inline void load_part(const T* p, int n, float (&f)[GRANULE]) { unpack(load_raw(p, n), f); }
 
 // Exchanges between lanes that need no LDS: within 2, 4, 8 and 16 lanes (after the step every lane of the group has
 // the same value, so that a mirrored partner is as good as the xor-ed one).
