@@ -36,7 +36,7 @@ struct Pointers2 {
 struct Workers {                          // those with rows
   int n;
   float w[DYNB_MAX_WORKERS];
-  uint8_t index[DYNB_MAX_WORKERS];
+  int32_t index[DYNB_MAX_WORKERS];        // (whole words: read by scalar instructions)
 };
 struct Rule {
   float lr, eps, beta1, beta2, omb1, omb2, inv_c1, inv_c2;
@@ -45,30 +45,40 @@ struct Rule {
 
 // ---- 4 neighbouring elements, of which the first n exist ------------------------------------------------------
 // Every byte is used once a step: accesses pass the caches by.
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
+typedef uint32_t u32_half __attribute__((aligned(2), may_alias));
 #define GLOBAL __attribute__((address_space(1)))
 
-__device__ inline void load4(const GLOBAL float* p, int n, float (&f)[4]) {
-  if (n >= 4) {
-    const f32x4_any q = __builtin_nontemporal_load((const GLOBAL f32x4_any*)p);
+// As they are stored: what waits for its use between load and arithmetic.
+template <typename T> struct Raw4;
+template <> struct Raw4<float> { f32x4_any v; };
+template <> struct Raw4<bf16> { u32x2 v; };
+__device__ inline Raw4<float> load4(const GLOBAL float* p, int n) {
+  if (n >= 4) return {__builtin_nontemporal_load((const GLOBAL f32x4_any*)p)};
+  Raw4<float> r = {{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = q[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = e < n ? p[e] : 0.f;
-  }
+  for (int e = 0; e < 3; ++e)
+    if (e < n) r.v[e] = p[e];
+  return r;
 }
-__device__ inline void load4(const GLOBAL bf16* p, int n, float (&f)[4]) {
-  if (n >= 4) {
-    const u32x2_any q = __builtin_nontemporal_load((const GLOBAL u32x2_any*)p);
-    f[0] = __uint_as_float(q[0] << 16);
-    f[1] = __uint_as_float(q[0] & 0xffff0000u);
-    f[2] = __uint_as_float(q[1] << 16);
-    f[3] = __uint_as_float(q[1] & 0xffff0000u);
-  } else {
+__device__ inline Raw4<bf16> load4(const GLOBAL bf16* p, int n) {
+  if (n >= 4) return {(u32x2)__builtin_nontemporal_load((const GLOBAL u32x2_any*)p)};
+  const GLOBAL uint16_t* h = (const GLOBAL uint16_t*)p;
+  Raw4<bf16> r = {{0, 0}};               // (written where they belong, so that nothing waits for them here)
+  if (n == 1) r.v[0] = *h;
+  if (n >= 2) r.v[0] = *(const GLOBAL u32_half*)h;
+  if (n == 3) r.v[1] = h[2];
+  return r;
+}
+__device__ inline void unpack(const Raw4<float>& r, float (&f)[4]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = e < n ? (float)p[e] : 0.f;
-  }
+  for (int e = 0; e < 4; ++e) f[e] = r.v[e];
+}
+__device__ inline void unpack(const Raw4<bf16>& r, float (&f)[4]) {
+  f[0] = __uint_as_float(r.v[0] << 16);
+  f[1] = __uint_as_float(r.v[0] & 0xffff0000u);
+  f[2] = __uint_as_float(r.v[1] << 16);
+  f[3] = __uint_as_float(r.v[1] & 0xffff0000u);
 }
 __device__ inline void store4(GLOBAL float* p, int n, const float (&f)[4]) {
   if (n >= 4) {
@@ -90,13 +100,16 @@ __device__ inline void store4(GLOBAL bf16* p, int n, const float (&f)[4]) {
       if (e < n) p[e] = (bf16)f[e];
   }
 }
-__device__ inline uint32_t load_codes(const GLOBAL uint8_t* p, int n) {
-  if (n >= 4) return __builtin_nontemporal_load((const GLOBAL u32_any*)p);
-  uint32_t q = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (e < n) q |= (uint32_t)p[e] << (8 * e);
-  return q;
+struct Codes {
+  uint32_t low, third;                   // the third of three comes apart
+};
+__device__ inline Codes load_codes(const GLOBAL uint8_t* p, int n) {
+  Codes c = {0, 0};
+  if (n >= 4) c.low = __builtin_nontemporal_load((const GLOBAL u32_any*)p);
+  if (n == 1) c.low = *p;
+  if (n == 2 || n == 3) c.low = *(const GLOBAL u16_any*)p;
+  if (n == 3) c.third = p[2];
+  return c;
 }
 __device__ inline void store_codes(GLOBAL uint8_t* p, int n, uint32_t q) {
   if (n >= 4) {
@@ -154,8 +167,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
   GLOBAL float *const scale1 = (GLOBAL float*)t.c1, *const scale2 = (GLOBAL float*)t.c2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float keep = 1.f - rule.lr * t.decay;
+  Raw4<P> p0[U];
+  Raw4<float> m0[U], v0[U];
   float p[U][4], m[U][4], v[U][4], g[U][4], c1[U], c2[U];
-  uint32_t q1[U], q2[U];
+  Codes q1[U], q2[U];
   int64_t at[U];
   int n[U];
 #pragma unroll
@@ -163,42 +178,50 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
     const int64_t begin = (int64_t)chunk.at * CHUNK + (wave * U + u) * BLOCK, left = t.n - begin - 4 * lane;
     at[u] = begin + 4 * lane;
     n[u] = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-    load4(param + at[u], n[u], p[u]);
+    p0[u] = load4(param + at[u], n[u]);
     if (EIGHT) {
       c1[u] = begin < t.n ? scale1[begin / BLOCK] : 0.f;
       c2[u] = begin < t.n ? scale2[begin / BLOCK] : 0.f;
       q1[u] = load_codes(codes1 + at[u], n[u]);
       q2[u] = load_codes(codes2 + at[u], n[u]);
     } else {
-      load4(state1 + at[u], n[u], m[u]);
-      load4(state2 + at[u], n[u], v[u]);
+      m0[u] = load4(state1 + at[u], n[u]);
+      v0[u] = load4(state2 + at[u], n[u]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) g[u][e] = 0.f;
   }
   constexpr int KS = 4;                   // workers whose gradients are asked for together
   for (int k0 = 0; k0 < workers.n; k0 += KS) {
-    float d[KS][U][4];
+    Raw4<G> d0[KS][U];
 #pragma unroll
     for (int k = 0; k < KS; ++k)
       if (k0 + k < workers.n)
 #pragma unroll
-        for (int u = 0; u < U; ++u) load4(grad + workers.index[k0 + k] * worker_stride + at[u], n[u], d[k][u]);
+        for (int u = 0; u < U; ++u) d0[k][u] = load4(grad + workers.index[k0 + k] * worker_stride + at[u], n[u]);
 #pragma unroll
     for (int k = 0; k < KS; ++k)
       if (k0 + k < workers.n)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+          float d[4];
+          unpack(d0[k][u], d);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) g[u][e] += workers.w[k0 + k] * d[k][u][e];
+          for (int e = 0; e < 4; ++e) g[u][e] += workers.w[k0 + k] * d[e];
+        }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (EIGHT) {
+    unpack(p0[u], p[u]);
+    if (!EIGHT) {
+      unpack(m0[u], m[u]);
+      unpack(v0[u], v[u]);
+    } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float r = decode<8>(q2[u], e, c2[u], c2[u] * 0x1p-15f);
-        m[u][e] = signed_as(decode<7>(q1[u], e, c1[u], c1[u] * 0x1p-15f), q1[u], e);
+        const uint32_t a1 = q1[u].low | q1[u].third << 16, a2 = q2[u].low | q2[u].third << 16;
+        const float r = decode<8>(a2, e, c2[u], c2[u] * 0x1p-15f);
+        m[u][e] = signed_as(decode<7>(a1, e, c1[u], c1[u] * 0x1p-15f), a1, e);
         v[u][e] = r * r;
       }
     }
@@ -248,7 +271,7 @@ __global__ __launch_bounds__(256) void read_states_kernel(const Tensor* tensors,
   const Tensor t = tensors[chunk.tensor];
   GLOBAL T *const to1 = (GLOBAL T*)out.a[chunk.tensor - first_tensor], *const to2 = (GLOBAL T*)out.b[chunk.tensor - first_tensor];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  uint32_t q1[U], q2[U];
+  Codes q1[U], q2[U];
   float c1[U], c2[U];
   int64_t at[U];
   int n[U];
@@ -267,8 +290,9 @@ __global__ __launch_bounds__(256) void read_states_kernel(const Tensor* tensors,
     float m[4], v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float r = decode<8>(q2[u], e, c2[u], c2[u] * 0x1p-15f);
-      m[e] = signed_as(decode<7>(q1[u], e, c1[u], c1[u] * 0x1p-15f), q1[u], e);
+      const uint32_t a1 = q1[u].low | q1[u].third << 16, a2 = q2[u].low | q2[u].third << 16;
+      const float r = decode<8>(a2, e, c2[u], c2[u] * 0x1p-15f);
+      m[e] = signed_as(decode<7>(a1, e, c1[u], c1[u] * 0x1p-15f), a1, e);
       v[e] = r * r;
     }
     store4(to1 + at[u], n[u], m);
@@ -298,12 +322,11 @@ template <typename P, typename G>
 void launch_step(const dynb_adamw* h, const Pointers& g, int first, int64_t blocks, int64_t stride, const Workers& w,
                  const Rule& r, hipStream_t st) {
   const Chunk* c = h->d_chunks + h->first_chunk[first];
+  const dim3 grid((unsigned)blocks), block(256);
   if (h->state == DYNB_STATE_8BIT)
-    hipLaunchKernelGGL((adamw_kernel<P, G, true>), dim3((unsigned)blocks), dim3(256), 0, st, h->d_tensors, c, g, first,
-                       stride, w, r);
+    hipLaunchKernelGGL((adamw_kernel<P, G, true>), grid, block, 0, st, h->d_tensors, c, g, first, stride, w, r);
   else
-    hipLaunchKernelGGL((adamw_kernel<P, G, false>), dim3((unsigned)blocks), dim3(256), 0, st, h->d_tensors, c, g, first,
-                       stride, w, r);
+    hipLaunchKernelGGL((adamw_kernel<P, G, false>), grid, block, 0, st, h->d_tensors, c, g, first, stride, w, r);
 }
 }  // namespace
 
@@ -331,7 +354,7 @@ extern "C" int dynb_adamw_create(const dynb_adamw_desc* d, dynb_adamw** out) {
       return fail(DYNB_ERR_BADARG, "adamw: tensor %d: a pointer is not a multiple of its element's size", i);
     chunks += (t.n + CHUNK - 1) / CHUNK;
   }
-  if (chunks > (1 << 24)) return fail(DYNB_ERR_UNSUPPORTED, "adamw: more than 2^36 elements");
+  if (chunks >= (1 << 24)) return fail(DYNB_ERR_UNSUPPORTED, "adamw: more than 2^35 elements");
   dynb_adamw* h = new (std::nothrow) dynb_adamw;
   if (!h) return fail(DYNB_ERR_STATE, "adamw: out of host memory");
   try {
@@ -398,7 +421,7 @@ extern "C" int dynb_adamw_step(dynb_adamw* h, const void* const* grads, const in
   for (int k = 0; k < K; ++k)
     if (b[k] > 0) {
       w.w[w.n] = (float)((double)b[k] / (double)seg.off[K]);
-      w.index[w.n++] = (uint8_t)k;
+      w.index[w.n++] = k;
     }
   Rule r;
   r.lr = rule->lr;

@@ -165,10 +165,11 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
     float s[N][GRANULE], ss = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      unpack(x[i], s[i]);
+      const int n = p.cols - (int)(t + i * 64 * waves) * GRANULE;
+      unpack(x[i], n, s[i]);
       if (p.residual) {
         float q[GRANULE];
-        unpack(res[i], q);
+        unpack(res[i], n, q);
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) s[i][e] += q[e];
       }
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
       const uint32_t c = (t + i * 64 * waves) * GRANULE;
       if (p.sum && c < (uint32_t)p.cols) store_part<PAST>((T*)p.sum + r * p.ld_sum + c, (int)(p.cols - c), s[i]);
       float g[GRANULE];
-      unpack(gain[i], g);
+      unpack(gain[i], p.gain ? (int)(p.cols - c) : GRANULE, g);
 #pragma unroll
       for (int e = 0; e < GRANULE; ++e) s[i][e] *= rstd * g[e];     // (elements that do not exist are zeros)
       if (OUT == DYNB_OUT_SAME && c < (uint32_t)p.cols) store_part<PAST>((T*)p.y + r * p.ld_y + c, (int)(p.cols - c), s[i]);
@@ -421,10 +422,11 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
     if (AHEAD && r + PER < end) ask(r + PER);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      const int n = p.cols - (int)(t + i * 64 * waves) * GRANULE;
       float a[GRANULE], d[GRANULE], g[GRANULE];
-      unpack(s0[i], a);
-      unpack(dy0[i], d);
-      unpack(gain[i], g);
+      unpack(s0[i], n, a);
+      unpack(dy0[i], n, d);
+      unpack(gain[i], p.gain ? n : GRANULE, g);
 #pragma unroll
       for (int e = 0; e < GRANULE; ++e) {
         const float q = d[e] * (a[e] * rstd0);
@@ -437,14 +439,15 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
     for (int i = 0; i < N; ++i) {
       const uint32_t c = (t + i * 64 * waves) * GRANULE;
       if (c >= (uint32_t)p.cols) continue;
+      const int n = p.cols - (int)(t + i * 64 * waves) * GRANULE;
       float a[GRANULE], d[GRANULE], g[GRANULE];
-      unpack(s0[i], a);
-      unpack(dy0[i], d);
-      unpack(gain[i], g);
+      unpack(s0[i], n, a);
+      unpack(dy0[i], n, d);
+      unpack(gain[i], p.gain ? n : GRANULE, g);
 #pragma unroll
       for (int e = 0; e < GRANULE; ++e) a[e] = rstd0 * (g[e] * d[e] - a[e] * rstd0 * c1);
       if (p.dsum) {
-        unpack(ds0[i], d);
+        unpack(ds0[i], n, d);
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
       }

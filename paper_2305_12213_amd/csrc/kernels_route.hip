@@ -220,7 +220,7 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void g
     for (int c = threadIdx.x % L * GRANULE; c < p.cols; c += L * GRANULE) {
       const int n = p.cols - c;
       float v[GRANULE];
-      unpack(load_raw<PAST>((const T*)p.in + t * p.ld_in + c, n), v);
+      unpack(load_raw<PAST>((const T*)p.in + t * p.ld_in + c, n), n, v);
       for (int j0 = 0; j0 < p.top_k; j0 += JS) {
         int s[JS];
 #pragma unroll
@@ -254,12 +254,12 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void c
 #pragma unroll
         for (int u = 0; u < JS; ++u)
           if (s[u] >= 0) row[u] = load_raw<PAST>((const T*)p.in + (int64_t)s[u] * p.ld_in + c, n);
-        if (j0 == 0 && p.addend) unpack(add, a);
+        if (j0 == 0 && p.addend) unpack(add, n, a);
 #pragma unroll
         for (int u = 0; u < JS; ++u) {
           if (s[u] < 0) continue;
           float v[GRANULE];
-          unpack(row[u], v);
+          unpack(row[u], n, v);
 #pragma unroll
           for (int e = 0; e < GRANULE; ++e) a[e] += w[u] * v[e];
         }
@@ -336,12 +336,12 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void c
 #pragma unroll
         for (int u = 0; u < JS; ++u)
           if (s[u] >= 0) row[u] = load_raw<PAST>((const T*)p.sorted + (int64_t)s[u] * p.ld_sorted + c, n);
-        unpack(dout, g);
+        unpack(dout, n, g);
 #pragma unroll
         for (int u = 0; u < JS; ++u) {
           if (s[u] < 0) continue;
           float y[GRANULE];
-          unpack(row[u], y);
+          unpack(row[u], n, y);
 #pragma unroll
           for (int e = 0; e < GRANULE; ++e) {
             dot[u] += g[e] * y[e];

@@ -14,10 +14,10 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // A granule is 8 neighbouring elements of a row.  Vector accesses need no alignment beyond the element's on this
 // target: the memory pipeline splits what crosses a line.
 constexpr int GRANULE = 8;
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
-typedef uint32_t u32_any __attribute__((aligned(1)));
-typedef uint16_t u16_any __attribute__((aligned(1)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1), may_alias));
+typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
+typedef uint16_t u16_any __attribute__((aligned(1), may_alias));
 
 // PAST: the access passes the caches by (data that is used once and is more than they hold).
 template <bool PAST = false> __device__ inline u32x4 load16(const void* p) {
@@ -36,41 +36,25 @@ __device__ inline uint32_t two_bf16(float a, float b) {   // round to nearest ev
          ((uint32_t)__builtin_bit_cast(unsigned short, (bf16)b) << 16);
 }
 
-// A granule as it is stored, 4 (bf16) or 8 (fp32) registers: what waits for its use between load and arithmetic.
+// The first n of 8 elements of a row (n >= 8: all, n <= 0: none) as they are loaded, 4 (bf16) or 8 (fp32) registers: what
+// waits for its use between load and arithmetic.  What is left of a row's last granule is 4, 2 and 1 elements, as the
+// bits of n say: three accesses at most, which stay apart until unpack() puts them in their places, so that nothing waits
+// for them before.  Nothing past the n-th element is touched; zeros stand for the others.
 template <typename T> struct Raw;
 template <> struct Raw<bf16> { u32x4 a; };
 template <> struct Raw<float> { u32x4 a, b; };
-__device__ inline void unpack(const Raw<bf16>& r, float (&f)[GRANULE]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = __uint_as_float(r.a[e] << 16);
-    f[2 * e + 1] = __uint_as_float(r.a[e] & 0xffff0000u);
-  }
-}
-__device__ inline void unpack(const Raw<float>& r, float (&f)[GRANULE]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[e] = __uint_as_float(r.a[e]);
-    f[4 + e] = __uint_as_float(r.b[e]);
-  }
-}
-
-// The first n of 8 elements (n >= 8: all, n <= 0: none); zeros behind them, and nothing past the n-th is touched.  What is
-// left of a row's last granule is 4, 2 and 1 elements, as the bits of n say: three accesses at most.
 template <bool PAST = false> __device__ inline Raw<bf16> load_raw(const bf16* p, int n) {
   Raw<bf16> r = {{0, 0, 0, 0}};
   if (n >= GRANULE) {
     r.a = load16<PAST>(p);
   } else if (n > 0) {
-    u32x2 four = {0, 0};
-    uint32_t two = 0, one = 0;
-    if (n & 4) four = *(const u32x2_any*)p;
-    if (n & 2) two = *(const u32_any*)(p + (n & 4));
-    if (n & 1) one = *(const u16_any*)(p + n - 1);
-    r.a[0] = n & 4 ? four[0] : n & 2 ? two : one;
-    r.a[1] = n & 4 ? four[1] : n & 2 ? one : 0;
-    r.a[2] = n & 4 ? (n & 2 ? two : one) : 0;
-    r.a[3] = (n & 6) == 6 ? one : 0;
+    if (n & 4) {
+      const u32x2 four = *(const u32x2_any*)p;
+      r.a[0] = four[0];
+      r.a[1] = four[1];
+    }
+    if (n & 2) r.a[2] = *(const u32_any*)(p + (n & 4));
+    if (n & 1) r.a[3] = *(const u16_any*)(p + n - 1);
   }
   return r;
 }
@@ -80,17 +64,38 @@ template <bool PAST = false> __device__ inline Raw<float> load_raw(const float* 
     r.a = load16<PAST>(p);
     r.b = load16<PAST>(p + 4);
   } else if (n > 0) {
-    u32x4 four = {0, 0, 0, 0};
-    u32x2 two = {0, 0};
-    uint32_t one = 0;
-    if (n & 4) four = load16(p);
-    if (n & 2) two = *(const u32x2_any*)(p + (n & 4));
-    if (n & 1) one = *(const uint32_t*)(p + n - 1);
-    const u32x4 rest = {n & 2 ? two[0] : one, two[1], n & 2 ? one : 0, 0};
-    r.a = n & 4 ? four : rest;
-    r.b = n & 4 ? rest : r.b;
+    if (n & 4) r.a = load16(p);
+    if (n & 2) {
+      const u32x2 two = *(const u32x2_any*)(p + (n & 4));
+      r.b[0] = two[0];
+      r.b[1] = two[1];
+    }
+    if (n & 1) r.b[2] = *(const uint32_t*)(p + n - 1);
   }
   return r;
+}
+__device__ inline void unpack(Raw<bf16> r, int n, float (&f)[GRANULE]) {
+  if (n > 0 && n < GRANULE) {
+    const uint32_t first = n & 2 ? r.a[2] : r.a[3], second = n & 2 ? r.a[3] : 0u;   // behind the four
+    r.a = n & 4 ? u32x4{r.a[0], r.a[1], first, second} : u32x4{first, second, 0, 0};
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = __uint_as_float(r.a[e] << 16);
+    f[2 * e + 1] = __uint_as_float(r.a[e] & 0xffff0000u);
+  }
+}
+__device__ inline void unpack(Raw<float> r, int n, float (&f)[GRANULE]) {
+  if (n > 0 && n < GRANULE) {
+    const u32x4 rest = {n & 2 ? r.b[0] : r.b[2], r.b[1], n & 2 ? r.b[2] : 0u, 0};   // behind the four
+    r.b = n & 4 ? rest : u32x4{0, 0, 0, 0};
+    r.a = n & 4 ? r.a : rest;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[e] = __uint_as_float(r.a[e]);
+    f[4 + e] = __uint_as_float(r.b[e]);
+  }
 }
 template <bool PAST = false> __device__ inline void store_part(bf16* p, int n, const float (&f)[GRANULE]) {
   u32x4 a;
@@ -122,7 +127,7 @@ template <bool PAST = false> __device__ inline void store_part(float* p, int n, 
     if (n & 1) *(uint32_t*)(p + n - 1) = n & 2 ? rest[2] : rest[0];
   }
 }
-template <typename T> __device__ inline void load_part(const T* p, int n, float (&f)[GRANULE]) { unpack(load_raw(p, n), f); }
+template <typename T> __device__ inline void load_part(const T* p, int n, float (&f)[GRANULE]) { unpack(load_raw(p, n), n, f); }
 
 // Exchanges between lanes that need no LDS: within 2, 4, 8 and 16 lanes (after the step every lane of the group has
 // the same value, so that a mirrored partner is as good as the xor-ed one).
