@@ -206,7 +206,10 @@ def _check(rc):
 def _ptr(t):
     if t is None:
         return None
-    return t.data_ptr() if hasattr(t, "data_ptr") else int(t)
+    try:                                # (asking first whether there is a data_ptr costs as much again)
+        return t.data_ptr()
+    except AttributeError:
+        return int(t)
 
 
 def _stream(stream):
@@ -229,7 +232,10 @@ def _stream(stream):
 
 
 def _i32(values):
-    return (C.c_int32 * len(values))(*[int(v) for v in values])
+    try:
+        return (C.c_int32 * len(values))(*values)
+    except TypeError:                   # (other kinds of numbers)
+        return (C.c_int32 * len(values))(*[int(v) for v in values])
 
 
 def _f64(values):
