@@ -24,6 +24,9 @@ struct Segs {
   int off[DYNB_MAX_WORKERS + 1];
 };
 
+// Whether a pointer is no multiple of `size` (a power of two).
+inline bool off_by(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }
+
 // Prefix sums of the sizes b[K]; refuses null, K out of range, negative sizes and sums beyond 2^31 - 1 in `who`'s name.
 int segments_of(const int32_t* b, int32_t K, const char* who, Segs& s);
 

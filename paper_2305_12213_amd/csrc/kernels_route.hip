@@ -1,5 +1,10 @@
 // Tokens sorted by expert and back: the plan (a stable counting sort), the rows' way there, their weighted sum on the
-// way back, and the gradients.
+// way back, and the gradients:
+//   sorted[slot[t][j]] = x[t];  out[t] = addend[t] + sum_j w[t][j] sorted[slot[t][j]];
+//   dsorted[slot[t][j]] = w[t][j] dout[t], dw[t][j] = <dout[t], sorted[slot[t][j]]>, and dx is the sum without weights.
+// Memory bounds the rows: 16384 tokens of 2048 bf16 columns, 8 choices each, 604 MB there in 118 us and 671 MB back in 110 us
+// (5.1 and 6.1 TB/s), both gradients of 8192 of 4096 columns and 2 choices 335 MB in 60 us and 268 MB in 42 us.  Sums are fp32
+// in the order of the choices and rounded once; nothing is added by atomics but whole numbers.
 #include <hip/hip_runtime.h>
 
 #include "dynb_internal.h"
@@ -394,11 +399,6 @@ int lanes_of(int granules, int64_t rows) {
   return 64;
 }
 
-// Calls of more bytes than the caches keep until the next one reads them pass them by.  Sorting and combination of 2048
-// columns in bf16, 8 choices: 1024 tokens (38 and 42 MB) 30.2 us either way, 2048 tokens 46 us past the caches and 55 through
-// them, 16384 tokens 245 and 279; gradients of 4 choices: 1024 tokens (38 and 21 MB) 15.8 and 13.8, 2048 27.0 and 30.2.
-bool past_caches(double bytes) { return bytes > 64e6; }
-
 #define ROUTE_LAUNCH(name, L) \
   hipLaunchKernelGGL((name##_kernel<T, L, PAST>), dim3(grid_of(a.tokens, L)), dim3(256), 0, st, a)
 #define ROUTE_LAUNCHES(name)                                                 \
@@ -423,8 +423,6 @@ template <typename T> void launch_choice_grad(const RowArgs& a, hipStream_t st) 
   else
     hipLaunchKernelGGL((choice_grad_kernel<T, 256>), dim3(grid_of(a.choices, 256)), block, 0, st, a);
 }
-
-bool off_by(const void* p, size_t size) { return ((uintptr_t)p & (size - 1)) != 0; }
 
 int describe(const dynb_route_desc* d, const char* who) {
   if (!d) return fail(DYNB_ERR_BADARG, "%s: null pointer", who);
