@@ -2,7 +2,7 @@
 // way back, and the gradients:
 //   sorted[slot[t][j]] = x[t];  out[t] = addend[t] + sum_j w[t][j] sorted[slot[t][j]];
 //   dsorted[slot[t][j]] = w[t][j] dout[t], dw[t][j] = <dout[t], sorted[slot[t][j]]>, and dx is the sum without weights.
-// Memory bounds the rows: 16384 tokens of 2048 bf16 columns, 8 choices each, 604 MB there in 118 us and 671 MB back in 110 us
+// Memory bounds the rows: 16384 tokens of 2048 bf16 columns, 8 choices each, 604 MB there in 119 us and 671 MB back in 110 us
 // (5.1 and 6.1 TB/s), both gradients of 8192 of 4096 columns and 2 choices 335 MB in 60 us and 268 MB in 42 us.  Sums are fp32
 // in the order of the choices and rounded once; nothing is added by atomics but whole numbers.
 #include <hip/hip_runtime.h>
@@ -208,8 +208,17 @@ template <typename T> __device__ void clear_rows(const RowArgs& p, int64_t from)
       store_part((T*)p.out + r * p.ld_out + c, p.cols - c, zeros);
 }
 
+// What no kernel of a call writes (slots, weights, offsets): where the address is the same in the whole wave, the compiler
+// reads it by scalar instructions only if told so.  Both gradients of 8192 tokens of 4096 bf16 columns and 2 choices 60 us,
+// by vector loads 64; one token's 8 choices there in 3.3 and 3.7, back in 3.7 and 4.2.  Not so the plain copies and sums of
+// calls beyond the caches: 16384 tokens of 2048 bf16 columns, 8 choices there in 122 and 119 us, back in 113 and 110.
+template <bool SCALAR = true, typename V> __device__ inline V constant(const V* p, int64_t i) {
+  if constexpr (SCALAR) return ((const __attribute__((address_space(4))) V*)p)[i];
+  else return p[i];
+}
+
 // L lanes take a row, a granule each and another one L granules on; 256 / L rows per workgroup.  From 64 lanes on a row
-// is the same in the whole wave, and what belongs to it (slots, weights) is read by scalar instructions.
+// is the same in the whole wave, and what belongs to it (slots, weights) can be read by scalar instructions.
 template <int L> __device__ inline int64_t row_of_thread() {
   const int64_t r = (int64_t)blockIdx.x * (256 / L);
   return r + (L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L);
@@ -220,7 +229,7 @@ constexpr int JS = 8;
 
 // One load and top_k stores.
 template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void gather_kernel(RowArgs p) {
-  const int kept = p.offsets[p.n_experts];
+  const int kept = constant(p.offsets, p.n_experts);
   for (int64_t t = row_of_thread<L>(); t < p.tokens; t += (int64_t)gridDim.x * (256 / L))
     for (int c = threadIdx.x % L * GRANULE; c < p.cols; c += L * GRANULE) {
       const int n = p.cols - c;
@@ -229,7 +238,7 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void g
       for (int j0 = 0; j0 < p.top_k; j0 += JS) {
         int s[JS];
 #pragma unroll
-        for (int u = 0; u < JS; ++u) s[u] = j0 + u < p.top_k ? p.slot[t * p.top_k + j0 + u] : -1;
+        for (int u = 0; u < JS; ++u) s[u] = j0 + u < p.top_k ? constant<!PAST>(p.slot, t * p.top_k + j0 + u) : -1;
 #pragma unroll
         for (int u = 0; u < JS; ++u)
           if (s[u] >= 0) store_part<PAST>((T*)p.out + (int64_t)s[u] * p.ld_out + c, n, v);
@@ -253,8 +262,8 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void c
 #pragma unroll
         for (int u = 0; u < JS; ++u) {
           const bool is = j0 + u < p.top_k;
-          s[u] = is ? p.slot[t * p.top_k + j0 + u] : -1;
-          w[u] = is && p.weights ? p.weights[t * p.top_k + j0 + u] : 1.f;
+          s[u] = is ? constant<!PAST>(p.slot, t * p.top_k + j0 + u) : -1;
+          w[u] = is && p.weights ? constant<!PAST>(p.weights, t * p.top_k + j0 + u) : 1.f;
         }
 #pragma unroll
         for (int u = 0; u < JS; ++u)
@@ -289,13 +298,13 @@ template <int L> __device__ inline float lanes_sum(float v) {
 // combination of the rows' gradient behind it 13.8 us, by tokens 16.2.
 template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_kernel(RowArgs p) {
   __shared__ float red[2][MOST_WAVES];
-  const int kept = p.offsets[p.n_experts];
+  const int kept = constant(p.offsets, p.n_experts);
   int turn = 0;
   for (int64_t i = row_of_thread<L>(); i < p.choices; i += (int64_t)gridDim.x * (256 / L), turn ^= 1) {
-    const int64_t t = i / p.top_k, s = p.slot[i];
+    const int64_t t = i / p.top_k, s = constant(p.slot, i);
+    const float w = constant(p.weights, i);
     float dot = 0.f;
     if (s >= 0) {
-      const float w = p.weights[i];
       for (int c = threadIdx.x % L * GRANULE; c < p.cols; c += L * GRANULE) {
         float g[GRANULE], y[GRANULE];
         load_part((const T*)p.in + t * p.ld_in + c, p.cols - c, g);
@@ -319,7 +328,7 @@ template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_
 template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void combine_grad_kernel(RowArgs p) {
   constexpr int WAVES = L > 64 ? L / 64 : 1;          // of a row
   __shared__ float part[4][JS];
-  const int kept = p.offsets[p.n_experts];
+  const int kept = constant(p.offsets, p.n_experts);
   const int64_t mine = row_of_thread<L>() - (int64_t)blockIdx.x * (256 / L);
   for (int64_t first = (int64_t)blockIdx.x * (256 / L); first < p.tokens; first += (int64_t)gridDim.x * (256 / L)) {
     const int64_t t = first + mine;
@@ -329,8 +338,9 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void c
       float w[JS], dot[JS];
 #pragma unroll
       for (int u = 0; u < JS; ++u) {
-        s[u] = live && j0 + u < p.top_k ? p.slot[t * p.top_k + j0 + u] : -1;
-        w[u] = s[u] >= 0 ? p.weights[t * p.top_k + j0 + u] : 0.f;
+        const bool is = live && j0 + u < p.top_k;
+        s[u] = is ? constant(p.slot, t * p.top_k + j0 + u) : -1;
+        w[u] = is ? constant(p.weights, t * p.top_k + j0 + u) : 0.f;
         dot[u] = 0.f;
       }
       for (int c = threadIdx.x % L * GRANULE; live && c < p.cols; c += L * GRANULE) {
