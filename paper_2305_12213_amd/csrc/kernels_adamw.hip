@@ -2,8 +2,8 @@
 // and the 16-bit copy of the parameters, in one pass over all of them.
 //   g = sum_k lambda_k g_k, m += (1 - beta1) (g - m), v += (1 - beta2) (g^2 - v),
 //   p -= lr (decay p + (m / c1) / (sqrt(v / c2) + eps)),  all in fp32.
-// Memory bounds it: 54.5 M parameters of 16 workers in fp32 with a 16-bit copy 4.9 GB, 813 us (6.0 TB/s); 235 M parameters, one
-// bf16 gradient, 8-bit states 3.76 GB, 608 us (6.2 TB/s), their values read back 226 us (6.2 TB/s).  A wave takes 256
+// Memory bounds it: 54.5 M parameters of 16 workers in fp32 with a 16-bit copy 4.9 GB, 860 us (5.7 TB/s); 235 M parameters, one
+// bf16 gradient, 8-bit states 3.76 GB, 628 us (6.0 TB/s), their values read back 226 us (6.2 TB/s).  A wave takes 256
 // neighbouring elements, a scale's block, so that the largest magnitude is an exchange inside it; a table on the device
 // says which tensor a workgroup works on, so that one launch does all of up to 256 tensors.
 #include <hip/hip_runtime.h>
@@ -19,10 +19,11 @@ namespace dynb {
 namespace {
 
 constexpr int BLOCK = DYNB_STATE_BLOCK;   // elements that share a scale: a wave, 4 neighbouring ones per lane
-// Blocks of a wave (235 M parameters with 8-bit states: one 602 us, two 608, four 614, and 259, 226 and 235 for the values read
-// back; four leave small models too few workgroups: 267 thousand parameters of 7 workers 5.2, 5.2 and 8.0 us).
-constexpr int U = 2;
-constexpr int CHUNK = 4 * U * BLOCK;      // elements of a workgroup
+// Blocks of a wave.  8-bit states: two (117 M parameters, a step and its values read back, fp32 gradient 462 us, with one 477,
+// bf16 gradient 434 and 437).  fp32 states: one (54.5 M parameters of 16 workers 860 us, with two 890; 532 thousand of 16
+// workers 10.8 and 11.5).
+constexpr int blocks_of_wave(bool eight) { return eight ? 2 : 1; }
+constexpr int chunk_of(bool eight) { return 4 * blocks_of_wave(eight) * BLOCK; }   // elements of a workgroup
 
 struct Tensor {
   void *param, *copy, *s1, *s2;
@@ -32,7 +33,7 @@ struct Tensor {
   int32_t ordinal;
 };
 struct Chunk {
-  int32_t tensor, at;                     // elements [at * CHUNK, (at + 1) * CHUNK) of the tensor
+  int32_t tensor, at;                     // the at-th chunk of the tensor
 };
 constexpr int POINTERS = 256;             // tensors of a launch
 struct Pointers {
@@ -52,7 +53,8 @@ struct Rule {
 };
 
 // ---- 4 neighbouring elements, of which the first n exist ------------------------------------------------------
-// Every byte is used once a step: accesses pass the caches by (54.5 M parameters of 16 workers: 890 us, 935 through them).
+// Every byte is used once a step: accesses pass the caches by (54.5 M parameters of 16 workers, two
+// blocks to a wave: 890 us, 935 through them).
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
 typedef uint32_t u32_half __attribute__((aligned(2), may_alias));
 #define GLOBAL __attribute__((address_space(1)))
@@ -166,6 +168,7 @@ template <typename P, typename G, bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const Chunk* chunks, Pointers grads,
                                                     int first_tensor, int64_t worker_stride, Workers workers,
                                                     Rule rule) {
+  constexpr int U = blocks_of_wave(EIGHT), CHUNK = chunk_of(EIGHT);
   const Chunk chunk = chunks[blockIdx.x];
   const Tensor t = tensors[chunk.tensor];
   const GLOBAL G* const grad = (const GLOBAL G*)grads.p[chunk.tensor - first_tensor];
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
 #pragma unroll
     for (int e = 0; e < 4; ++e) g[u][e] = 0.f;
   }
-  constexpr int KS = 4;                   // workers whose gradients are asked for together
+  constexpr int KS = 8 / U;               // workers whose gradients are asked for together
   for (int k0 = 0; k0 < workers.n; k0 += KS) {
     Raw4<G> d0[KS][U];
 #pragma unroll
@@ -276,6 +279,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
 template <typename T>
 __global__ __launch_bounds__(256) void read_states_kernel(const Tensor* tensors, const Chunk* chunks, Pointers2 out,
                                                           int first_tensor) {
+  constexpr int U = blocks_of_wave(true), CHUNK = chunk_of(true);
   const Chunk chunk = chunks[blockIdx.x];
   const Tensor t = tensors[chunk.tensor];
   GLOBAL T *const to1 = (GLOBAL T*)out.a[chunk.tensor - first_tensor], *const to2 = (GLOBAL T*)out.b[chunk.tensor - first_tensor];
@@ -324,17 +328,20 @@ struct dynb_adamw {
 };
 
 namespace {
+constexpr int64_t MOST_GRID = 1 << 23;    // workgroups of a launch: fewer than 2^32 threads
 size_t tensor_bytes(const dynb_adamw* h) { return (size_t)round_up((int64_t)(h->tensors.size() * sizeof(Tensor)), 16); }
 
 template <typename P, typename G>
 void launch_step(const dynb_adamw* h, const Pointers& g, int first, int64_t blocks, int64_t stride, const Workers& w,
                  const Rule& r, hipStream_t st) {
   const Chunk* c = h->d_chunks + h->first_chunk[first];
-  const dim3 grid((unsigned)blocks), block(256);
-  if (h->state == DYNB_STATE_8BIT)
-    hipLaunchKernelGGL((adamw_kernel<P, G, true>), grid, block, 0, st, h->d_tensors, c, g, first, stride, w, r);
-  else
-    hipLaunchKernelGGL((adamw_kernel<P, G, false>), grid, block, 0, st, h->d_tensors, c, g, first, stride, w, r);
+  for (; blocks > 0; blocks -= MOST_GRID, c += MOST_GRID) {
+    const dim3 grid((unsigned)(blocks < MOST_GRID ? blocks : MOST_GRID)), block(256);
+    if (h->state == DYNB_STATE_8BIT)
+      hipLaunchKernelGGL((adamw_kernel<P, G, true>), grid, block, 0, st, h->d_tensors, c, g, first, stride, w, r);
+    else
+      hipLaunchKernelGGL((adamw_kernel<P, G, false>), grid, block, 0, st, h->d_tensors, c, g, first, stride, w, r);
+  }
 }
 }  // namespace
 
@@ -347,6 +354,7 @@ extern "C" int dynb_adamw_create(const dynb_adamw_desc* d, dynb_adamw** out) {
   if (d->state != DYNB_STATE_F32 && d->state != DYNB_STATE_8BIT) return fail(DYNB_ERR_BADARG, "adamw: unknown state type");
   if (d->n_tensors < 1) return fail(DYNB_ERR_BADARG, "adamw: at least one tensor");
   const bool eight = d->state == DYNB_STATE_8BIT;
+  const int64_t chunk = chunk_of(eight);
   int64_t chunks = 0;
   for (int i = 0; i < d->n_tensors; ++i) {
     const dynb_adamw_tensor& t = d->tensors[i];
@@ -360,9 +368,9 @@ extern "C" int dynb_adamw_create(const dynb_adamw_desc* d, dynb_adamw** out) {
     if (off_by(t.param, d->param_dtype == DYNB_F32 ? 4 : 2) || off_by(t.copy, 2) ||
         (!eight && (off_by(t.state1, 4) || off_by(t.state2, 4))) || (eight && (off_by(t.scale1, 4) || off_by(t.scale2, 4))))
       return fail(DYNB_ERR_BADARG, "adamw: tensor %d: a pointer is not a multiple of its element's size", i);
-    chunks += (t.n + CHUNK - 1) / CHUNK;
+    chunks += (t.n + chunk - 1) / chunk;
   }
-  if (chunks >= (1 << 24)) return fail(DYNB_ERR_UNSUPPORTED, "adamw: more than 2^35 elements");
+  if (chunks >= ((int64_t)1 << 35) / chunk) return fail(DYNB_ERR_UNSUPPORTED, "adamw: more than 2^35 elements");
   dynb_adamw* h = new (std::nothrow) dynb_adamw;
   if (!h) return fail(DYNB_ERR_STATE, "adamw: out of host memory");
   try {
@@ -374,7 +382,7 @@ extern "C" int dynb_adamw_create(const dynb_adamw_desc* d, dynb_adamw** out) {
       const dynb_adamw_tensor& t = d->tensors[i];
       h->tensors.push_back({t.param, t.copy, t.state1, t.state2, t.scale1, t.scale2, t.n, t.weight_decay, i});
       h->first_chunk.push_back((int64_t)h->chunks.size());
-      for (int64_t c = 0; c * CHUNK < t.n; ++c) h->chunks.push_back({i, (int32_t)c});
+      for (int64_t c = 0; c * chunk < t.n; ++c) h->chunks.push_back({i, (int32_t)c});
     }
     h->first_chunk.push_back((int64_t)h->chunks.size());
   } catch (...) {
