@@ -2,7 +2,7 @@
 //   s = x + residual, rstd = (mean s^2 + eps)^(-1/2), y = s rstd gain;
 //   dx = rstd (gain dy - shat mean(gain dy shat)) + dsum, dgain_k = sum over worker k's rows of dy shat, shat = s rstd.
 // About 8 and 12 operations per element: memory bounds it, 16384 x 8192 bf16 to fp8 160 us (939 MB, 5.9 TB/s), 4096 x 4096
-// forward 25 us (5.4 TB/s), gradients 28 - 32 us and 4.7 for the sums over chunks (142 MB in the first); small calls take what a
+// forward 25 us (5.4 TB/s), gradients 28 - 33 us and 4.7 for the sums over chunks (142 MB in the first); small calls take what a
 // launch takes.  Statistics, products and sums are fp32; s, y and dx are rounded once where they are stored, and y comes
 // from the s that has not been rounded.
 #include <hip/hip_runtime.h>
