@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256) void segments_kernel(const int32_t* offsets, c
   if (k == seg.K) lo = hi;
   const int from = k < seg.K ? seg.off[k] * top_k : 0;
   while (lo < hi) {
-    const int step = (hi - lo + 63) / 64;
+    const int step = (int)(((int64_t)hi - lo + 63) / 64);
     const int64_t at = lo + (int64_t)lane * step;
     const int below = __popcll(__ballot(at < hi && source[at < hi ? at : lo] < from));   // (a prefix of the lanes)
     if (below == 0) break;
@@ -300,7 +300,7 @@ template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_
   __shared__ float red[2][MOST_WAVES];
   const int kept = constant(p.offsets, p.n_experts);
   int turn = 0;
-  for (int64_t i = row_of_thread<L>(); i < p.choices; i += (int64_t)gridDim.x * (256 / L), turn ^= 1) {
+  for (int64_t i = row_of_thread<L>(); i < p.choices; i += (int64_t)gridDim.x * (256 / L)) {
     const int64_t t = i / p.top_k, s = constant(p.slot, i);
     const float w = constant(p.weights, i);
     float dot = 0.f;
@@ -317,6 +317,7 @@ template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_
         store_part((T*)p.out + s * p.ld_out + c, p.cols - c, g);
       }
       dot = L > 64 ? block_sum(dot, L / 64, red[turn]) : lanes_sum<(L < 64 ? L : 64)>(dot);
+      turn ^= 1;
     }
     if (threadIdx.x % L == 0) p.dweights[i] = dot;
   }

@@ -243,3 +243,55 @@ def test_offsets_beyond_32_bits(dynb):
     assert torch.equal(back[:, 0], (2 * n).to(torch.bfloat16))
     want = x[:, 0].float() ** 2 + x[:, -1].float() ** 2
     assert torch.equal(dw[:, 0], want) and torch.equal(dw[:, 1], want)
+
+
+def test_segments_of_almost_2_31_rows(dynb):
+    """One expert with 2^31 - 1 rows: where the workers begin."""
+    import torch
+    n = (1 << 31) - 1
+    b = [1 << 30, 7, 0, n - (1 << 30) - 7 - 1, 1]
+    d = binding.route_desc("bf16", 8, n, 1, 1)
+    source = torch.arange(n, device="cuda", dtype=torch.int32)
+    offsets = torch.tensor([0, n], device="cuda", dtype=torch.int32)
+    segments = torch.full((1, 6), -7, device="cuda", dtype=torch.int32)
+    binding.route_segments(d, offsets, source, b, segments)
+    torch.cuda.synchronize()
+    assert segments[0].tolist() == [0] + np.cumsum(np.array(b, np.int64)).tolist()
+
+
+def test_graph(dynb):
+    """Plan, sorting, combination and gradients recorded into a graph: every replay gives what the calls give."""
+    import torch
+    tokens, k, experts, cols, b = 900, 6, 40, 260, [500, 0, 400]
+    ids = torch.zeros(tokens, k, device="cuda", dtype=torch.int32)
+    x, w = torch.zeros(tokens, cols, device="cuda", dtype=torch.bfloat16), torch.rand(tokens, k, device="cuda")
+    d = binding.route_desc("bf16", cols, tokens, k, experts)
+    n = binding.route_workspace_bytes(d)
+    ws = torch.empty(max(16, n), device="cuda", dtype=torch.uint8)
+
+    def buffers():
+        ints = lambda *s: torch.full(s, -7, device="cuda", dtype=torch.int32)  # noqa: E731
+        rows = lambda r: torch.zeros(r, cols, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+        return dict(offsets=ints(experts + 1), slot=ints(tokens, k), source=ints(tokens * k), segments=ints(experts, 4),
+                    there=rows(tokens * k), back=rows(tokens), dsorted=rows(tokens * k), dw=torch.zeros(tokens, k, device="cuda"))
+
+    def calls(o):
+        binding.route_plan(d, ids, o["offsets"], o["slot"], o["source"], ws, n)
+        binding.route_segments(d, o["offsets"], o["source"], b, o["segments"])
+        binding.route_gather(d, x, o["offsets"], o["slot"], o["there"])
+        binding.route_combine(d, o["there"], o["slot"], w, x, o["back"])
+        binding.route_combine_backward(d, o["back"], o["there"], o["offsets"], o["slot"], w, o["dsorted"], o["dw"])
+
+    one, two = buffers(), buffers()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        calls(two)
+    for i in range(3):
+        x.normal_()
+        ids.copy_(torch.from_numpy(ids_of(tokens, k, experts, ("even", "holes", "skewed")[i])))
+        calls(one)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in one:
+            assert torch.equal(one[name].view(torch.uint8), two[name].view(torch.uint8)), name
