@@ -202,7 +202,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
       float g[GRANULE];
       unpack(gain[i], p.gain ? (int)(p.cols - c) : GRANULE, g);
 #pragma unroll
-      for (int e = 0; e < GRANULE; ++e) s[i][e] *= rstd * g[e];     // (elements that do not exist are zeros)
+      for (int e = 0; e < GRANULE; ++e) s[i][e] = s[i][e] * rstd * g[e];   // (elements that do not exist are zeros)
       if (OUT == DYNB_OUT_SAME && c < (uint32_t)p.cols) store_part<PAST>((T*)p.y + r * p.ld_y + c, (int)(p.cols - c), s[i]);
     }
     const int64_t now = r;

@@ -195,7 +195,8 @@ __device__ inline uint32_t block_max(uint32_t v, int waves, uint32_t* red) {
 }
 
 // Values of 8 bits with a scale: the largest magnitude's bits (a NaN's are above an infinity's) give scale and factor.
-// Below 2^-100 a block counts as zeros: the factor could overflow.
+// Below 2^-100 a block counts as zeros: the factor could overflow.  (Of a 16th of it: the hardware's reciprocal of values beyond
+// 2^126 is 0.)
 struct Scale {
   float scale, inv;
 };
@@ -203,7 +204,7 @@ __device__ inline Scale scale_of(uint32_t amax_bits, float top) {
   if (amax_bits >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.f};
   if (amax_bits < (27u << 23)) return {0.f, 0.f};
   const float a = __uint_as_float(amax_bits);
-  return {a * (1.f / top), top * __builtin_amdgcn_rcpf(a)};
+  return {a * (1.f / top), top * 0x1p-4f * __builtin_amdgcn_rcpf(a * 0x1p-4f)};
 }
 
 }  // namespace dynb

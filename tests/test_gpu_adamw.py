@@ -243,3 +243,53 @@ def test_graph(dynb):
         torch.cuda.synchronize()
         for a, b in zip(one.tensors, two.tensors):
             assert torch.equal(a["param"], b["param"]) and torch.equal(a["state1"], b["state1"])
+
+
+def test_states_near_the_largest_value(dynb):
+    """m of almost 2^128 in 8 bits (beta1 = 0: it is the gradient), v as large as its square allows."""
+    import torch
+    rng = np.random.default_rng(3)
+    for size, which in ((2e38, 0), (1e19, 1)):
+        c = Case([1000], [1], state="8bit")
+        x = rng.uniform(0.01, 1.5, 1000) * rng.choice([-1.0, 1.0], 1000) * size
+        c.grads[0, c.starts[0]:c.starts[0] + 1000] = torch.from_numpy(x.astype(np.float32)).cuda()
+        c.h.step([c.grads[0, c.starts[0]:]], [1], c.stride, step=1, seed=5, lr=1e-3, beta1=0.0, beta2=0.0, eps=1e-8)
+        torch.cuda.synchronize()
+        _, m, v = c.read()[0]
+        got, want = (m, x) if which == 0 else (np.sqrt(v), np.abs(x))
+        top = np.array([np.abs(x[i:i + 256]).max() for i in range(0, 1000, 256)]).repeat(256)[:1000]
+        # a step (1/8 or 1/16 of an octave, 2^-15 of the scale at least), and fp32's share
+        assert_within(got, want, np.maximum(np.abs(want) / (8 << which), top * 2.0 ** -17) * 1.01, "state")
+
+
+def test_offsets_beyond_32_bits(dynb):
+    """A tensor of more than 2^31 elements and a worker's gradients behind 2^31 others."""
+    import torch
+    n, tail = (1 << 31) + 700, 900
+    rng = np.random.default_rng(11)
+    g = torch.zeros(n, device="cuda", dtype=torch.bfloat16)
+    p, m, v = torch.zeros_like(g), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    for t, values in ((g, rng.standard_normal(tail)), (p, rng.standard_normal(tail))):
+        t[n - tail:] = torch.from_numpy(values).cuda().to(t.dtype)
+    before = host(p[n - tail:])
+    h = binding.AdamW([dict(n=n, param=p, copy=None, state1=m, state2=v, weight_decay=0.1)], "bf16", "bf16", "f32")
+    ws = torch.empty(h.workspace_bytes(), device="cuda", dtype=torch.uint8)
+    h.bind(ws, ws.numel())
+    h.step([g], [1], 0, step=1, **RULE)
+    torch.cuda.synchronize()
+    gh = host(g[n - tail:])
+    wp, wm, wv = oo.adamw(before, np.zeros(tail), np.zeros(tail), gh[None], [1], 0.1, step=1, **RULE)
+    assert_within(host(m[n - tail:]), wm, 16 * EPS * np.abs(gh), "m")
+    assert_within(host(v[n - tail:]), wv, 16 * EPS * gh * gh, "v")
+    assert_within(host(p[n - tail:]), wp, 1.01 * 2.0 ** -8 * np.abs(wp) + 32 * EPS * (np.abs(before) + RULE["lr"]), "p")
+    assert not bool(p[:4096].any()) and not bool(m[:4096].any()) and not bool(v[n - tail - 4096:n - tail].any())
+    # the second worker's gradients are the last elements of the same memory
+    q = torch.zeros(tail, device="cuda")
+    small = binding.AdamW([dict(n=tail, param=q, copy=None, state1=torch.zeros_like(q), state2=torch.zeros_like(q),
+                                weight_decay=0.0)], "f32", "bf16", "f32")
+    ws = torch.empty(small.workspace_bytes(), device="cuda", dtype=torch.uint8)
+    small.bind(ws, ws.numel())
+    small.step([g], [0, 3], n - tail, step=1, **RULE)
+    torch.cuda.synchronize()
+    wp, _, _ = oo.adamw(np.zeros(tail), np.zeros(tail), np.zeros(tail), np.stack([gh, gh]), [0, 3], 0.0, step=1, **RULE)
+    assert_within(host(q), wp, 64 * EPS * np.abs(wp) + 64 * EPS * RULE["lr"], "q")

@@ -282,3 +282,94 @@ def test_results_repeat(dynb):
     with torch.cuda.stream(side):
         again = backward([700, 0, 301, 1024], 1000, "bf16", dsum=True, gain=True)
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("out,block", [("same", 0), ("fp8", 0), ("fp8", 32), ("int8", 0), ("int8", 96)])
+@pytest.mark.parametrize("cols", [64, 200, 2050, 4100, 66000])
+@pytest.mark.parametrize("size,gain", [(1.0, 1e38), (1e30, 1e-15), (1e-10, 1e38), (3e18, 1e-20)])
+def test_extreme_rows_and_gains(dynb, out, block, cols, size, gain):
+    """Results near the largest fp32 value, and factors whose products would leave the range though the result does not."""
+    import torch
+    rng = np.random.default_rng([8, cols])
+    x = (rng.uniform(0.5, 1.5, (5, cols)) * rng.choice([-1.0, 1.0], (5, cols)) * size).astype(np.float32)
+    g = (rng.uniform(0.5, 1.5, cols) * gain).astype(np.float32)
+    eps = 1e-30
+    _, _, want = oo.rms_norm(x.astype(np.float64), None, g, eps)
+    d = binding.rms_norm_desc("f32", cols, out, block, eps)
+    n = binding.scale_blocks(d)
+    y = empty_rows(5, cols, "f32" if out == "same" else out)
+    scales = torch.full((5, max(1, n)), -7.0, device="cuda")
+    binding.rms_norm(d, 5, torch.from_numpy(x).cuda(), None, torch.from_numpy(g).cuda(), None, y, scales if n else None, None)
+    rel = chain(cols)
+    if out == "same":
+        assert_within(host(y), want, (rel + EPS) * np.abs(want), "y")
+        return
+    v = empty_rows(5, cols, "f32")
+    binding.dequantise(d, 5, y, scales, v, "f32")
+    ws = oo.block_scales(want, oo.FP8_TOP if out == "fp8" else oo.INT8_TOP, block)
+    assert_within(host(scales), ws, 2 * rel * ws, "scales")
+    per = np.repeat(ws, block or cols, axis=1)[:, :cols]
+    half = 0.5 * per if out == "int8" else np.maximum(np.abs(want) * 2.0 ** -4, per * 2.0 ** -10)
+    assert_within(host(v), want, half * (1 + 1e-3) + 4 * rel * np.abs(want) + EPS * (np.abs(want) + half), "values")
+
+
+def test_offsets_beyond_32_bits(dynb):
+    """Rows whose starts are 2^30 elements apart, forward and backward: the last one lies behind 4 GiB."""
+    import torch
+    rows, cols, ld = 4, 520, (1 << 30) + 3
+    rng, x = inputs(rows, cols, 9)
+    _, dy = inputs(rows, cols, 10)
+    big = torch.empty((rows - 1) * ld + cols, device="cuda", dtype=torch.bfloat16).as_strided((rows, cols), (ld, 1))
+    big.copy_(torch.from_numpy(x))
+    xh = host(big)
+    s, rstd, want = oo.rms_norm(xh, None, None, NORM_EPS)
+    y, r = torch.empty(rows, cols, device="cuda", dtype=torch.bfloat16), torch.empty(rows, device="cuda")
+    d = binding.rms_norm_desc("bf16", cols, "same", 0, NORM_EPS, ld, 0, ld, 0)
+    binding.rms_norm(d, rows, big, None, None, None, y, None, r)
+    rel = chain(cols)
+    assert_within(host(y), want, (rel + 1.01 * STORED["bf16"]) * np.abs(want), "y")
+    dyd = torch.from_numpy(dy).cuda().to(torch.bfloat16)
+    dx, dgain = torch.empty_like(y), torch.empty(1, cols, device="cuda")
+    n = binding.rms_norm_backward_workspace_bytes(d, [rows])
+    ws = torch.empty(max(1, n), device="cuda", dtype=torch.uint8)
+    binding.rms_norm_backward(d, [rows], big, r, None, dyd, None, dx, dgain, cols, ws, n)
+    wdx, wdg = oo.rms_norm_grad(xh, host(r), None, host(dyd), None, [rows])
+    mag = np.abs(host(dyd)) + np.abs(s * rstd[:, None]) * np.abs(host(dyd) * s * rstd[:, None]).mean(1)[:, None]
+    assert_within(host(dx), wdx, 4 * rel * mag * rstd[:, None] + 1.01 * STORED["bf16"] * np.abs(wdx), "dx")
+    assert_within(host(dgain), wdg, 4 * rel * np.abs(host(dyd) * s * rstd[:, None]).sum(0), "dgain")
+
+
+def test_graph(dynb):
+    """Forward with 8-bit rows, values and both gradients recorded into a graph: every replay gives what the calls give."""
+    import torch
+    rows, cols, b = 70, 1300, [40, 0, 30]
+    x = torch.randn(rows, cols, device="cuda").to(torch.bfloat16)
+    dy, gain = torch.randn_like(x), torch.randn(cols, device="cuda")
+    d, same = binding.rms_norm_desc("bf16", cols, "fp8", 0, NORM_EPS), binding.rms_norm_desc("bf16", cols, "same", 0, NORM_EPS)
+    n = binding.rms_norm_backward_workspace_bytes(same, b)
+    ws = torch.empty(max(1, n), device="cuda", dtype=torch.uint8)
+
+    def buffers():
+        return dict(y=torch.zeros(rows, cols, device="cuda", dtype=torch.float8_e4m3fn), v=torch.zeros_like(x),
+                    scales=torch.zeros(rows, 1, device="cuda"), rstd=torch.zeros(rows, device="cuda"), dx=torch.zeros_like(x),
+                    dgain=torch.zeros(3, cols, device="cuda"))
+
+    def calls(o):
+        binding.rms_norm(d, rows, x, None, gain, None, o["y"], o["scales"], o["rstd"])
+        binding.dequantise(d, rows, o["y"], o["scales"], o["v"], "bf16")
+        binding.rms_norm_backward(same, b, x, o["rstd"], gain, dy, None, o["dx"], o["dgain"], cols, ws, n)
+
+    one, two = buffers(), buffers()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        calls(two)
+    for _ in range(3):
+        x.normal_()
+        for t in two.values():
+            t.zero_()
+        calls(one)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in one:
+            assert torch.equal(one[name].view(torch.uint8), two[name].view(torch.uint8)), name
