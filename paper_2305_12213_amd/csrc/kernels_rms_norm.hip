@@ -80,57 +80,124 @@ template <typename F> __device__ inline float rstd_of(float ss, float inv_cols, 
   return 0x1p-80f / sqrtf(scaled_sum() * inv_cols);
 }
 
-// Rows of any width and scale blocks of any width, a workgroup per row that reads it two or three times: rows beyond WIDEST
-// granules (16384 elements), scale blocks beyond 512 columns or of no power of two.
+// Rows beyond WIDEST granules, and blocks that no group of lanes holds: a workgroup per row goes over it two or three times,
+// the later ones in the caches.  group: lanes that share a scale, -1 where it is no power of two up to 64 (then by LDS), 0
+// where all threads take a block at a time.  (4096 x 18432 bf16 with a residual 130 us, 4.6 TB/s, element by element 278; one row
+// of 20480 6.7 us.  To fp8 and back 4096 x 4096: blocks of 96 columns 59 us, a wave per block 121; of 1024 55 and 57.)
+constexpr int MOST_SLOTS = 64 * MOST_WAVES / 12;   // blocks of 96 columns, the narrowest that are no power of two
 template <typename T, int OUT>
-__global__ __launch_bounds__(256) void rms_norm_any_kernel(NormArgs p) {
+__global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_any_kernel(NormArgs p, int group) {
   __shared__ float red[3][MOST_WAVES];
-  __shared__ uint32_t redu[MOST_WAVES];
+  __shared__ uint32_t redu[2][MOST_WAVES], tops[3][MOST_SLOTS];
   constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
-  int turn = 0;
+  const int t = threadIdx.x, threads = blockDim.x, waves = threads >> 6;
+  int turn = 0, round = 0;
+  for (int i = t; i < 3 * MOST_SLOTS; i += threads) (&tops[0][0])[i] = 0;
+  __syncthreads();
   for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
-    const T* x = (const T*)p.x + r * p.ld_x;
-    const T* res = p.residual ? (const T*)p.residual + r * p.ld_residual : nullptr;
-    T* sum = p.sum ? (T*)p.sum + r * p.ld_sum : nullptr;
-    auto value = [&](int c) { return to_float(x[c]) + (res ? to_float(res[c]) : 0.f); };
-    float ss = 0.f;
-    for (int c = threadIdx.x; c < p.cols; c += 256) {
-      const float s = value(c);
-      ss += s * s;
-    }
-    ss = block_sum(ss, 4, red[turn]);
-    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() {
-      float a = 0.f;
-      for (int c = threadIdx.x; c < p.cols; c += 256) {
-        const float s = value(c) * 0x1p-80f;
-        a += s * s;
+    const T* const x = (const T*)p.x + r * p.ld_x;
+    const T* const res = p.residual ? (const T*)p.residual + r * p.ld_residual : nullptr;
+    auto values = [&](int c, float (&s)[GRANULE]) {
+      const Raw<T> a = load_raw(x + c, p.cols - c);
+      if (res) {
+        float q[GRANULE];
+        const Raw<T> b = load_raw(res + c, p.cols - c);
+        unpack(a, p.cols - c, s);
+        unpack(b, p.cols - c, q);
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) s[e] += q[e];
+      } else {
+        unpack(a, p.cols - c, s);
       }
-      return block_sum(a, 4, red[2]);
-    });
-    if (threadIdx.x == 0 && p.rstd) p.rstd[r] = rstd;
-    auto result = [&](float s, int c) { return s * rstd * (p.gain ? p.gain[c] : 1.f); };
-    if (OUT == DYNB_OUT_SAME) {
-      for (int c = threadIdx.x; c < p.cols; c += 256) {
-        const float s = value(c);
-        if (sum) sum[c] = (T)s;
-        ((T*)p.y)[r * p.ld_y + c] = (T)result(s, c);
+    };
+    auto sum_of_squares = [&](float factor) {
+      float ss = 0.f;
+      for (int c = t * GRANULE; c < p.cols; c += threads * GRANULE) {
+        float s[GRANULE];
+        values(c, s);
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) ss += (s[e] * factor) * (s[e] * factor);
       }
-      continue;
-    }
-    // (the lane that reads an element for the block's largest is the one that stores it: outputs may lie on inputs)
-    const bool whole = p.n_blocks == 1;
-    const int lane = whole ? threadIdx.x : threadIdx.x & 63, lanes = whole ? 256 : 64;
-    for (int b = whole ? 0 : threadIdx.x >> 6; b < p.n_blocks; b += whole ? 1 : 4) {
-      const int c0 = b * p.scale_block, c1 = min(c0 + p.scale_block, p.cols);
+      return ss;
+    };
+    const float ss = block_sum(sum_of_squares(1.f), waves, red[turn]);
+    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() { return block_sum(sum_of_squares(0x1p-80f), waves, red[2]); });
+    if (t == 0 && p.rstd) p.rstd[r] = rstd;
+    auto results = [&](int c, float (&s)[GRANULE]) {
+      if (!p.gain) {
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) s[e] *= rstd;
+        return;
+      }
+      float g[GRANULE];
+      load_part(p.gain + c, p.cols - c, g);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) s[e] = s[e] * rstd * g[e];
+    };
+    auto largest = [&](const float (&y)[GRANULE]) {                   // (elements that do not exist are zeros)
       uint32_t a = 0;
-      for (int c = c0 + lane; c < c1; c += lanes) a = max(a, __float_as_uint(result(value(c), c)) & 0x7fffffffu);
-      a = whole ? block_max(a, 4, redu) : wave_max(a);
-      const Scale s = scale_of(a, TOP);
-      if (lane == 0) p.scales[r * p.n_blocks + b] = s.scale;
-      for (int c = c0 + lane; c < c1; c += lanes) {
-        const float v = value(c);
-        if (sum) sum[c] = (T)v;
-        ((uint8_t*)p.y)[r * p.ld_y + c] = eight_bits<OUT>(result(v, c), s.inv);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) a = max(a, __float_as_uint(y[e]) & 0x7fffffffu);
+      return a;
+    };
+    auto keep = [&](int c, const float (&s)[GRANULE]) {
+      if (p.sum && c < p.cols) store_part((T*)p.sum + r * p.ld_sum + c, p.cols - c, s);
+    };
+    // (the lane that reads an element for the block's largest is the one that stores it: outputs may lie on inputs)
+    uint8_t* const y = (uint8_t*)p.y + r * p.ld_y;
+    if (OUT == DYNB_OUT_SAME) {
+      for (int c = t * GRANULE; c < p.cols; c += threads * GRANULE) {
+        float s[GRANULE];
+        values(c, s);
+        keep(c, s);
+        results(c, s);
+        store_part((T*)p.y + r * p.ld_y + c, p.cols - c, s);
+      }
+    } else if (group != 0) {              // a granule per thread, whole blocks to a round
+      const int lanes = p.scale_block / GRANULE, slots = threads / lanes, slot = t / lanes;
+      for (int c0 = 0; c0 < p.cols; c0 += slots * p.scale_block) {
+        const int c = c0 + t * GRANULE;
+        const bool mine = slot < slots && c < p.cols;
+        float s[GRANULE] = {};
+        if (mine) {
+          values(c, s);
+          keep(c, s);
+          results(c, s);
+        }
+        uint32_t a = largest(s);
+        if (group > 0) {
+          a = group_max(a, group);
+        } else {
+          if (mine) atomicMax(&tops[round][slot], a);                 // (whole numbers: any order)
+          __syncthreads();
+          if (mine) a = tops[round][slot];
+          if (t < MOST_SLOTS) tops[round == 0 ? 2 : round - 1][t] = 0;  // (read before this barrier, used behind the next)
+          round = round == 2 ? 0 : round + 1;
+        }
+        if (!mine) continue;
+        const Scale scale = scale_of(a, TOP);
+        if (t == slot * lanes) p.scales[r * p.n_blocks + c / p.scale_block] = scale.scale;
+        store_eight<OUT, false>(y + c, p.cols - c, s, scale.inv);
+      }
+    } else {
+      for (int b = 0; b < p.n_blocks; ++b) {
+        const int c0 = b * p.scale_block, c1 = min(c0 + p.scale_block, p.cols);
+        uint32_t a = 0;
+        for (int c = c0 + t * GRANULE; c < c1; c += threads * GRANULE) {
+          float s[GRANULE];
+          values(c, s);
+          results(c, s);
+          a = max(a, largest(s));
+        }
+        const Scale scale = scale_of(block_max(a, waves, redu[b & 1]), TOP);
+        if (t == 0) p.scales[r * p.n_blocks + b] = scale.scale;
+        for (int c = c0 + t * GRANULE; c < c1; c += threads * GRANULE) {
+          float s[GRANULE];
+          values(c, s);
+          keep(c, s);
+          results(c, s);
+          store_eight<OUT, false>(y + c, c1 - c, s, scale.inv);
+        }
       }
     }
   }
@@ -243,37 +310,6 @@ struct NormGradArgs {
   float inv_cols;
 };
 
-// Gradients of rows of any width: the rows' by a workgroup per row, the gain's by a thread per column.
-template <typename T>
-__global__ __launch_bounds__(256) void rms_norm_grad_any_kernel(NormGradArgs p) {
-  __shared__ float red[2][MOST_WAVES];
-  int turn = 0;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
-    const T *s = (const T*)p.sum + r * p.ld_sum, *dy = (const T*)p.dy + r * p.ld_dy;
-    const T* dsum = p.dsum ? (const T*)p.dsum + r * p.ld_dsum : nullptr;
-    T* dx = (T*)p.dx + r * p.ld_dx;
-    const float rstd = p.rstd[r];
-    float c1 = 0.f;
-    for (int c = threadIdx.x; c < p.cols; c += 256)
-      c1 += (p.gain ? p.gain[c] : 1.f) * to_float(dy[c]) * (to_float(s[c]) * rstd);
-    c1 = block_sum(c1, 4, red[turn]) * p.inv_cols;
-    for (int c = threadIdx.x; c < p.cols; c += 256) {
-      const float g = (p.gain ? p.gain[c] : 1.f) * to_float(dy[c]);
-      dx[c] = (T)(rstd * (g - to_float(s[c]) * rstd * c1) + (dsum ? to_float(dsum[c]) : 0.f));
-    }
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void rms_norm_gain_grad_kernel(NormGradArgs p, Segs seg) {
-  const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
-  if (c >= p.cols) return;
-  float a = 0.f;
-  for (int64_t r = seg.off[k]; r < seg.off[k + 1]; ++r)
-    a += to_float(((const T*)p.dy)[r * p.ld_dy + c]) * (to_float(((const T*)p.sum)[r * p.ld_sum + c]) * p.rstd[r]);
-  p.dgain[k * p.dgain_stride + c] = a;
-}
-
 // A thread takes 8 neighbouring values of a row at a time (16384 x 8192 fp8 to bf16: 74 us, 5.4 TB/s; two at a time 85 us).
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void dequantise_kernel(NormArgs p, int out, T* to, int64_t ld_to) {
@@ -347,12 +383,13 @@ template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream
   // lanes that share a scale: a power of two within a wave, or the whole row
   const int granules = (a.cols + GRANULE - 1) / GRANULE, lanes = a.scale_block / GRANULE;
   const bool whole = OUT == DYNB_OUT_SAME || a.n_blocks == 1;
-  const int group = whole ? 0 : lanes;
-  if (granules > WIDEST || (!whole && (lanes > 64 || (lanes & (lanes - 1))))) {
-    hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
+  const int waves = (granules + 63) / 64, threads = 64 * (waves < MOST_WAVES ? waves : MOST_WAVES);
+  const int group = whole || lanes > threads ? 0 : lanes > 64 || (lanes & (lanes - 1)) ? -1 : lanes;
+  if (granules > WIDEST || group < 0 || (group == 0 && !whole)) {
+    const dim3 block(threads);
+    hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), dim3(grid_of_rows(a.rows)), block, 0, st, a, group);
     return;
   }
-  const int waves = (granules + 63) / 64;
   if (waves == 1) launch_norm_as<T, OUT, false, 1>(a, 4, group, st);
   else if (waves == 2) launch_norm_as<T, OUT, false, 2>(a, 4, group, st);
   else if (waves <= ONE_GRANULE) launch_norm_as<T, OUT, true, 1>(a, waves, group, st);
@@ -483,6 +520,85 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
   }
 }
 
+// Gradients of rows beyond WIDEST granules, in two launches: the rows' by a workgroup per row that goes over it twice, the
+// gain's over a chunk's rows by a thread per granule, UNDER rows at a time.  (4096 x 18432 bf16 with dsum 210 us, moving 906 MB;
+// a thread per column and worker and single elements 1950.)
+template <typename T>
+__global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_grad_any_kernel(NormGradArgs p) {
+  __shared__ float red[2][MOST_WAVES];
+  const int threads = blockDim.x;
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
+    const T *const s = (const T*)p.sum + r * p.ld_sum, *const dy = (const T*)p.dy + r * p.ld_dy;
+    const float rstd = p.rstd[r];
+    auto values = [&](int c, float (&a)[GRANULE], float (&gd)[GRANULE]) {        // shat, gain dy
+      const int n = p.cols - c;
+      const Raw<T> s0 = load_raw(s + c, n), d0 = load_raw(dy + c, n);
+      float g[GRANULE];
+      if (p.gain) load_part(p.gain + c, n, g);
+      unpack(s0, n, a);
+      unpack(d0, n, gd);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) {
+        a[e] *= rstd;
+        if (p.gain) gd[e] *= g[e];
+      }
+    };
+    float c1 = 0.f;
+    for (int c = threadIdx.x * GRANULE; c < p.cols; c += threads * GRANULE) {
+      float a[GRANULE], gd[GRANULE];
+      values(c, a, gd);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) c1 += gd[e] * a[e];
+    }
+    c1 = block_sum(c1, threads >> 6, red[turn]) * p.inv_cols;
+    for (int c = threadIdx.x * GRANULE; c < p.cols; c += threads * GRANULE) {
+      float a[GRANULE], gd[GRANULE], d[GRANULE];
+      if (p.dsum) load_part((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c, d);
+      values(c, a, gd);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) a[e] = rstd * (gd[e] - a[e] * c1);
+      if (p.dsum)
+#pragma unroll
+        for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
+      store_part((T*)p.dx + r * p.ld_dx + c, p.cols - c, a);
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void rms_norm_gain_grad_kernel(NormGradArgs p, Segs seg, Chunks ch, float* partial) {
+  constexpr int UNDER = 4;
+  const int chunk = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * GRANULE, n = p.cols - c;
+  int k = 0;
+  while (k + 1 < seg.K && chunk >= ch.first[k + 1]) ++k;
+  const int64_t begin = seg.off[k] + (int64_t)(chunk - ch.first[k]) * ch.rows;
+  const int64_t end = begin + ch.rows < seg.off[k + 1] ? begin + ch.rows : seg.off[k + 1];
+  float acc[GRANULE] = {};
+  for (int64_t r = begin; r < end; r += UNDER) {
+    Raw<T> s[UNDER], dy[UNDER];
+    float rstd[UNDER];
+#pragma unroll
+    for (int u = 0; u < UNDER; ++u) {
+      const int some = r + u < end ? n : 0;
+      rstd[u] = r + u < end ? p.rstd[r + u] : 0.f;
+      s[u] = load_raw((const T*)p.sum + (r + u) * p.ld_sum + c, some);
+      dy[u] = load_raw((const T*)p.dy + (r + u) * p.ld_dy + c, some);
+    }
+#pragma unroll
+    for (int u = 0; u < UNDER; ++u) {
+      if (r + u >= end) break;
+      float a[GRANULE], d[GRANULE];
+      unpack(s[u], n, a);
+      unpack(dy[u], n, d);
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) acc[e] += d[e] * (a[e] * rstd[u]);
+    }
+  }
+  float* const to = ch.first[k + 1] - ch.first[k] == 1 ? p.dgain + k * p.dgain_stride : partial + (int64_t)chunk * p.cols;
+  store_part(to + c, n, acc);
+}
+
 // Sums of the workers' chunks, COLS columns per workgroup: GROUPS groups of threads take every GROUPS-th chunk, then the
 // groups are added in order.  Workers without rows get zeros; those with one chunk have their sum.
 template <int COLS, int GROUPS>
@@ -511,7 +627,7 @@ __global__ __launch_bounds__(COLS * GROUPS) void sum_chunks_kernel(const float* 
 // 38.7, 4096 x 4096 35.3 and 32.2).
 int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   const int granules = (cols + GRANULE - 1) / GRANULE;
-  const int64_t rows = seg.off[seg.K], target = granules <= 64 ? 1024 : 512;
+  const int64_t rows = seg.off[seg.K], target = granules <= 64 ? 1024 : granules <= WIDEST ? 512 : 128;
   int64_t of_chunk = (rows + target - 1) / target;
   if (granules <= 128) of_chunk = round_up(of_chunk < 4 ? 4 : of_chunk, 4);      // (a row for each wave)
   else if (of_chunk < 2) of_chunk = 2;
@@ -537,15 +653,13 @@ void launch_norm_grad_as(const NormGradArgs& a, const Segs& seg, const Chunks& c
 template <typename T>
 void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hipStream_t st) {
   const int granules = (a.cols + GRANULE - 1) / GRANULE;
-  if (granules > WIDEST) {
-    if (a.dgain)   // (first: dx may lie on dy)
-      hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((a.cols + 255) / 256, seg.K), dim3(256), 0, st, a, seg);
-    if (a.rows) hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(256), 0, st, a);
-    return;
-  }
   Chunks ch;
   const int n = chunks_of(seg, a.cols, ch);
-  if (n > 0) {
+  if (n > 0 && granules > WIDEST) {
+    if (a.dgain)   // (first: dx may lie on dy)
+      hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((granules + 255) / 256, n), dim3(256), 0, st, a, seg, ch, partial);
+    hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(64 * MOST_WAVES), 0, st, a);
+  } else if (n > 0) {
     const int waves = (granules + 63) / 64;
     if (granules <= 64) launch_norm_grad_as<T, false, 1>(a, seg, ch, 4, partial, st);
     else if (granules <= 128) launch_norm_grad_as<T, false, 2>(a, seg, ch, 4, partial, st);
@@ -573,7 +687,6 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
 // Bytes of the chunks' sums (none where every worker has one chunk at most).
 size_t partial_bytes(const Segs& seg, int cols) {
   Chunks ch;
-  if ((cols + GRANULE - 1) / GRANULE > WIDEST) return 0;
   const int n = chunks_of(seg, cols, ch);
   bool more = false;
   for (int k = 0; k < seg.K; ++k) more |= ch.first[k + 1] - ch.first[k] > 1;

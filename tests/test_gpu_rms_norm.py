@@ -373,3 +373,22 @@ def test_graph(dynb):
         torch.cuda.synchronize()
         for name in one:
             assert torch.equal(one[name].view(torch.uint8), two[name].view(torch.uint8)), name
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "int8"), ("bf16", "fp8")])
+@pytest.mark.parametrize("cols,block", [(12000, 8224), (40000, 8224), (20000, 8192), (66000, 33024), (300, 160), (2051, 224),
+                                        (9000, 736), (17000, 1056), (5000, 512), (5000, 544), (100, 96), (30000, 32)])
+@pytest.mark.parametrize("alias", [None, "in place"])
+def test_blocks_of_any_width(dynb, dtype, out, cols, block, alias):
+    forward(7, cols, dtype, out, block, residual=True, gain=cols % 3 == 0, pads=(1, 0, 0, 2), alias=alias)
+
+
+@pytest.mark.parametrize("b", [[9], [0, 3, 130, 0, 5], [2] * 20])
+@pytest.mark.parametrize("cols,dtype", [(16390, "f32"), (18432, "bf16"), (33001, "bf16")])
+def test_gradient_workers_of_wide_rows(dynb, b, cols, dtype):
+    backward(b, cols, dtype, dsum=True, gain=True)
+
+
+@pytest.mark.parametrize("cols,out,block", [(18001, "same", 0), (20000, "fp8", 96), (1000, "int8", 96)])
+def test_more_rows_than_workgroups_at_once(dynb, cols, out, block):
+    forward(1500, cols, "bf16", out, block, residual=True, gain=True)
