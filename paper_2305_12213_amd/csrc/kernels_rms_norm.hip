@@ -23,6 +23,15 @@ constexpr int WIDEST = 2 * 64 * MOST_WAVES;   // granules of the widest rows tha
 // x 8192: 58.2 us, with two 60.4).
 constexpr int ONE_GRANULE = 8, ONE_GRANULE_GRAD = MOST_WAVES;
 
+// Lanes of a row: 8, 16, 32 or 64, or whole waves.
+constexpr int WIDE = 128;
+template <int L> __device__ inline int row_in_block() {
+  return L == WIDE ? 0 : L == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x / L;
+}
+template <int L> __device__ inline float row_sum(float v, int waves, float* red) {
+  return L < 64 ? lanes_sum<L>(v) : block_sum(v, waves, red);
+}
+
 struct NormArgs {
   const void *x, *residual;
   const float* gain;
@@ -203,19 +212,20 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_any_kernel(NormArgs 
   }
 }
 
-// Rows that fit in registers, N granules per thread: one read, one write.  WIDE: a workgroup of as many waves as a row needs
-// takes a row at a time; else each of its four waves does.  A thread keeps its part of the gain over all rows of the
+// Rows that fit in registers, N granules per thread: one read, one write.  L lanes of a workgroup of four waves take a row at a
+// time (16384 x 64 bf16: 8 lanes 3.8 us, 64 9.0; 131072 x 128: 16 lanes 23.5, 64 36.0; x 256: 32 lanes 45.7, 64 49.1), or,
+// where L is WIDE, as many waves as a row needs.  A thread keeps its part of the gain over all rows of the
 // workgroup, and asks for the next row before it writes the present one in 8 bits.  group: lanes that share a scale (a
 // power of two), 0 where the whole row does.
-template <typename T, int OUT, bool WIDE, int N, bool PAST>
-__global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(NormArgs p, int group) {
-  constexpr int PER = WIDE ? 1 : 4;        // rows of a workgroup
+template <typename T, int OUT, int L, int N, bool PAST>
+__global__ __launch_bounds__(L == WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(NormArgs p, int group) {
+  constexpr int PER = L == WIDE ? 1 : 256 / L;   // rows of a workgroup
   constexpr float TOP = OUT == DYNB_OUT_FP8 ? FP8_TOP : INT8_TOP;
   __shared__ float red[3][MOST_WAVES];
   __shared__ uint32_t redu[2][MOST_WAVES];
-  const uint32_t waves = WIDE ? blockDim.x >> 6 : 1;
-  const uint32_t t = WIDE ? threadIdx.x : threadIdx.x & 63;
-  int64_t r = (int64_t)blockIdx.x * PER + (WIDE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  const uint32_t waves = L == WIDE ? blockDim.x >> 6 : 1;
+  const uint32_t t = L == WIDE ? threadIdx.x : threadIdx.x % L;
+  int64_t r = (int64_t)blockIdx.x * PER + row_in_block<L>();
   int turn = 0;
   Raw<T> x[N], res[N];
   auto ask = [&](int64_t row) {
@@ -251,14 +261,14 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
 #pragma unroll
       for (int e = 0; e < GRANULE; ++e) ss += s[i][e] * s[i][e];
     }
-    ss = block_sum(ss, waves, red[turn]);
+    ss = row_sum<L>(ss, waves, red[turn]);
     const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() {
       float a = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) a += (s[i][e] * 0x1p-80f) * (s[i][e] * 0x1p-80f);
-      return block_sum(a, waves, red[2]);
+      return row_sum<L>(a, waves, red[2]);
     });
     if (t == 0 && p.rstd) p.rstd[r] = rstd;
     uint32_t amax = 0;
@@ -281,7 +291,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_kernel(
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < GRANULE; ++e) amax = max(amax, __float_as_uint(s[i][e]) & 0x7fffffffu);
-      scale = scale_of(block_max(amax, waves, redu[turn]), TOP);
+      scale = scale_of(L < 64 ? group_max(amax, L) : block_max(amax, waves, redu[turn]), TOP);
       if (t == 0) p.scales[now] = scale.scale;
     }
 #pragma unroll
@@ -373,10 +383,11 @@ int resident(int64_t units, int threads) {
   return (int)(units < most ? units : most);
 }
 
-template <typename T, int OUT, bool WIDE, int N> void launch_norm_as(const NormArgs& a, int waves, int group, hipStream_t st) {
-  const dim3 block(64 * waves), grid(resident(WIDE ? a.rows : (a.rows + 3) / 4, 64 * waves));
-  if (past_caches(a.bytes)) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, WIDE, N, true>), grid, block, 0, st, a, group);
-  else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, WIDE, N, false>), grid, block, 0, st, a, group);
+template <typename T, int OUT, int L, int N> void launch_norm_as(const NormArgs& a, int waves, int group, hipStream_t st) {
+  constexpr int PER = L == WIDE ? 1 : 256 / L;
+  const dim3 block(64 * waves), grid(resident(((int64_t)a.rows + PER - 1) / PER, 64 * waves));
+  if (past_caches(a.bytes)) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, L, N, true>), grid, block, 0, st, a, group);
+  else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, L, N, false>), grid, block, 0, st, a, group);
 }
 
 template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream_t st) {
@@ -390,10 +401,13 @@ template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream
     hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), dim3(grid_of_rows(a.rows)), block, 0, st, a, group);
     return;
   }
-  if (waves == 1) launch_norm_as<T, OUT, false, 1>(a, 4, group, st);
-  else if (waves == 2) launch_norm_as<T, OUT, false, 2>(a, 4, group, st);
-  else if (waves <= ONE_GRANULE) launch_norm_as<T, OUT, true, 1>(a, waves, group, st);
-  else launch_norm_as<T, OUT, true, 2>(a, (waves + 1) / 2, group, st);
+  if (granules <= 8) launch_norm_as<T, OUT, 8, 1>(a, 4, group, st);
+  else if (granules <= 16) launch_norm_as<T, OUT, 16, 1>(a, 4, group, st);
+  else if (granules <= 32) launch_norm_as<T, OUT, 32, 1>(a, 4, group, st);
+  else if (waves == 1) launch_norm_as<T, OUT, 64, 1>(a, 4, group, st);
+  else if (waves == 2) launch_norm_as<T, OUT, 64, 2>(a, 4, group, st);
+  else if (waves <= ONE_GRANULE) launch_norm_as<T, OUT, WIDE, 1>(a, waves, group, st);
+  else launch_norm_as<T, OUT, WIDE, 2>(a, (waves + 1) / 2, group, st);
 }
 
 template <typename T> void launch_norm(const NormArgs& a, int out, hipStream_t st) {
@@ -402,22 +416,24 @@ template <typename T> void launch_norm(const NormArgs& a, int out, hipStream_t s
   else launch_norm_out<T, DYNB_OUT_INT8>(a, st);
 }
 
-// Both gradients of rows that fit in registers, N granules per thread, in one pass: the rows' gradient, and the gain's summed over the rows of a chunk (of one worker) in registers, then over the chunks by sum_chunks_kernel.
-// WIDE: a workgroup of as many waves as a row needs takes a row at a time; else each of its four waves takes every fourth row
-// of the chunk, and their sums are added in LDS.  A row's loads are issued while the row before it is reduced.
+// Both gradients of rows that fit in registers, N granules per thread, in one pass: the rows' gradient, and the gain's summed over
+// the rows of a chunk (of one worker) in registers, then over the chunks by sum_chunks_kernel.  L lanes take every (256 / L)-th
+// row of the chunk and their sums are added by exchanges and in LDS (131072 x 64 bf16: 8 lanes 18.2 us, 64 46.7); WIDE: a
+// workgroup of as many waves as a row needs takes a row at a time.  A row's loads are issued while the row before it is
+// reduced.
 struct Chunks {
   int rows;                               // of a chunk, the last one of a worker may be shorter
   int first[DYNB_MAX_WORKERS + 1];        // of each worker's chunks
 };
-template <typename T, bool WIDE, int N, bool PAST>
-__global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_kernel(NormGradArgs p, Segs seg, Chunks ch,
+template <typename T, int L, int N, bool PAST>
+__global__ __launch_bounds__(L == WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_kernel(NormGradArgs p, Segs seg, Chunks ch,
                                                                              float* partial) {
-  constexpr int PER = WIDE ? 1 : 4, COLS = 64 * N * GRANULE;
-  constexpr bool AHEAD = !WIDE || N == 1;  // (two granules, up to 16 waves: the next row would spill)
+  constexpr int PER = L == WIDE ? 1 : 256 / L, LANES = L == WIDE ? 64 : L, COLS = LANES * N * GRANULE;
+  constexpr bool AHEAD = L != WIDE || N == 1;  // (two granules, up to 16 waves: the next row would spill)
   __shared__ float red[2][MOST_WAVES];
-  __shared__ float sums[WIDE ? 1 : 3 * COLS];
-  const uint32_t waves = WIDE ? blockDim.x >> 6 : 1;
-  const uint32_t t = WIDE ? threadIdx.x : threadIdx.x & 63, wave = WIDE ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ float sums[L == WIDE ? 1 : 3 * COLS];
+  const uint32_t waves = L == WIDE ? blockDim.x >> 6 : 1;
+  const uint32_t t = L == WIDE ? threadIdx.x : threadIdx.x % L;
   int turn = 0;
   int k = 0;
   while (k + 1 < seg.K && (int)blockIdx.x >= ch.first[k + 1]) ++k;
@@ -435,7 +451,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
       if (p.dsum) ds[i] = load_raw<PAST>((const T*)p.dsum + r * p.ld_dsum + c, (int)(p.cols - c));
     }
   };
-  int64_t r = begin + wave;
+  int64_t r = begin + row_in_block<L>();
   if (AHEAD && r < end) ask(r);
   float acc[N][GRANULE];
   Raw<float> gain[N];
@@ -475,7 +491,7 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
         c1 += g[e] * q;
       }
     }
-    c1 = block_sum(c1, waves, red[turn]) * p.inv_cols;
+    c1 = row_sum<L>(c1, waves, red[turn]) * p.inv_cols;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint32_t c = (t + i * 64 * waves) * GRANULE;
@@ -496,20 +512,26 @@ __global__ __launch_bounds__(WIDE ? 64 * MOST_WAVES : 256) void rms_norm_grad_ke
     }
   }
   if (!p.dgain) return;
-  if (!WIDE) {
-    if (wave > 0)
+  if (L != WIDE) {                         // the rows of a wave by exchanges, the waves through LDS
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool mine = L >= 64 || (threadIdx.x & 63) < L;
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2)
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) acc[0][e] += __shfl_xor(acc[0][e], d);
+    if (wave > 0 && mine)
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < GRANULE; ++e) sums[(wave - 1) * COLS + e * 64 * N + i * 64 + t] = acc[i][e];
+        for (int e = 0; e < GRANULE; ++e) sums[(wave - 1) * COLS + e * LANES * N + i * LANES + t] = acc[i][e];
     __syncthreads();
-    if (wave > 0) return;
+    if (wave > 0 || !mine) return;
 #pragma unroll
     for (int w = 0; w < 3; ++w)
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < GRANULE; ++e) acc[i][e] += sums[w * COLS + e * 64 * N + i * 64 + t];
+        for (int e = 0; e < GRANULE; ++e) acc[i][e] += sums[w * COLS + e * LANES * N + i * LANES + t];
   }
   // a worker's only chunk is its sum
   float* const to = ch.first[k + 1] - ch.first[k] == 1 ? p.dgain + k * p.dgain_stride : partial + (int64_t)blockIdx.x * p.cols;
@@ -623,13 +645,14 @@ __global__ __launch_bounds__(COLS * GROUPS) void sum_chunks_kernel(const float* 
 }
 
 // How the workers' rows are cut, and how many chunks: enough workgroups for the chip, and rows enough in each that the
-// chunks' sums are a small part of what is read (1024 and 512 chunks: 40000 x 128 bf16 22.9 and 28.5 us, 20000 x 1000 41.0 and
-// 38.7, 4096 x 4096 35.3 and 32.2).
+// chunks' sums are a small part of what is read (512 and 1024 chunks: 16384 x 128 bf16 10.0 and 11.2 us, 16384 x 512 17.7 and
+// 19.0, 4096 x 4096 32.2 and 35.3; 512 and 256: 131072 x 128 29.0 and 35.1).  A chunk is whole rounds of a workgroup's rows.
 int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   const int granules = (cols + GRANULE - 1) / GRANULE;
-  const int64_t rows = seg.off[seg.K], target = granules <= 64 ? 1024 : granules <= WIDEST ? 512 : 128;
+  const int64_t rows = seg.off[seg.K], target = granules <= WIDEST ? 512 : 128;
   int64_t of_chunk = (rows + target - 1) / target;
-  if (granules <= 128) of_chunk = round_up(of_chunk < 4 ? 4 : of_chunk, 4);      // (a row for each wave)
+  const int at_once = granules <= 8 ? 32 : granules <= 16 ? 16 : granules <= 32 ? 8 : granules <= 128 ? 4 : 0;
+  if (at_once) of_chunk = round_up(of_chunk < at_once ? at_once : of_chunk, at_once);
   else if (of_chunk < 2) of_chunk = 2;
   ch.rows = (int)of_chunk;
   int n = 0;
@@ -641,13 +664,13 @@ int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   return n;
 }
 
-template <typename T, bool WIDE, int N>
+template <typename T, int L, int N>
 void launch_norm_grad_as(const NormGradArgs& a, const Segs& seg, const Chunks& ch, int waves, float* partial, hipStream_t st) {
   const dim3 grid(ch.first[seg.K]), block(64 * waves);
   if (past_caches((double)a.rows * a.cols * sizeof(T) * (3 + (a.dsum != nullptr))))
-    hipLaunchKernelGGL((rms_norm_grad_kernel<T, WIDE, N, true>), grid, block, 0, st, a, seg, ch, partial);
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, L, N, true>), grid, block, 0, st, a, seg, ch, partial);
   else
-    hipLaunchKernelGGL((rms_norm_grad_kernel<T, WIDE, N, false>), grid, block, 0, st, a, seg, ch, partial);
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, L, N, false>), grid, block, 0, st, a, seg, ch, partial);
 }
 
 template <typename T>
@@ -661,10 +684,13 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
     hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(64 * MOST_WAVES), 0, st, a);
   } else if (n > 0) {
     const int waves = (granules + 63) / 64;
-    if (granules <= 64) launch_norm_grad_as<T, false, 1>(a, seg, ch, 4, partial, st);
-    else if (granules <= 128) launch_norm_grad_as<T, false, 2>(a, seg, ch, 4, partial, st);
-    else if (waves <= ONE_GRANULE_GRAD) launch_norm_grad_as<T, true, 1>(a, seg, ch, waves, partial, st);
-    else launch_norm_grad_as<T, true, 2>(a, seg, ch, (waves + 1) / 2, partial, st);
+    if (granules <= 8) launch_norm_grad_as<T, 8, 1>(a, seg, ch, 4, partial, st);
+    else if (granules <= 16) launch_norm_grad_as<T, 16, 1>(a, seg, ch, 4, partial, st);
+    else if (granules <= 32) launch_norm_grad_as<T, 32, 1>(a, seg, ch, 4, partial, st);
+    else if (granules <= 64) launch_norm_grad_as<T, 64, 1>(a, seg, ch, 4, partial, st);
+    else if (granules <= 128) launch_norm_grad_as<T, 64, 2>(a, seg, ch, 4, partial, st);
+    else if (waves <= ONE_GRANULE_GRAD) launch_norm_grad_as<T, WIDE, 1>(a, seg, ch, waves, partial, st);
+    else launch_norm_grad_as<T, WIDE, 2>(a, seg, ch, (waves + 1) / 2, partial, st);
   }
   bool left = false;
   int most = 0;

@@ -282,17 +282,6 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void c
     }
 }
 
-// Sum over L neighbouring lanes (L <= 64), the same in all of them.
-template <int L> __device__ inline float lanes_sum(float v) {
-  if (L == 64) return wave_sum(v);
-  v += from_lane<DPP_XOR1>(v);
-  v += from_lane<DPP_XOR2>(v);
-  v += from_lane<DPP_HALF_MIRROR>(v);
-  v += from_lane<DPP_MIRROR>(v);
-  if (L == 32) v += __shfl_xor(v, 16);
-  return v;
-}
-
 // L lanes take a choice: its row of dsorted, and the product of the two rows.  For calls that the caches hold, where more and
 // shorter chains count (the gradient is read again for each choice): 1024 tokens of 4 choices of 2048 bf16 columns and the
 // combination of the rows' gradient behind it 13.8 us, by tokens 16.2.

@@ -152,6 +152,16 @@ __device__ inline float wave_sum(float v) {
   v += from_lane<DPP_MIRROR>(v);
   return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
 }
+// Over L neighbouring lanes (8, 16, 32 or 64), the same in all of them.
+template <int L> __device__ inline float lanes_sum(float v) {
+  if (L == 64) return wave_sum(v);
+  v += from_lane<DPP_XOR1>(v);
+  v += from_lane<DPP_XOR2>(v);
+  v += from_lane<DPP_HALF_MIRROR>(v);
+  if (L > 8) v += from_lane<DPP_MIRROR>(v);
+  if (L > 16) v += __shfl_xor(v, 16);
+  return v;
+}
 // Over groups of 2, 4, ... 64 neighbouring lanes (`lanes` the same in the whole wave).
 __device__ inline uint32_t group_max(uint32_t v, int lanes) {
   if (lanes > 1) v = max(v, from_lane<DPP_XOR1>(v));

@@ -392,3 +392,25 @@ def test_gradient_workers_of_wide_rows(dynb, b, cols, dtype):
 @pytest.mark.parametrize("cols,out,block", [(18001, "same", 0), (20000, "fp8", 96), (1000, "int8", 96)])
 def test_more_rows_than_workgroups_at_once(dynb, cols, out, block):
     forward(1500, cols, "bf16", out, block, residual=True, gain=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1, 7, 8, 33, 63, 64, 65, 100, 127, 128, 129, 200, 255, 256, 257, 480, 512])
+@pytest.mark.parametrize("rows", [1, 5, 31, 33, 4099])
+def test_narrow_rows(dynb, dtype, cols, rows):
+    """Several rows to a wave, some of them beyond the last: forward in each output, and the gradients of ragged workers."""
+    forward(rows, cols, dtype, "same", 0, residual=True, gain=True, pads=(1, 0, 2, 0))
+    forward(rows, cols, dtype, "fp8", 0, residual=False, gain=True)
+    forward(rows, cols, dtype, "int8", 32, residual=True, gain=False, pads=(0, 1, 0, 3))
+    backward([rows // 3, 0, rows - rows // 3], cols, dtype, dsum=True, gain=True)
+
+
+@pytest.mark.parametrize("cols", [40, 100, 200])
+def test_extremes_of_narrow_rows_stay_in_their_row(dynb, cols):
+    rng, x = inputs(40, cols, 12)
+    x[3] *= 1e30                      # squares overflow
+    x[4] = 0
+    x[5, 2] = np.inf
+    x[6, cols - 1] = np.nan
+    for out, block in (("same", 0), ("fp8", 0), ("int8", 32)):
+        forward(40, cols, "f32", out, block, residual=False, gain=False, x=x)
