@@ -43,14 +43,8 @@ struct NormArgs {
   double bytes;                            // of the call
 };
 
-// One value in 8 bits.  (Of a block with an infinity or NaN it does not matter which: its scale is NaN.)
-template <int OUT> __device__ inline uint8_t eight_bits(float v, float inv) {
-  const float t = v * inv;
-  if (OUT == DYNB_OUT_INT8) return (uint8_t)(int8_t)rintf(t);
-  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(t, t, 0, false) & 0xff);
-}
-
-// 8 neighbouring values, the first n of them.
+// 8 neighbouring values in 8 bits, the first n of them.  (Of a block with an infinity or NaN it does not matter which: its
+// scale is NaN.)
 template <int OUT, bool PAST>
 __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE], float inv) {
   u32x2 q;

@@ -35,8 +35,6 @@ template <bool PAST = false> __device__ inline void store16(void* p, const u32x4
   else *(u32x4_any*)p = v;
 }
 
-__device__ inline float to_float(float v) { return v; }
-__device__ inline float to_float(bf16 v) { return (float)v; }
 __device__ inline uint32_t two_bf16(float a, float b) {   // round to nearest even
   return (uint32_t)__builtin_bit_cast(unsigned short, (bf16)a) |
          ((uint32_t)__builtin_bit_cast(unsigned short, (bf16)b) << 16);
