@@ -7,6 +7,7 @@
 // from the s that has not been rounded.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "dynb_internal.h"
@@ -640,14 +641,16 @@ __global__ __launch_bounds__(COLS * GROUPS) void sum_chunks_kernel(const float* 
 
 // How the workers' rows are cut, and how many chunks: enough workgroups for the chip, and rows enough in each that the
 // chunks' sums are a small part of what is read (512 and 1024 chunks: 16384 x 128 bf16 10.0 and 11.2 us, 16384 x 512 17.7 and
-// 19.0, 4096 x 4096 32.2 and 35.3; 512 and 256: 131072 x 128 29.0 and 35.1).  A chunk is whole rounds of a workgroup's rows.
+// 19.0, 4096 x 4096 32.2 and 35.3; 512 and 256: 131072 x 128 29.0 and 35.1, 40000 x 2048 129 and 149).  256 where a workgroup has
+// 9 waves or more, or would have less than 6 rows (256 and 512: 4096 x 16384 105 and 111, 1531 x 2050 13.8 and 14.9, 1024 x 8192
+// 19.7 and 23.2).  A chunk is whole rounds of a workgroup's rows.
 int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   const int granules = (cols + GRANULE - 1) / GRANULE;
-  const int64_t rows = seg.off[seg.K], target = granules <= WIDEST ? 512 : 128;
-  int64_t of_chunk = (rows + target - 1) / target;
-  const int at_once = granules <= 8 ? 32 : granules <= 16 ? 16 : granules <= 32 ? 8 : granules <= 128 ? 4 : 0;
-  if (at_once) of_chunk = round_up(of_chunk < at_once ? at_once : of_chunk, at_once);
-  else if (of_chunk < 2) of_chunk = 2;
+  const int64_t rows = seg.off[seg.K];
+  const int target = granules > WIDEST ? 128 : granules > 512 || (granules > 128 && rows <= 5 * 512) ? 256 : 512;
+  const int at_once = granules <= 8 ? 32 : granules <= 16 ? 16 : granules <= 32 ? 8 : granules <= 128 ? 4 : 2;
+  const int64_t share = (rows + target - 1) / target;
+  const int64_t of_chunk = granules <= 128 ? round_up(std::max<int64_t>(share, 1), at_once) : std::max<int64_t>(share, at_once);
   ch.rows = (int)of_chunk;
   int n = 0;
   for (int k = 0; k < seg.K; ++k) {
