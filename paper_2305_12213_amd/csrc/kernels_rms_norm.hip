@@ -20,9 +20,11 @@ constexpr float FP8_TOP = 448.f, INT8_TOP = 127.f;
 constexpr int MAX_COLS = 1 << 20;
 constexpr int WIDEST = 2 * 64 * MOST_WAVES;   // granules of the widest rows that stay in registers
 // Rows of up to so many waves take one granule per thread, wider ones two (4096 bf16 columns: one row 3.2 us, with two granules
-// 3.8, 4096 rows 25.2 and 26.1; 8192 columns: 53.3 us with one, 49.9 with two).  Gradients: one as far as the waves go (4096
-// x 8192: 58.2 us, with two 60.4).
-constexpr int ONE_GRANULE = 8, ONE_GRANULE_GRAD = MOST_WAVES;
+// 3.8, 4096 rows 25.2 and 26.1; 8192 columns: 53.3 us with one, 49.9 with two).  8-bit outputs, there and back: 4096 x 6000 bf16
+// 50.0 us with one, 61.8 with two, 856 x 6437 22.2 and 19.6.  Gradients: one as far as the waves go (4096 x 8192: 58.2 us, with
+// two 60.4).
+constexpr int one_granule(int out) { return out == DYNB_OUT_SAME ? 8 : 12; }
+constexpr int ONE_GRANULE_GRAD = MOST_WAVES;
 
 // Lanes of a row: 8, 16, 32 or 64, or whole waves.
 constexpr int WIDE = 128;
@@ -401,7 +403,7 @@ template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream
   else if (granules <= 32) launch_norm_as<T, OUT, 32, 1>(a, 4, group, st);
   else if (waves == 1) launch_norm_as<T, OUT, 64, 1>(a, 4, group, st);
   else if (waves == 2) launch_norm_as<T, OUT, 64, 2>(a, 4, group, st);
-  else if (waves <= ONE_GRANULE) launch_norm_as<T, OUT, WIDE, 1>(a, waves, group, st);
+  else if (waves <= one_granule(OUT)) launch_norm_as<T, OUT, WIDE, 1>(a, waves, group, st);
   else launch_norm_as<T, OUT, WIDE, 2>(a, (waves + 1) / 2, group, st);
 }
 
