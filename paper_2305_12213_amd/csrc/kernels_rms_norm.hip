@@ -2,7 +2,7 @@
 //   s = x + residual, rstd = (mean s^2 + eps)^(-1/2), y = s rstd gain;
 //   dx = rstd (gain dy - shat mean(gain dy shat)) + dsum, dgain_k = sum over worker k's rows of dy shat, shat = s rstd.
 // About 8 and 12 operations per element: memory bounds it, 16384 x 8192 bf16 to fp8 160 us (939 MB, 5.9 TB/s), 4096 x 4096
-// forward 25 us (5.4 TB/s), gradients 28 - 33 us and 4.7 for the sums over chunks (142 MB in the first); small calls take what a
+// forward 25 us (5.4 TB/s), gradients 28 us and 4.7 for the sums over chunks (142 MB in the first); small calls take what a
 // launch takes.  Statistics, products and sums are fp32; s, y and dx are rounded once where they are stored, and y comes
 // from the s that has not been rounded.
 #include <hip/hip_runtime.h>
@@ -646,20 +646,27 @@ __global__ __launch_bounds__(COLS * GROUPS) void sum_chunks_kernel(const float* 
 // 19.0, 4096 x 4096 32.2 and 35.3; 512 and 256: 131072 x 128 29.0 and 35.1, 40000 x 2048 129 and 149).  256 where a workgroup has
 // 9 waves or more, or would have less than 6 rows (256 and 512: 4096 x 16384 105 and 111, 1531 x 2050 13.8 and 14.9, 1024 x 8192
 // 19.7 and 23.2).  A chunk is whole rounds of a workgroup's rows.
+// And no more of them than that where workers are ragged, or a few workgroups would run alone behind the others (4096 x 4096
+// of 16 workers: 519 chunks 39.3 us, 463 33.0; 4096 x 8192 of 8: 88 and 59.5).
 int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   const int granules = (cols + GRANULE - 1) / GRANULE;
   const int64_t rows = seg.off[seg.K];
   const int target = granules > WIDEST ? 128 : granules > 512 || (granules > 128 && rows <= 5 * 512) ? 256 : 512;
   const int at_once = granules <= 8 ? 32 : granules <= 16 ? 16 : granules <= 32 ? 8 : granules <= 128 ? 4 : 2;
-  const int64_t share = (rows + target - 1) / target;
-  const int64_t of_chunk = granules <= 128 ? round_up(std::max<int64_t>(share, 1), at_once) : std::max<int64_t>(share, at_once);
-  ch.rows = (int)of_chunk;
+  static_assert(DYNB_MAX_WORKERS < 128, "every worker has a chunk of its own");
   int n = 0;
-  for (int k = 0; k < seg.K; ++k) {
-    ch.first[k] = n;
-    n += (int)((seg.off[k + 1] - (int64_t)seg.off[k] + of_chunk - 1) / of_chunk);
+  for (int most : {target, target - seg.K}) {
+    const int64_t share = std::max<int64_t>((rows + most - 1) / most, 1);
+    const int64_t of_chunk = granules <= 128 ? round_up(share, at_once) : std::max<int64_t>(share, at_once);
+    ch.rows = (int)of_chunk;
+    n = 0;
+    for (int k = 0; k < seg.K; ++k) {
+      ch.first[k] = n;
+      n += (int)((seg.off[k + 1] - (int64_t)seg.off[k] + of_chunk - 1) / of_chunk);
+    }
+    ch.first[seg.K] = n;
+    if (n <= target) break;
   }
-  ch.first[seg.K] = n;
   return n;
 }
 
