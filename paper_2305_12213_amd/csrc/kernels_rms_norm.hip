@@ -647,7 +647,7 @@ __global__ __launch_bounds__(COLS * GROUPS) void sum_chunks_kernel(const float* 
 // 9 waves or more, or would have less than 6 rows (256 and 512: 4096 x 16384 105 and 111, 1531 x 2050 13.8 and 14.9, 1024 x 8192
 // 19.7 and 23.2).  A chunk is whole rounds of a workgroup's rows.
 // And no more of them than that where workers are ragged, or a few workgroups would run alone behind the others (4096 x 4096
-// of 16 workers: 519 chunks 39.3 us, 463 33.0; 4096 x 8192 of 8: 88 and 59.5).
+// of 16 workers: 519 chunks 39.3 us, 464 33.0; 4096 x 8192 of 8: 88 and 59.5).
 int chunks_of(const Segs& seg, int cols, Chunks& ch) {
   const int granules = (cols + GRANULE - 1) / GRANULE;
   const int64_t rows = seg.off[seg.K];
