@@ -18,12 +18,13 @@ EPS = 1e-5
 
 
 class ExpertBlock:
-    """Parameters, gradients [K][P] and optimizer states as flat vectors; work tensors for `max_tokens` rows."""
+    """Parameters, gradients [K][P] and optimizer states as flat vectors, for at most `max_tokens` rows of
+    `max_workers` workers."""
 
     def __init__(self, width, hidden, experts, top_k, classes, max_tokens, max_workers, dtype="bf16",
                  state="8bit", seed=0, device="cuda"):
         self.width, self.hidden, self.experts, self.top_k, self.classes = width, hidden, experts, top_k, classes
-        self.dtype, self.device = dtype, device
+        self.dtype, self.device, self.max_tokens, self.max_workers = dtype, device, max_tokens, max_workers
         self.t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         shapes = dict(gain1=(width,), router=(width, experts), w1=(experts, width, hidden),
                       w2=(experts, hidden, width), gain2=(width,), head=(width, classes))
@@ -76,6 +77,8 @@ class ExpertBlock:
     def gradients(self, h, labels, b):
         """Every worker's gradient into self.grads[:K]; returns the workers' mean losses (device)."""
         T, H, K, k, E = h.shape[0], self.width, len(b), self.top_k, self.experts
+        if T > self.max_tokens or K > self.max_workers or sum(b) != T:
+            raise ValueError("more rows or workers than the block was made for, or batch sizes that are not the rows")
         ints = dict(dtype=torch.int32)
         norm = binding.rms_norm_desc(self.dtype, H, eps=EPS)
         route = binding.route_desc(self.dtype, H, T, k, E)

@@ -57,3 +57,12 @@ def test_gradients_are_those_of_the_workers_losses(dynb, b):
 def test_it_learns(dynb):
     losses = expert_block.main(iterations=30, width=64, hidden=96, experts=6, top_k=2, classes=8, tokens=256)
     assert float(losses.mean()) < 0.5 * np.log(8)
+
+
+def test_it_refuses_more_than_it_was_made_for(dynb):
+    import torch
+    block = expert_block.ExpertBlock(48, 40, 5, 2, 7, 20, 2)
+    h, labels = torch.zeros(20, 48, device="cuda", dtype=torch.bfloat16), torch.zeros(20, device="cuda", dtype=torch.int32)
+    for b, rows in (([10, 5, 5], 20), ([10, 9], 20), ([10, 11], 21)):
+        with pytest.raises(ValueError):
+            block.gradients(h.new_zeros(rows, 48), labels, b)
