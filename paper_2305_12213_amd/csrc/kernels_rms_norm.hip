@@ -21,10 +21,12 @@ constexpr int MAX_COLS = 1 << 20;
 constexpr int WIDEST = 2 * 64 * MOST_WAVES;   // granules of the widest rows that stay in registers
 // Rows of up to so many waves take one granule per thread, wider ones two (4096 bf16 columns: one row 3.2 us, with two granules
 // 3.8, 4096 rows 25.2 and 26.1; 8192 columns: 53.3 us with one, 49.9 with two).  8-bit outputs, there and back: 4096 x 6000 bf16
-// 50.0 us with one, 61.8 with two, 856 x 6437 22.2 and 19.6.  Gradients: one as far as the waves go (4096 x 8192: 58.2 us, with
-// two 60.4).
+// 50.0 us with one, 61.8 with two, 856 x 6437 22.2 and 19.6.
 constexpr int one_granule(int out) { return out == DYNB_OUT_SAME ? 8 : 12; }
-constexpr int ONE_GRANULE_GRAD = MOST_WAVES;
+// Gradients take one granule as far as the waves go (4096 x 8192 bf16: 58.2 us, with two 60.4), then bf16 rows two; fp32 rows do
+// not fit in the registers then, and take the two launches of wider ones (4096 x 16384 355 us, with two granules 367; bf16 107 and
+// with two launches 189).
+constexpr int widest_grad(size_t element) { return element == 2 ? WIDEST : WIDEST / 2; }
 
 // Lanes of a row: 8, 16, 32 or 64, or whole waves.
 constexpr int WIDE = 128;
@@ -539,7 +541,7 @@ __global__ __launch_bounds__(L == WIDE ? 64 * MOST_WAVES : 256) void rms_norm_gr
   }
 }
 
-// Gradients of rows beyond WIDEST granules, in two launches: the rows' by a workgroup per row that goes over it twice, the
+// Gradients of rows beyond widest_grad() granules, in two launches: the rows' by a workgroup per row that goes over it twice, the
 // gain's over a chunk's rows by a thread per granule, UNDER rows at a time.  (4096 x 18432 bf16 with dsum 210 us, moving 906 MB;
 // a thread per column and worker and single elements 1950.)
 template <typename T>
@@ -684,7 +686,7 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
   const int granules = (a.cols + GRANULE - 1) / GRANULE;
   Chunks ch;
   const int n = chunks_of(seg, a.cols, ch);
-  if (n > 0 && granules > WIDEST) {
+  if (n > 0 && granules > widest_grad(sizeof(T))) {
     if (a.dgain)   // (first: dx may lie on dy)
       hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((granules + 255) / 256, n), dim3(256), 0, st, a, seg, ch, partial);
     hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(64 * MOST_WAVES), 0, st, a);
@@ -695,8 +697,8 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
     else if (granules <= 32) launch_norm_grad_as<T, 32, 1>(a, seg, ch, 4, partial, st);
     else if (granules <= 64) launch_norm_grad_as<T, 64, 1>(a, seg, ch, 4, partial, st);
     else if (granules <= 128) launch_norm_grad_as<T, 64, 2>(a, seg, ch, 4, partial, st);
-    else if (waves <= ONE_GRANULE_GRAD) launch_norm_grad_as<T, WIDE, 1>(a, seg, ch, waves, partial, st);
-    else launch_norm_grad_as<T, WIDE, 2>(a, seg, ch, (waves + 1) / 2, partial, st);
+    else if (waves <= MOST_WAVES) launch_norm_grad_as<T, WIDE, 1>(a, seg, ch, waves, partial, st);
+    else if constexpr (sizeof(T) == 2) launch_norm_grad_as<T, WIDE, 2>(a, seg, ch, (waves + 1) / 2, partial, st);
   }
   bool left = false;
   int most = 0;

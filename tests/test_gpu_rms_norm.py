@@ -414,3 +414,10 @@ def test_extremes_of_narrow_rows_stay_in_their_row(dynb, cols):
     x[6, cols - 1] = np.nan
     for out, block in (("same", 0), ("fp8", 0), ("int8", 32)):
         forward(40, cols, "f32", out, block, residual=False, gain=False, x=x)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [8185, 8192, 8193, 8200, 12288, 16384])
+@pytest.mark.parametrize("b,alias", [([3], None), ([1, 0, 70, 5], "dy"), ([40], "dsum")])
+def test_gradients_around_the_widest_one_granule_rows(dynb, dtype, cols, b, alias):
+    backward(b, cols, dtype, dsum=True, gain=True, pads=(1, 2, 0, 3) if alias is None else (0, 0, 0, 0), alias=alias)
