@@ -74,11 +74,23 @@ class ExpertBlock:
     def empty(self, *shape, dtype=None):
         return torch.empty(*shape, device=self.device, dtype=dtype or self.t)
 
-    def gradients(self, h, labels, b):
-        """Every worker's gradient into self.grads[:K]; returns the workers' mean losses (device)."""
-        T, H, K, k, E = h.shape[0], self.width, len(b), self.top_k, self.experts
-        if T > self.max_tokens or K > self.max_workers or sum(b) != T:
+    def _check(self, h, labels, b):
+        """What the library cannot see from addresses: it reads width * T elements of the block's type."""
+        device = torch.device(self.device).type
+        if h.dim() != 2 or h.shape[1] != self.width or h.dtype != self.t or h.device.type != device:
+            raise ValueError("h must be [rows][%d] of %s on %s" % (self.width, self.t, device))
+        T, K = h.shape[0], len(b)
+        if T > self.max_tokens or K > self.max_workers or sum(b) != T or any(n < 0 for n in b):
             raise ValueError("more rows or workers than the block was made for, or batch sizes that are not the rows")
+        if labels.shape != (T,) or labels.is_floating_point() or labels.device != h.device:
+            raise ValueError("labels must be whole numbers, one per row, where the rows are")
+
+    def gradients(self, h, labels, b):
+        """Every worker's gradient into self.grads[:K]; returns the workers' mean losses (device).  h: [sum(b)][width] of
+        the block's type, any strides; labels: [sum(b)] in [0, classes)."""
+        self._check(h, labels, b)
+        h = h.contiguous()
+        T, H, K, k, E = h.shape[0], self.width, len(b), self.top_k, self.experts
         ints = dict(dtype=torch.int32)
         norm = binding.rms_norm_desc(self.dtype, H, eps=EPS)
         route = binding.route_desc(self.dtype, H, T, k, E)
@@ -95,7 +107,11 @@ class ExpertBlock:
         binding.route_segments(route, offsets, source, b, segments)
         z, y, a = self.empty(T * k, H), self.empty(T * k, H), self.empty(T * k, self.hidden)
         binding.route_gather(route, n1, offsets, slot, z)
-        cut = segments.tolist()                       # the products below need the sizes on the host
+        strange = ((labels < 0) | (labels >= self.classes)).sum().to(torch.int32)
+        cut = torch.cat([segments.flatten(), strange[None]]).tolist()   # the products below need the sizes on the host
+        if cut.pop():
+            raise ValueError("a label is not one of the %d classes" % self.classes)
+        cut = [cut[i:i + K + 1] for i in range(0, len(cut), K + 1)]
         w1, w2 = self.weight("w1"), self.weight("w2")
         for e in range(E):
             r = slice(cut[e][0], cut[e][K])
@@ -152,6 +168,8 @@ class ExpertBlock:
 
     def step(self, b, lr):
         """The weighted average of the workers' gradients, applied."""
+        if len(b) > self.max_workers:
+            raise ValueError("more workers than the block was made for")
         self.steps += 1
         self.optimizer.step(self.pointers, b, self.size, lr=lr, beta1=0.9, beta2=0.95, eps=1e-8, step=self.steps,
                             seed=self.steps)

@@ -66,3 +66,27 @@ def test_it_refuses_more_than_it_was_made_for(dynb):
     for b, rows in (([10, 5, 5], 20), ([10, 9], 20), ([10, 11], 21)):
         with pytest.raises(ValueError):
             block.gradients(h.new_zeros(rows, 48), labels, b)
+
+
+def test_it_refuses_labels_that_are_no_classes(dynb):
+    import torch
+    block = expert_block.ExpertBlock(48, 40, 5, 2, 7, 20, 2)
+    h, good = torch.randn(20, 48, device="cuda").to(torch.bfloat16), torch.arange(20, device="cuda") % 7
+    for at, value in ((0, -1), (19, 7)):
+        labels = good.clone()
+        labels[at] = value
+        with pytest.raises(ValueError):
+            block.gradients(h, labels, [10, 10])
+    assert bool(block.gradients(h, good, [10, 10]).isfinite().all())
+
+
+def test_rows_with_a_pitch(dynb):
+    """A slice of wider rows gives what its copy gives."""
+    import torch
+    block = expert_block.ExpertBlock(48, 40, 5, 2, 7, 20, 2)
+    wide, labels = torch.randn(20, 60, device="cuda").to(torch.bfloat16), torch.arange(20, device="cuda") % 7
+    block.gradients(wide[:, 3:51].clone(), labels, [12, 8])
+    want = block.grads.clone()
+    block.gradients(wide[:, 3:51], labels, [12, 8])
+    # the same inputs in the same calls: nothing but the order of sums inside torch's products could differ
+    assert bool(((block.grads - want).abs() <= 1e-2 * want.abs().max()).all())
