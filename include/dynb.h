@@ -367,7 +367,9 @@ int dynb_route_combine_backward(const dynb_route_desc* d, const void* dout, cons
  * (bits(t + 2^-15) - bits(2^-15)) / 2^shift + u, bits() the fp32 encoding as an integer: equal steps in
  * each of 16 octaves below the largest magnitude, exact zero.  m: sign in the highest bit, 8 steps an
  * octave (top 1.875, shift 20); sqrt(v): 16 steps (top 1.9375, shift 19).  scale = a / top (0 for a below
- * 2^-100: stored zeros; NaN where the block has an infinity or NaN: all of it reads as NaN then).  u in [0, 1) makes the
+ * 2^-100: stored zeros; NaN where the block has an infinity or NaN: all of it reads as NaN then).  A positive sqrt(v)
+ * has code 1 at least, a * 2^-19 / top: read as zero beside an m that is not, it would make steps of m / eps, without
+ * bound; like this no element's m / sqrt(v) is beyond about twice what the largest of its block may have.  Else u in [0, 1) makes the
  * rounding unbiased: rounded to nearest, a step of 1/16 would hold v where it is (it changes by 1 - beta2
  * at most when it falls).  u is a function of the element's index i in its tensor, the tensor's position o
  * in the list and `seed`, modulo 2^32: x = i * 0x9E3779B1 + o * 0x7F4A7C15 + seed; x = (x ^ x >> 16) *

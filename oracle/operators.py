@@ -146,6 +146,14 @@ def encode(x, bits, u):
     return codes, np.array(scales)
 
 
+def encode_root(root, u):
+    """sqrt(v) as it is kept: 8 bits, and a positive value has code 1 at least (0 beside an m that is not 0 would make a
+    step of m / eps)."""
+    codes, scales = encode(root, 8, u)
+    lowest = (np.asarray(root) > 0) & (np.repeat(scales, BLOCK)[:len(codes)] > 0)
+    return np.maximum(codes, lowest), scales
+
+
 def decode(codes, scales, bits):
     codes = np.asarray(codes, np.int64)
     table = code_values(bits)

@@ -149,11 +149,11 @@ template <int MAG> __device__ inline float decode(uint32_t q, int e, float scale
 __device__ inline float signed_as(float magnitude, uint32_t q, int e) {       // bit 7 of byte `e`
   return __uint_as_float(__float_as_uint(magnitude) ^ (q << (24 - 8 * e) & 0x80000000u));
 }
-// u16: 16 random bits, 65536ths of a step.  (A factor of 0 gives code 0; of a block with an infinity or NaN it does not
-// matter which code: its scale is NaN.)
-template <int MAG> __device__ inline uint32_t encode(float magnitude, float inv, uint32_t u16) {
+// u16: 16 random bits, 65536ths of a step.  least: the lowest code that the value may get.  (A factor of 0 gives code 0; of
+// a block with an infinity or NaN it does not matter which code: its scale is NaN.)
+template <int MAG> __device__ inline uint32_t encode(float magnitude, float inv, uint32_t u16, uint32_t least) {
   const uint32_t bits = __float_as_uint(__builtin_fmaf(magnitude, inv, 0x1p-15f)) - LOW_BITS + (u16 << (Code<MAG>::SHIFT - 16));
-  return min(bits >> Code<MAG>::SHIFT, (1u << MAG) - 1);
+  return min(max(bits >> Code<MAG>::SHIFT, least), (1u << MAG) - 1);
 }
 __device__ inline uint32_t random_bits(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x6A09E667u;
@@ -263,8 +263,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensor* tensors, const
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t r = random_bits((uint32_t)(at[u] + e) * 0x9E3779B1u + t.ordinal * 0x7F4A7C15u + rule.seed);
-      to1 |= (encode<7>(fabsf(m[u][e]), s1.inv, r >> 16) | (__float_as_uint(m[u][e]) >> 24 & 0x80u)) << (8 * e);
-      to2 |= encode<8>(root[e], s2.inv, r & 0xffffu) << (8 * e);
+      to1 |= (encode<7>(fabsf(m[u][e]), s1.inv, r >> 16, 0) | (__float_as_uint(m[u][e]) >> 24 & 0x80u)) << (8 * e);
+      // (a root below half a step that became 0 beside an m that did not would make a step of m / eps)
+      to2 |= encode<8>(root[e], s2.inv, r & 0xffffu, root[e] > 0.f ? 1 : 0) << (8 * e);
     }
     store_codes(codes1 + at[u], n[u], to1);
     store_codes(codes2 + at[u], n[u], to2);

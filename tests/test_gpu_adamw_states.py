@@ -1,0 +1,62 @@
+"""AdamW's states where the values of a block differ by many octaves: the lowest code of sqrt(v), and many steps."""
+import numpy as np
+import pytest
+
+from oracle import operators as oo
+from paper_2305_12213_amd import binding
+from tests.operators_harness import host
+
+pytestmark = pytest.mark.gpu
+
+
+def optimizer(n, state, param=None):
+    """(handle, tensors) of one tensor with zero states."""
+    import torch
+    new = lambda size, **kw: torch.zeros(size, device="cuda", **kw)  # noqa: E731
+    kind = dict(dtype=torch.uint8) if state == "8bit" else {}
+    blocks = -(-n // 256)
+    t = dict(n=n, param=new(n) if param is None else param, state1=new(n, **kind), state2=new(n, **kind), scale1=new(blocks),
+             scale2=new(blocks), weight_decay=0.0)
+    h = binding.AdamW([t], state=state)
+    size = h.workspace_bytes()
+    h.bind(torch.zeros(size, device="cuda", dtype=torch.uint8), size)
+    return h, t
+
+
+def test_a_positive_root_has_a_code_and_zero_has_none(dynb):
+    import torch
+    n = 1000
+    rng = np.random.default_rng(8)
+    g = rng.choice([-1.0, 1.0], n) * 10.0 ** rng.uniform(-9, 0, n)
+    g[::7] = 0
+    g = torch.from_numpy(g.astype(np.float32)).cuda()
+    for seed in range(5):
+        h, t = optimizer(n, "8bit")
+        h.step([g], [1], 0, lr=1e-3, beta1=0.9, beta2=0.98, eps=1e-8, step=1, seed=seed)
+        root = np.sqrt(0.02) * np.abs(host(g))
+        codes = t["state2"].cpu().numpy().astype(int)
+        assert np.array_equal(codes > 0, root > 0)
+        want, _ = oo.encode_root(root, (oo.random_bits(n, 0, seed) & 65535) / 65536)
+        # a value within fp32's error of a threshold may fall on its other side: one step, fewer than one in a thousand
+        assert np.abs(codes - want).max() <= 1 and (codes != want).sum() <= 1
+
+
+@pytest.mark.parametrize("ratio", [1e6, 1e9])
+@pytest.mark.parametrize("beta2", [0.95, 0.999])
+def test_no_step_without_bound(dynb, ratio, beta2):
+    """The largest step over many, in units of the learning rate: at most 10 (2.07 times (1 - beta1) / sqrt(1 - beta2) =
+    6.6, and a code's step on both sides), with fp32 states at most 4."""
+    import torch
+    n, steps = 256, 300
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    runs = [(*optimizer(n, state), most) for state, most in (("8bit", 10), ("f32", 4))]
+    worst = [torch.zeros((), device="cuda") for _ in runs]
+    for step in range(1, steps + 1):
+        g = torch.randn(n, generator=gen, device="cuda")
+        g[0] *= ratio
+        for i, (h, t, _) in enumerate(runs):
+            before = t["param"].clone()
+            h.step([g], [1], 0, lr=1.0, beta1=0.9, beta2=beta2, eps=1e-8, step=step, seed=step)
+            worst[i] = torch.maximum(worst[i], (t["param"] - before).abs().max())
+    for (_, _, most), w in zip(runs, worst):
+        assert float(w) <= most
