@@ -360,6 +360,8 @@ int dynb_route_combine_backward(const dynb_route_desc* d, const void* dout, cons
 /* AdamW over a list of tensors in one call: Adam with weight decay taken from the parameter itself,
  *   g = sum_k (b_k / sum_i b_i) g_k;  m = beta1 m + (1-beta1) g;  v = beta2 v + (1-beta2) g^2;
  *   p -= lr * (weight_decay * p + (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)).
+ * v is fp32 in the step (subnormal values included): gradients below about 2^-75 / sqrt(1-beta2) leave none, and sqrt(v)
+ * counts as 2^-75 at least in the division, so that eps = 0 divides by no zero.  In 8 bits an m whose v is 0 is kept as 0.
  *
  * States in 8 bits (DYNB_STATE_8BIT) are uint8 [n] with one fp32 scale per 256 elements (the last block
  * may be shorter): state1 holds m, state2 holds sqrt(v), whose range is half as many octaves as v's.  With

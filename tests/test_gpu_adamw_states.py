@@ -60,3 +60,50 @@ def test_no_step_without_bound(dynb, ratio, beta2):
             worst[i] = torch.maximum(worst[i], (t["param"] - before).abs().max())
     for (_, _, most), w in zip(runs, worst):
         assert float(w) <= most
+
+
+TINY = [1e-17, 3e-19, 1e-19, 1e-20, 1e-21]
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-8])
+@pytest.mark.parametrize("state", ["f32", "8bit"])
+def test_gradients_whose_squares_are_subnormal(dynb, state, eps):
+    """The first step is lr times the gradient's sign, however small the gradient: v = (1 - beta2) g^2 is off by 2^-149 (two
+    roundings to a multiple of it) and 4 * 2^-24 of itself: by d in all, the step by 1 / sqrt(1 - d) and 8 * 2^-24."""
+    import torch
+    n = 1000
+    rng = np.random.default_rng(12)
+    g = rng.choice([-1.0, 1.0], n) * rng.uniform(0.5, 2.0, n) * np.repeat(TINY, n // 5)
+    gd = torch.from_numpy(g.astype(np.float32)).cuda()
+    h, t = optimizer(n, state)
+    h.step([gd], [1], 0, lr=1.0, beta1=0.9, beta2=0.98, eps=eps, step=1, seed=3)
+    g = host(gd)
+    want, m, v = oo.adamw(np.zeros(n), np.zeros(n), np.zeros(n), g[None], [1], 0.0, 1.0, 0.9, 0.98, eps, 1)
+    off = (1 - 2.0 ** -149 / v - 4 * 2.0 ** -24) ** -0.5 - 1 + 8 * 2.0 ** -24
+    assert (np.abs(host(t["param"]) - want) <= 1.01 * off * np.abs(want)).all()
+    if state == "f32":
+        assert (np.abs(host(t["state1"]) - m) <= 4 * 2.0 ** -24 * np.abs(m)).all()
+        assert (np.abs(host(t["state2"]) - v) <= 2.0 ** -149 + 4 * 2.0 ** -24 * v).all()
+    else:
+        assert (t["state2"] > 0).all() and (host(t["scale2"]) > 0).all()
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-30])
+@pytest.mark.parametrize("state,most", [("f32", 10), ("8bit", 20)])
+def test_no_division_by_a_vanished_root(dynb, state, most, eps):
+    """Gradients around and below the least whose square fp32 holds, others far above them, some zero: steps of at most
+    1 / sqrt(1 - beta2) = 7.1 (8-bit states: 2.07 times that), and a code's step or a quantum of v on top."""
+    import torch
+    n = 1024
+    rng = np.random.default_rng(13)
+    h, t = optimizer(n, state)
+    sizes = 10.0 ** rng.uniform(-27, -17, n)
+    sizes[256:512] = 10.0 ** rng.uniform(-45, -21, 256)
+    sizes[512:768:5] = 0.0
+    sizes[768:1024:7] = 1e-3
+    for step in range(1, 61):
+        g = rng.standard_normal(n) * sizes * (rng.random(n) < 0.7)
+        before = host(t["param"])
+        h.step([torch.from_numpy(g.astype(np.float32)).cuda()], [1], 0, lr=1.0, beta1=0.9, beta2=0.98, eps=eps, step=step, seed=step)
+        assert np.abs(host(t["param"]) - before).max() <= most, step
+    assert not host(t["param"])[512:768:5].any()
