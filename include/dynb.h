@@ -279,6 +279,8 @@ typedef struct {
  *   q = 448 or 127, scale = a / q and y is stored as round(y / scale) (nearest-even).  A block whose
  *   a is below 2^-100 has scale 0 and stored zeros; one with an infinity or NaN has scale NaN, so that all
  *   of it stands for NaN.
+ * Squares that overflow fp32, or vanish in it beside an eps below 2^-100, are taken of the scaled row: any row with a root mean
+ * square of at least 2^-126 is normed (rstd has to be an fp32 number).  eps = 0: a row of zeros has rstd infinity and y NaN.
  * sum and a y of dtype may be x's or residual's memory (same pointer, same ld).  rows >= 0.
  * DYNB_ERR_BADARG: null pointers, unknown type, cols, scale_block, eps (negative or not finite), an ld
  * below cols, a pointer that is not a multiple of its element's size, rows beyond 2^31 - 1. */

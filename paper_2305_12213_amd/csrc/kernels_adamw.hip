@@ -167,7 +167,7 @@ __device__ inline uint32_t random_bits(uint32_t x) {
 // gradient's square is below fp32's range): its root counts as LEAST_ROOT in the division, and such an m is 1 / sqrt(1 - beta2)
 // times that at most; its 8-bit code is 0 as well.  (117 M parameters, a bf16 gradient: 8-bit states 317 us,
 // fp32 states 554, without any of this 317 and 554.)
-constexpr uint32_t LEAST_ROOT = 52u << 23;          // bits of 2^-75, half of the smallest v's root
+constexpr uint32_t LEAST_ROOT = 52u << 23;          // bits of 2^-75 (the smallest v has 2^-74.5)
 constexpr int SUBNORMAL = 0x80;                     // of the class test: positive ones
 
 // A wave takes U blocks; all it reads is asked for before anything is used.

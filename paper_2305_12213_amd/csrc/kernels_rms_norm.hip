@@ -80,12 +80,14 @@ __device__ inline void store_eight(uint8_t* p, int n, const float (&f)[GRANULE],
 
 // 1 / sqrt(mean + eps) from the sum of squares, by the hardware's root (one unit in the last place).  Where the sum has
 // overflowed, from the squares of the row times 2^-80, which `scaled_sum` gives (eps is nothing beside them; a row with an
-// infinity or NaN ends the same either way); where it is too small for the hardware's root, by the library's.
+// infinity or NaN ends the same either way); where squares may have been lost below fp32's range (eps is below 2^-100 then), of
+// the row times 2^80, with eps times 2^160: rows down to a root mean square of 2^-126.
 template <typename F> __device__ inline float rstd_of(float ss, float inv_cols, float eps, F scaled_sum) {
   const float m = __builtin_fmaf(ss, inv_cols, eps);
-  if (m >= 0x1p-126f && m <= 3e38f) return __builtin_amdgcn_rsqf(m);
-  if (m < 1.f) return 1.f / sqrtf(m);
-  return 0x1p-80f / sqrtf(scaled_sum() * inv_cols);
+  // (said to be likely, or the other two paths cost the narrow kernels 2 %)
+  if (__builtin_expect(m >= 0x1p-100f && m <= 3e38f, 1)) return __builtin_amdgcn_rsqf(m);
+  if (m < 1.f) return 0x1p80f / sqrtf(__builtin_fmaf(scaled_sum(0x1p80f), inv_cols, eps * 0x1p80f * 0x1p80f));
+  return 0x1p-80f / sqrtf(scaled_sum(0x1p-80f) * inv_cols);
 }
 
 // Rows beyond WIDEST granules, and blocks that no group of lanes holds: a workgroup per row goes over it two or three times,
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_any_kernel(NormArgs 
       return ss;
     };
     const float ss = block_sum(sum_of_squares(1.f), waves, red[turn]);
-    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() { return block_sum(sum_of_squares(0x1p-80f), waves, red[2]); });
+    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&](float by) { return block_sum(sum_of_squares(by), waves, red[2]); });
     if (t == 0 && p.rstd) p.rstd[r] = rstd;
     auto results = [&](int c, float (&s)[GRANULE]) {
       if (!p.gain) {
@@ -261,12 +263,12 @@ __global__ __launch_bounds__(L == WIDE ? 64 * MOST_WAVES : 256) void rms_norm_ke
       for (int e = 0; e < GRANULE; ++e) ss += s[i][e] * s[i][e];
     }
     ss = row_sum<L>(ss, waves, red[turn]);
-    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&]() {
+    const float rstd = rstd_of(ss, p.inv_cols, p.eps, [&](float by) {
       float a = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < GRANULE; ++e) a += (s[i][e] * 0x1p-80f) * (s[i][e] * 0x1p-80f);
+        for (int e = 0; e < GRANULE; ++e) a += (s[i][e] * by) * (s[i][e] * by);
       return row_sum<L>(a, waves, red[2]);
     });
     if (t == 0 && p.rstd) p.rstd[r] = rstd;
