@@ -28,6 +28,13 @@ constexpr int one_granule(int out) { return out == DYNB_OUT_SAME ? 8 : 12; }
 // with two launches 189).
 constexpr int widest_grad(size_t element) { return element == 2 ? WIDEST : WIDEST / 2; }
 
+// A workgroup per row, also of more rows than a grid has workgroups in one direction.
+dim3 grid_of_rows(int64_t rows) {
+  constexpr int64_t MOST = 1 << 20;
+  return dim3((unsigned)std::min(rows, MOST), (unsigned)((rows + MOST - 1) / MOST));
+}
+__device__ inline int64_t row_of_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Lanes of a row: 8, 16, 32 or 64, or whole waves.
 constexpr int WIDE = 128;
 template <int L> __device__ inline int row_in_block() {
@@ -104,7 +111,7 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_any_kernel(NormArgs 
   int turn = 0, round = 0;
   for (int i = t; i < 3 * MOST_SLOTS; i += threads) (&tops[0][0])[i] = 0;
   __syncthreads();
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
+  for (int64_t r = row_of_block(); r < p.rows; r += (int64_t)gridDim.x * gridDim.y, turn ^= 1) {
     const T* const x = (const T*)p.x + r * p.ld_x;
     const T* const res = p.residual ? (const T*)p.residual + r * p.ld_residual : nullptr;
     auto values = [&](int c, float (&s)[GRANULE]) {
@@ -350,8 +357,6 @@ __global__ __launch_bounds__(256) void dequantise_kernel(NormArgs p, int out, T*
   }
 }
 
-int grid_of_rows(int64_t rows) { return (int)(rows < (1 << 20) ? rows : 1 << 20); }
-
 // Checks a description and fills what the kernels take of it.
 int describe(const dynb_rms_norm_desc* d, const char* who, NormArgs& a) {
   if (!d) return fail(DYNB_ERR_BADARG, "%s: null pointer", who);
@@ -398,8 +403,11 @@ template <typename T, int OUT> void launch_norm_out(const NormArgs& a, hipStream
   const int waves = (granules + 63) / 64, threads = 64 * (waves < MOST_WAVES ? waves : MOST_WAVES);
   const int group = whole || lanes > threads ? 0 : lanes > 64 || (lanes & (lanes - 1)) ? -1 : lanes;
   if (granules > WIDEST || group < 0 || (group == 0 && !whole)) {
-    const dim3 block(threads);
-    hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), dim3(grid_of_rows(a.rows)), block, 0, st, a, group);
+    // A workgroup per row, or, 8-bit outputs, for as many rows as there are more than the chip holds (16384 x 18432 bf16 461 us,
+    // several rows each 504; to fp8 in blocks of 96 columns 574 and 524, 200000 x 200 170 and 150, 16384 x 4096 in blocks of
+    // 1024 152 and 131, whole rows of 16384 x 18432 561 and 567).
+    const dim3 grid = OUT == DYNB_OUT_SAME ? grid_of_rows(a.rows) : dim3(resident(a.rows, threads));
+    hipLaunchKernelGGL((rms_norm_any_kernel<T, OUT>), grid, dim3(threads), 0, st, a, group);
     return;
   }
   if (granules <= 8) launch_norm_as<T, OUT, 8, 1>(a, 4, group, st);
@@ -548,44 +556,43 @@ __global__ __launch_bounds__(L == WIDE ? 64 * MOST_WAVES : 256) void rms_norm_gr
 // a thread per column and worker and single elements 1950.)
 template <typename T>
 __global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_grad_any_kernel(NormGradArgs p) {
-  __shared__ float red[2][MOST_WAVES];
+  __shared__ float red[MOST_WAVES];
   const int threads = blockDim.x;
-  int turn = 0;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
-    const T *const s = (const T*)p.sum + r * p.ld_sum, *const dy = (const T*)p.dy + r * p.ld_dy;
-    const float rstd = p.rstd[r];
-    auto values = [&](int c, float (&a)[GRANULE], float (&gd)[GRANULE]) {        // shat, gain dy
-      const int n = p.cols - c;
-      const Raw<T> s0 = load_raw(s + c, n), d0 = load_raw(dy + c, n);
-      float g[GRANULE];
-      if (p.gain) load_part(p.gain + c, n, g);
-      unpack(s0, n, a);
-      unpack(d0, n, gd);
+  const int64_t r = row_of_block();
+  if (r >= p.rows) return;
+  const T *const s = (const T*)p.sum + r * p.ld_sum, *const dy = (const T*)p.dy + r * p.ld_dy;
+  const float rstd = p.rstd[r];
+  auto values = [&](int c, float (&a)[GRANULE], float (&gd)[GRANULE]) {        // shat, gain dy
+    const int n = p.cols - c;
+    const Raw<T> s0 = load_raw(s + c, n), d0 = load_raw(dy + c, n);
+    float g[GRANULE];
+    if (p.gain) load_part(p.gain + c, n, g);
+    unpack(s0, n, a);
+    unpack(d0, n, gd);
 #pragma unroll
-      for (int e = 0; e < GRANULE; ++e) {
-        a[e] *= rstd;
-        if (p.gain) gd[e] *= g[e];
-      }
-    };
-    float c1 = 0.f;
-    for (int c = threadIdx.x * GRANULE; c < p.cols; c += threads * GRANULE) {
-      float a[GRANULE], gd[GRANULE];
-      values(c, a, gd);
-#pragma unroll
-      for (int e = 0; e < GRANULE; ++e) c1 += gd[e] * a[e];
+    for (int e = 0; e < GRANULE; ++e) {
+      a[e] *= rstd;
+      if (p.gain) gd[e] *= g[e];
     }
-    c1 = block_sum(c1, threads >> 6, red[turn]) * p.inv_cols;
-    for (int c = threadIdx.x * GRANULE; c < p.cols; c += threads * GRANULE) {
-      float a[GRANULE], gd[GRANULE], d[GRANULE];
-      if (p.dsum) load_part((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c, d);
-      values(c, a, gd);
+  };
+  float c1 = 0.f;
+  for (int c = threadIdx.x * GRANULE; c < p.cols; c += threads * GRANULE) {
+    float a[GRANULE], gd[GRANULE];
+    values(c, a, gd);
 #pragma unroll
-      for (int e = 0; e < GRANULE; ++e) a[e] = rstd * (gd[e] - a[e] * c1);
-      if (p.dsum)
+    for (int e = 0; e < GRANULE; ++e) c1 += gd[e] * a[e];
+  }
+  c1 = block_sum(c1, threads >> 6, red) * p.inv_cols;
+  for (int c = threadIdx.x * GRANULE; c < p.cols; c += threads * GRANULE) {
+    float a[GRANULE], gd[GRANULE], d[GRANULE];
+    if (p.dsum) load_part((const T*)p.dsum + r * p.ld_dsum + c, p.cols - c, d);
+    values(c, a, gd);
 #pragma unroll
-        for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
-      store_part((T*)p.dx + r * p.ld_dx + c, p.cols - c, a);
-    }
+    for (int e = 0; e < GRANULE; ++e) a[e] = rstd * (gd[e] - a[e] * c1);
+    if (p.dsum)
+#pragma unroll
+      for (int e = 0; e < GRANULE; ++e) a[e] += d[e];
+    store_part((T*)p.dx + r * p.ld_dx + c, p.cols - c, a);
   }
 }
 
@@ -691,7 +698,7 @@ void launch_norm_grad(const NormGradArgs& a, const Segs& seg, float* partial, hi
   if (n > 0 && granules > widest_grad(sizeof(T))) {
     if (a.dgain)   // (first: dx may lie on dy)
       hipLaunchKernelGGL(rms_norm_gain_grad_kernel<T>, dim3((granules + 255) / 256, n), dim3(256), 0, st, a, seg, ch, partial);
-    hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, dim3(grid_of_rows(a.rows)), dim3(64 * MOST_WAVES), 0, st, a);
+    hipLaunchKernelGGL(rms_norm_grad_any_kernel<T>, grid_of_rows(a.rows), dim3(64 * MOST_WAVES), 0, st, a);
   } else if (n > 0) {
     const int waves = (granules + 63) / 64;
     if (granules <= 8) launch_norm_grad_as<T, 8, 1>(a, seg, ch, 4, partial, st);
