@@ -284,12 +284,12 @@ template <typename T, int L, bool PAST> __global__ __launch_bounds__(256) void c
 
 // L lanes take a choice: its row of dsorted, and the product of the two rows.  For calls that the caches hold, where more and
 // shorter chains count (the gradient is read again for each choice): 1024 tokens of 4 choices of 2048 bf16 columns and the
-// combination of the rows' gradient behind it 13.8 us, by tokens 16.2.
+// combination of the rows' gradient behind it 13.8 us, by tokens 16.2.  Such calls have fewer than 2^20 * 256 / L choices.
 template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_kernel(RowArgs p) {
-  __shared__ float red[2][MOST_WAVES];
+  __shared__ float red[MOST_WAVES];
   const int kept = constant(p.offsets, p.n_experts);
-  int turn = 0;
-  for (int64_t i = row_of_thread<L>(); i < p.choices; i += (int64_t)gridDim.x * (256 / L)) {
+  const int64_t i = row_of_thread<L>();
+  if (i < p.choices) {
     const int64_t t = i / p.top_k, s = constant(p.slot, i);
     const float w = constant(p.weights, i);
     float dot = 0.f;
@@ -305,8 +305,7 @@ template <typename T, int L> __global__ __launch_bounds__(256) void choice_grad_
         }
         store_part((T*)p.out + s * p.ld_out + c, p.cols - c, g);
       }
-      dot = L > 64 ? block_sum(dot, L / 64, red[turn]) : lanes_sum<(L < 64 ? L : 64)>(dot);
-      turn ^= 1;
+      dot = L > 64 ? block_sum(dot, L / 64, red) : lanes_sum<(L < 64 ? L : 64)>(dot);
     }
     if (threadIdx.x % L == 0) p.dweights[i] = dot;
   }
@@ -414,14 +413,14 @@ int lanes_of(int granules, int64_t rows) {
 ROUTE_LAUNCHES(gather)
 ROUTE_LAUNCHES(combine)
 ROUTE_LAUNCHES(combine_grad)
+template <typename T, int L> void launch_choice_grad_as(const RowArgs& a, hipStream_t st) {   // (every choice has its lanes)
+  hipLaunchKernelGGL((choice_grad_kernel<T, L>), dim3((unsigned)((a.choices + 256 / L - 1) / (256 / L))), dim3(256), 0, st, a);
+}
 template <typename T> void launch_choice_grad(const RowArgs& a, hipStream_t st) {
-  const dim3 block(256);
-  if (a.granules <= 16) hipLaunchKernelGGL((choice_grad_kernel<T, 16>), dim3(grid_of(a.choices, 16)), block, 0, st, a);
-  else if (a.granules <= 32) hipLaunchKernelGGL((choice_grad_kernel<T, 32>), dim3(grid_of(a.choices, 32)), block, 0, st, a);
-  else if (a.granules <= 128 || a.choices >= 1024)
-    hipLaunchKernelGGL((choice_grad_kernel<T, 64>), dim3(grid_of(a.choices, 64)), block, 0, st, a);
-  else
-    hipLaunchKernelGGL((choice_grad_kernel<T, 256>), dim3(grid_of(a.choices, 256)), block, 0, st, a);
+  if (a.granules <= 16) launch_choice_grad_as<T, 16>(a, st);
+  else if (a.granules <= 32) launch_choice_grad_as<T, 32>(a, st);
+  else if (a.granules <= 128 || a.choices >= 1024) launch_choice_grad_as<T, 64>(a, st);
+  else launch_choice_grad_as<T, 256>(a, st);
 }
 
 int describe(const dynb_route_desc* d, const char* who) {
