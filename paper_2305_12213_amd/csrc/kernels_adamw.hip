@@ -2,8 +2,9 @@
 // and the 16-bit copy of the parameters, in one pass over all of them.
 //   g = sum_k lambda_k g_k, m += (1 - beta1) (g - m), v += (1 - beta2) (g^2 - v),
 //   p -= lr (decay p + (m / c1) / (sqrt(v / c2) + eps)),  all in fp32.
-// Memory bounds it: 54.5 M parameters of 16 workers in fp32 with a 16-bit copy 4.9 GB, 860 us (5.7 TB/s); 235 M parameters, one
-// bf16 gradient, 8-bit states 3.76 GB, 628 us (6.0 TB/s), their values read back 226 us (6.2 TB/s).  A wave takes 256
+// Memory bounds it: 54.5 M parameters of 16 workers in fp32 with a 16-bit copy 4.9 GB, 869 us (5.6 TB/s); 235 M parameters, one
+// bf16 gradient, 8-bit states 3.76 GB, 638 us (5.9 TB/s), their values read back 232 us (6.0 TB/s); 117 M bf16 parameters, a bf16
+// gradient, fp32 states 2.58 GB, 428 us (6.0 TB/s).  A wave takes 256
 // neighbouring elements, a scale's block, so that the largest magnitude is an exchange inside it; a table on the device
 // says which tensor a workgroup works on, so that one launch does all of up to 256 tensors.
 #include <hip/hip_runtime.h>
@@ -54,7 +55,7 @@ struct Rule {
 
 // ---- 4 neighbouring elements, of which the first n exist ------------------------------------------------------
 // Every byte is used once a step: accesses pass the caches by (54.5 M parameters of 16 workers, two
-// blocks to a wave: 890 us, 935 through them).
+// blocks to a wave: 890 us, 935 through them; nothing behind the step read the copy).
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
 typedef uint32_t u32_half __attribute__((aligned(2), may_alias));
 #define GLOBAL __attribute__((address_space(1)))

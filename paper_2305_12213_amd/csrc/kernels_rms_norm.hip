@@ -24,8 +24,8 @@ constexpr int WIDEST = 2 * 64 * MOST_WAVES;   // granules of the widest rows tha
 // 50.0 us with one, 61.8 with two, 856 x 6437 22.2 and 19.6.
 constexpr int one_granule(int out) { return out == DYNB_OUT_SAME ? 8 : 12; }
 // Gradients take one granule as far as the waves go (4096 x 8192 bf16: 58.2 us, with two 60.4), then bf16 rows two; fp32 rows do
-// not fit in the registers then, and take the two launches of wider ones (4096 x 16384 355 us, with two granules 367; bf16 107 and
-// with two launches 189).
+// not fit in the registers then, and take the two launches of wider ones (4096 x 16384 353 us, with two granules, which spill, 367;
+// bf16 107 and with two launches 189).
 constexpr int widest_grad(size_t element) { return element == 2 ? WIDEST : WIDEST / 2; }
 
 // A workgroup per row, also of more rows than a grid has workgroups in one direction.
@@ -100,7 +100,8 @@ template <typename F> __device__ inline float rstd_of(float ss, float inv_cols, 
 // Rows beyond WIDEST granules, and blocks that no group of lanes holds: a workgroup per row goes over it two or three times,
 // the later ones in the caches.  group: lanes that share a scale, -1 where it is no power of two up to 64 (then by LDS), 0
 // where all threads take a block at a time.  (4096 x 18432 bf16 with a residual 130 us, 4.6 TB/s, element by element 278; one row
-// of 20480 6.7 us.  To fp8 and back 4096 x 4096: blocks of 96 columns 59 us, a wave per block 121; of 1024 55 and 57.)
+// of 20480 6.5 us.  To fp8 4096 x 4096 with a residual: blocks of 96 columns 41 us, of 1024 37; and back 59, a wave per block 121,
+// and 55, 57.)
 constexpr int MOST_SLOTS = 64 * MOST_WAVES / 12;   // blocks of 96 columns, the narrowest that are no power of two
 template <typename T, int OUT>
 __global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_any_kernel(NormArgs p, int group) {
@@ -552,7 +553,7 @@ __global__ __launch_bounds__(L == WIDE ? 64 * MOST_WAVES : 256) void rms_norm_gr
 }
 
 // Gradients of rows beyond widest_grad() granules, in two launches: the rows' by a workgroup per row that goes over it twice, the
-// gain's over a chunk's rows by a thread per granule, UNDER rows at a time.  (4096 x 18432 bf16 with dsum 210 us, moving 906 MB;
+// gain's over a chunk's rows by a thread per granule, UNDER rows at a time.  (4096 x 18432 bf16 with dsum 196 us, moving 906 MB;
 // a thread per column and worker and single elements 1950.)
 template <typename T>
 __global__ __launch_bounds__(64 * MOST_WAVES) void rms_norm_grad_any_kernel(NormGradArgs p) {

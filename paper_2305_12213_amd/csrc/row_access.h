@@ -22,7 +22,9 @@ typedef uint16_t u16_any __attribute__((aligned(1), may_alias));
 // Calls of more bytes than the caches keep until the next one reads them pass them by.  Sorting and combination of 2048
 // columns in bf16, 8 choices: 1024 tokens (38 and 42 MB) 30.2 us either way, 2048 tokens 46 us past the caches and 55 through
 // them, 16384 tokens 245 and 279; gradients of 4 choices: 1024 tokens (38 and 21 MB) 15.8 and 13.8, 2048 27.0 and 30.2; the norm
-// of 16384 x 8192 to fp8 165 and 185.
+// of 16384 x 8192 to fp8 165 and 185.  With a product behind the call that reads what it wrote: norm of 4096 x 2048 with residual
+// (67 MB) 51.4 us past the caches and 48.4 through them, 4096 x 4096 57 and 56, 16384 x 4096 (536 MB) 159 and 172; 4096 tokens of
+// 2048 columns and 4 choices sorted (83 MB) 56 and 50, 16384 of 8 (603 MB) 275 and 299.
 inline bool past_caches(double bytes) { return bytes > 64e6; }
 
 // PAST: the access passes the caches by (data that is used once and is more than they hold).
