@@ -427,6 +427,111 @@ int dynb_adamw_step(dynb_adamw* h, const void* const* grads, const int32_t* b, i
 int dynb_adamw_read_states(dynb_adamw* h, void* const* out1, void* const* out2, int32_t out_dtype,
                            void* stream);
 
+/* ---- products around routed experts: dense layers, gated feed-forward blocks, embeddings ---------------------
+ * Rows, weights and pitches as in the operators above: dtype is the type of all rows and weights, products and sums are
+ * fp32 and each stored value is rounded once (nearest-even); what a backward pass keeps between two of its products (the
+ * gradients of pre-activations, and `hidden`) is stored in dtype.  Weights are dense, in C order, at any multiple of their
+ * element's size.  Gradients of weights and biases are per worker, fp32 or (grad_dtype) of the rows' type.
+ * Results are the same from run to run.  Calls may be captured into a graph; a workspace is used by one call at a time.
+ * Values past the rows, or between them, are neither read nor written. */
+enum { DYNB_ACT_NONE = 0, DYNB_ACT_RELU = 1, DYNB_ACT_SILU = 2, DYNB_ACT_GELU = 3 };
+/*   RELU max(v, 0);  SILU v / (1 + e^-v);  GELU v (1 + erf(v / sqrt 2)) / 2;  a NaN stays one */
+
+/* A dense layer with what surrounds it.  n_in, n_out: 1 .. 2^20. */
+typedef struct {
+  int32_t dtype;
+  int32_t grad_dtype; /* of dweight and dbias: DYNB_F32, or dtype */
+  int32_t activation; /* DYNB_ACT_* */
+  int32_t n_in, n_out;
+  int64_t ld_x, ld_residual, ld_pre, ld_out; /* forward; ld_x and ld_pre also in the backward pass */
+  int64_t ld_dout, ld_dx;                    /* backward */
+} dynb_linear_desc;
+
+/* out = act(z) + residual, z = x W + bias.
+ *   weight: [n_in][n_out];  bias: fp32 [n_out], or NULL;  residual: rows, or NULL;
+ *   pre: receives z (what the backward pass of an activation needs), or NULL.  rows >= 0.
+ * out may be residual's memory (same pointer, same ld); nothing else may overlap what is written.
+ * workspace: device, 16-byte aligned, dynb_linear_workspace_bytes(d, rows) bytes (0 on bad arguments; may be 0, and
+ * workspace NULL). */
+size_t dynb_linear_workspace_bytes(const dynb_linear_desc* d, int64_t rows);
+int dynb_linear(const dynb_linear_desc* d, int64_t rows, const void* x, const void* weight, const float* bias,
+                const void* residual, void* pre, void* out, void* workspace, size_t workspace_bytes,
+                void* stream);
+
+/* Its gradients, with dz = dout act'(z) (the residual's gradient is dout itself):
+ *   dx = dz W^T (or NULL);  dweight[k] = x^T dz and dbias[k] = the sum of dz over worker k's rows, zeros for an idle one;
+ *   worker k's at dweight + k * dweight_stride (>= n_in * n_out elements of grad_dtype) and dbias + k * dbias_stride
+ *   (>= n_out); either may be NULL.  pre: as dynb_linear stored it (may be NULL without an activation).
+ * b: host [K], rows = sum(b).  Nothing written may overlap what is read.  workspace as above. */
+size_t dynb_linear_backward_workspace_bytes(const dynb_linear_desc* d, const int32_t* b, int32_t K);
+int dynb_linear_backward(const dynb_linear_desc* d, const int32_t* b, int32_t K, const void* x, const void* weight,
+                         const void* pre, const void* dout, void* dx, void* dweight, int64_t dweight_stride,
+                         void* dbias, int64_t dbias_stride, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/* The gated feed-forward of routed experts, over rows sorted by expert (dynb_route_plan, dynb_route_gather).
+ * cols, hidden: 1 .. 2^20;  n_experts: 1 .. DYNB_MAX_EXPERTS;  rows: of every row tensor, offsets[n_experts] of them
+ * or fewer are in use.  ld_kept: rows of the pre-activations (0: hidden). */
+typedef struct {
+  int32_t dtype;
+  int32_t grad_dtype; /* of the weights' gradients: DYNB_F32, or dtype */
+  int32_t activation; /* DYNB_ACT_* */
+  int32_t cols, hidden;
+  int32_t n_experts;
+  int64_t rows;
+  int64_t ld_x, ld_y, ld_dy, ld_dx, ld_kept;
+} dynb_gated_block_desc;
+
+/* For expert e's rows [offsets[e], offsets[e + 1]):
+ *   gate = x Wg[e], up = x Wu[e], hidden = act(gate) * up (from the sums before they are rounded), y = hidden Wd[e].
+ *   offsets: device int32 [n_experts + 1], ascending from 0, or NULL for one expert that has all rows;
+ *   w_gate, w_up: [n_experts][cols][hidden];  w_down: [n_experts][hidden][cols];
+ *   gate, up: receive the pre-activations (for the backward pass), or both NULL.
+ * Rows behind the last expert's are neither read nor written (whatever stands in offsets, nothing outside `rows` is).
+ * y may be x's memory (same pointer, same ld).  workspace: device, 16-byte aligned,
+ * dynb_gated_block_workspace_bytes(d) bytes (0 on a bad description). */
+size_t dynb_gated_block_workspace_bytes(const dynb_gated_block_desc* d);
+int dynb_gated_block(const dynb_gated_block_desc* d, const int32_t* offsets, const void* x, const void* w_gate,
+                     const void* w_up, const void* w_down, void* gate, void* up, void* y, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Its gradients from the kept pre-activations, with dhidden = dy Wd^T, dgate = dhidden * up * act'(gate),
+ * dup = dhidden * act(gate):
+ *   dx = dgate Wg^T + dup Wu^T (or NULL; may be dy's memory only if the weights' gradients are NULL);
+ *   dw_gate[k][e] = x^T dgate, dw_up[k][e] = x^T dup, dw_down[k][e] = hidden^T dy over the rows of expert e from worker k,
+ *   zeros where there are none; worker k's at + k * worker_stride elements of grad_dtype (>= n_experts * cols * hidden),
+ *   laid out as the weights; or all three NULL.
+ *   segments: device int32 [n_experts][K + 1] (dynb_route_segments), or NULL for K = 1: the offsets.
+ * workspace as above, dynb_gated_block_backward_workspace_bytes(d, K) bytes. */
+size_t dynb_gated_block_backward_workspace_bytes(const dynb_gated_block_desc* d, int32_t K);
+int dynb_gated_block_backward(const dynb_gated_block_desc* d, int32_t K, const int32_t* offsets,
+                              const int32_t* segments, const void* x, const void* w_gate, const void* w_up,
+                              const void* w_down, const void* gate, const void* up, const void* dy, void* dx,
+                              void* dw_gate, void* dw_up, void* dw_down, int64_t worker_stride, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Rows of a table by token.  vocabulary: 1 .. 2^24;  cols: 1 .. 2^20;  tokens: 0 .. 2^31 - 1;  scale: finite. */
+typedef struct {
+  int32_t dtype; /* of the table, the rows and their gradient */
+  int32_t cols;
+  int64_t vocabulary, tokens;
+  float scale;
+  int64_t ld_table, ld_out, ld_dout;
+} dynb_embedding_desc;
+
+/* out[t] = scale * table[ids[t]]; ids: device int32 [tokens], one outside [0, vocabulary) gives a row of zeros (and reads
+ * nothing). */
+int dynb_embedding(const dynb_embedding_desc* d, const int32_t* ids, const void* table, void* out, void* stream);
+
+/* Its gradient, every worker's: dtable[k][v] = scale * the sum of dout[t] over worker k's tokens with ids[t] = v, in a fixed
+ * order, fp32 [vocabulary][cols] at dtable + k * worker_stride (>= vocabulary * cols).  All of it is written: zeros for tokens
+ * that do not appear.  b: host [K], sum(b) = tokens.  The tokens are sorted by (worker, id) first, in
+ * workspace: device, 16-byte aligned, dynb_embedding_backward_workspace_bytes(d, K) bytes (0 on bad arguments). */
+size_t dynb_embedding_backward_workspace_bytes(const dynb_embedding_desc* d, int32_t K);
+int dynb_embedding_backward(const dynb_embedding_desc* d, const int32_t* b, int32_t K, const int32_t* ids,
+                            const void* dout, float* dtable, int64_t worker_stride, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* ---- controller (host only) ---------------------------------------------------- */
 
 /* One controller invocation (four-step summary of "Control stability"): from the

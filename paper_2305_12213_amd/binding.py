@@ -35,7 +35,10 @@ SYMBOLS = [
     "dynb_rms_norm_backward", "dynb_route_workspace_bytes", "dynb_route_plan", "dynb_route_segments",
     "dynb_route_gather", "dynb_route_combine", "dynb_route_combine_backward", "dynb_adamw_create",
     "dynb_adamw_destroy", "dynb_adamw_workspace_bytes", "dynb_adamw_bind", "dynb_adamw_step",
-    "dynb_adamw_read_states",
+    "dynb_adamw_read_states", "dynb_linear_workspace_bytes", "dynb_linear",
+    "dynb_linear_backward_workspace_bytes", "dynb_linear_backward", "dynb_gated_block_workspace_bytes",
+    "dynb_gated_block", "dynb_gated_block_backward_workspace_bytes", "dynb_gated_block_backward",
+    "dynb_embedding", "dynb_embedding_backward_workspace_bytes", "dynb_embedding_backward",
 ]
 
 
@@ -115,6 +118,29 @@ class AdamWRule(C.Structure):
                 ("step", C.c_int64), ("seed", C.c_uint32)]
 
 
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("activation", C.c_int32),
+                ("n_in", C.c_int32), ("n_out", C.c_int32), ("ld_x", C.c_int64),
+                ("ld_residual", C.c_int64), ("ld_pre", C.c_int64), ("ld_out", C.c_int64),
+                ("ld_dout", C.c_int64), ("ld_dx", C.c_int64)]
+
+
+class GatedBlockDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("activation", C.c_int32),
+                ("cols", C.c_int32), ("hidden", C.c_int32), ("n_experts", C.c_int32),
+                ("rows", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_dy", C.c_int64),
+                ("ld_dx", C.c_int64), ("ld_kept", C.c_int64)]
+
+
+class EmbeddingDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("cols", C.c_int32), ("vocabulary", C.c_int64),
+                ("tokens", C.c_int64), ("scale", C.c_float), ("ld_table", C.c_int64),
+                ("ld_out", C.c_int64), ("ld_dout", C.c_int64)]
+
+
 _lib = None
 
 
@@ -189,6 +215,17 @@ def load():
         "dynb_adamw_bind": (C.c_int, [vp, vp, C.c_size_t, vp]),
         "dynb_adamw_step": (C.c_int, [vp, C.POINTER(vp), pi32, i32, i64, C.POINTER(AdamWRule), vp]),
         "dynb_adamw_read_states": (C.c_int, [vp, C.POINTER(vp), C.POINTER(vp), i32, vp]),
+        "dynb_linear_workspace_bytes": (C.c_size_t, [vp, i64]),
+        "dynb_linear": (C.c_int, [vp, i64] + [vp] * 7 + [C.c_size_t, vp]),
+        "dynb_linear_backward_workspace_bytes": (C.c_size_t, [vp, pi32, i32]),
+        "dynb_linear_backward": (C.c_int, [vp, pi32, i32] + [vp] * 6 + [i64, vp, i64, vp, C.c_size_t, vp]),
+        "dynb_gated_block_workspace_bytes": (C.c_size_t, [vp]),
+        "dynb_gated_block": (C.c_int, [vp] * 10 + [C.c_size_t, vp]),
+        "dynb_gated_block_backward_workspace_bytes": (C.c_size_t, [vp, i32]),
+        "dynb_gated_block_backward": (C.c_int, [vp, i32] + [vp] * 13 + [i64, vp, C.c_size_t, vp]),
+        "dynb_embedding": (C.c_int, [vp] * 5),
+        "dynb_embedding_backward_workspace_bytes": (C.c_size_t, [vp, i32]),
+        "dynb_embedding_backward": (C.c_int, [vp, pi32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -511,6 +548,83 @@ class AdamW:
         if getattr(self, "_h", None) and _lib is not None:
             _lib.dynb_adamw_destroy(self._h)
             self._h = None
+
+
+# ---- products around routed experts: dense layers, gated blocks, embeddings
+
+_ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU}
+
+
+def linear_desc(dtype, n_in, n_out, activation="none", grad="f32", ld_x=0, ld_residual=0, ld_pre=0, ld_out=0,
+                ld_dout=0, ld_dx=0):
+    return LinearDesc(_DTYPES[dtype], _DTYPES[grad], _ACTS[activation], int(n_in), int(n_out), int(ld_x),
+                      int(ld_residual), int(ld_pre), int(ld_out), int(ld_dout), int(ld_dx))
+
+
+def linear_workspace_bytes(desc, rows):
+    return int(load().dynb_linear_workspace_bytes(C.addressof(desc), rows))
+
+
+def linear(desc, rows, x, weight, bias, residual, pre, out, workspace, workspace_bytes, stream=None):
+    _check(load().dynb_linear(C.addressof(desc), rows, _ptr(x), _ptr(weight), _ptr(bias), _ptr(residual),
+                              _ptr(pre), _ptr(out), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def linear_backward_workspace_bytes(desc, b):
+    return int(load().dynb_linear_backward_workspace_bytes(C.addressof(desc), _i32(b), len(b)))
+
+
+def linear_backward(desc, b, x, weight, pre, dout, dx, dweight, dweight_stride, dbias, dbias_stride, workspace,
+                    workspace_bytes, stream=None):
+    _check(load().dynb_linear_backward(C.addressof(desc), _i32(b), len(b), _ptr(x), _ptr(weight), _ptr(pre),
+                                       _ptr(dout), _ptr(dx), _ptr(dweight), dweight_stride, _ptr(dbias),
+                                       dbias_stride, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def gated_block_desc(dtype, cols, hidden, n_experts, rows, activation="silu", grad="f32", ld_x=0, ld_y=0, ld_dy=0,
+                     ld_dx=0, ld_kept=0):
+    return GatedBlockDesc(_DTYPES[dtype], _DTYPES[grad], _ACTS[activation], int(cols), int(hidden),
+                          int(n_experts), int(rows), int(ld_x), int(ld_y), int(ld_dy), int(ld_dx), int(ld_kept))
+
+
+def gated_block_workspace_bytes(desc):
+    return int(load().dynb_gated_block_workspace_bytes(C.addressof(desc)))
+
+
+def gated_block(desc, offsets, x, w_gate, w_up, w_down, gate, up, y, workspace, workspace_bytes, stream=None):
+    _check(load().dynb_gated_block(C.addressof(desc), _ptr(offsets), _ptr(x), _ptr(w_gate), _ptr(w_up),
+                                   _ptr(w_down), _ptr(gate), _ptr(up), _ptr(y), _ptr(workspace), workspace_bytes,
+                                   _stream(stream)))
+
+
+def gated_block_backward_workspace_bytes(desc, K):
+    return int(load().dynb_gated_block_backward_workspace_bytes(C.addressof(desc), K))
+
+
+def gated_block_backward(desc, K, offsets, segments, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up,
+                         dw_down, worker_stride, workspace, workspace_bytes, stream=None):
+    _check(load().dynb_gated_block_backward(
+        C.addressof(desc), K, _ptr(offsets), _ptr(segments), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+        _ptr(gate), _ptr(up), _ptr(dy), _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), worker_stride,
+        _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def embedding_desc(dtype, cols, vocabulary, tokens, scale=1.0, ld_table=0, ld_out=0, ld_dout=0):
+    return EmbeddingDesc(_DTYPES[dtype], int(cols), int(vocabulary), int(tokens), float(scale), int(ld_table),
+                         int(ld_out), int(ld_dout))
+
+
+def embedding(desc, ids, table, out, stream=None):
+    _check(load().dynb_embedding(C.addressof(desc), _ptr(ids), _ptr(table), _ptr(out), _stream(stream)))
+
+
+def embedding_backward_workspace_bytes(desc, K):
+    return int(load().dynb_embedding_backward_workspace_bytes(C.addressof(desc), K))
+
+
+def embedding_backward(desc, b, ids, dout, dtable, worker_stride, workspace, workspace_bytes, stream=None):
+    _check(load().dynb_embedding_backward(C.addressof(desc), _i32(b), len(b), _ptr(ids), _ptr(dout), _ptr(dtable),
+                                          worker_stride, _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def make_gains(kp=1.0, deadband=0.05, ewma_alpha=1.0, b_min=1, b_max=1 << 30, **_ignored):

@@ -64,6 +64,8 @@ enum KClass {
   KC_GEMM_64,            // bf16 forward / input-gradient products on the 64 x 64-tile kernel
   KC_GEMM_128X64,        // ... on 128 x 64 tiles
   KC_ROUTE,              // tokens sorted by expert and back
+  KC_DENSE,              // dense layers and gated blocks with their epilogues, and their gradients
+  KC_EMBEDDING,          // rows of a table by token, and the table's gradient
   KC_COUNT
 };
 

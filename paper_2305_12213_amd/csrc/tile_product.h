@@ -1,0 +1,501 @@
+// Matrix products over groups of rows, with what follows a product computed on its results while they are in registers:
+//   ROWS_NN   out[i] = sum_k x[i][k] W[e][k][j]          rows i of group e (an expert's rows, or all of a dense layer)
+//   ROWS_NT   out[i] = sum_k x[i][k] W[e][j][k]          ... against the weight turned: gradients of the rows
+//   WEIGHTS   out[g][i][j] = sum_r x[r][i] y[r][j]       over the rows r of group g: gradients of the weights
+// Where a group begins and ends stands in device memory, so nothing waits for the host: a workgroup finds its group by
+// itself, the grid is the largest that the sizes allow, and workgroups past the last tile end at once.
+//
+// A stage is 128 bytes of reduction per row (64 bf16, 32 fp32), in LDS as memory has it.  An operand whose rows run
+// along the reduction is read in granules of 16 bytes; of one whose rows run across it ("turned") bf16 is fetched by the LDS
+// transpose reads, fp32 element by element.  One step is two granules: a 32 x 32 x 16 matrix instruction in bf16, four of
+// 32 x 32 x 2 in fp32, whose k are numbered so that both operands' lanes hold the same ones.
+//
+// DIRECT: copies go from memory straight to LDS, a ring of NB stages, a step's fragments are fetched one step ahead, and
+// fetches and copies stand between the matrix instructions (as in the dense layers' products).  Otherwise (rows that are
+// no multiple of 16 bytes) they pass through registers, which can fill up partial granules with zeros.
+#ifndef DYNB_TILE_PRODUCT_H
+#define DYNB_TILE_PRODUCT_H
+
+#include <hip/hip_runtime.h>
+
+#include "device_rows.h"
+#include "dynb_internal.h"
+#include "lds_async.h"
+#include "row_access.h"
+
+namespace dynb {
+
+enum Form { ROWS_NN, ROWS_NT, WEIGHTS };
+
+struct Product {
+  const void* A[2];
+  const void* B[2];          // of two products that share A (dual), or of two whose sum is wanted (pairs = 2)
+  int64_t lda, ldb;          // elements
+  int64_t b_stride;          // elements from one group's B to the next (ROWS_*)
+  int M, N;                  // WEIGHTS: output rows; output columns of one product
+  int K;                     // ROWS_*: reduction length of one pair
+  int pairs;
+  int64_t rows;              // rows there are (ROWS_*: of A; WEIGHTS: of both)
+  const int32_t* offsets;    // ROWS_*: device [groups + 1], or null: one group of all rows.  WEIGHTS: see `segments`
+  const int32_t* segments;   // WEIGHTS: device [groups / workers][workers + 1]; null: `offsets`, or the launch's Segs
+  int groups, workers;
+  int splits;                // parts that the reduction is divided into; > 1: sums of the parts go to `partial`
+  float* partial;            // fp32 [splits][partial_rows][columns of all products]
+  int64_t partial_rows;
+};
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+constexpr uint32_t PARKED = 0x80000000u;   // an offset past the end of a buffer: the copy writes zeros
+
+// Workgroup -> place in the tile sequence: consecutive workgroups go round the 8 XCDs, each of which gets a run of it.
+__device__ inline int64_t run_of_xcd(int64_t pid, int64_t total) {
+  if (total < 16) return pid;
+  const int64_t per = total / 8, extra = total % 8, xcd = pid % 8;
+  return xcd * per + (xcd < extra ? xcd : extra) + pid / 8;
+}
+// Place -> tile, in bands of 8 tile rows, so that a run covers a compact rectangle.
+__device__ inline void tile_of_place(int64_t t, int tiles_i, int tiles_j, int& ti, int& tj) {
+  const int64_t bsz = (int64_t)8 * tiles_j;
+  const int b0 = (int)(t / bsz), r = (int)(t % bsz);
+  const int rows = tiles_i - b0 * 8 < 8 ? tiles_i - b0 * 8 : 8;
+  ti = b0 * 8 + r % rows;
+  tj = r / rows;
+}
+
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Rows [first, last) of a group, whatever stands in memory kept inside [0, rows).
+__device__ inline void group_rows(const int32_t* bounds, int64_t rows, int64_t& first, int64_t& last) {
+  const int64_t a = bounds[0], b = bounds[1];
+  first = a < 0 ? 0 : a > rows ? rows : a;
+  last = b < first ? first : b > rows ? rows : b;
+}
+// Sum over the wave's lanes up to this one.
+__device__ inline int sum_upto(int v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(v, d);
+    v += (int)(threadIdx.x & 63) >= d ? o : 0;
+  }
+  return v;
+}
+// Tiles of BM rows over all groups; and the group that has tile `ti` of them, its rows from that tile on.
+__device__ inline int row_tiles(const Product& p, int BM) {
+  if (!p.offsets) return (int)((p.rows + BM - 1) / BM);
+  int total = 0;
+  for (int e0 = 0; e0 < p.groups; e0 += 64) {
+    const int e = e0 + (threadIdx.x & 63);
+    int64_t first = 0, last = 0;
+    if (e < p.groups) group_rows(p.offsets + e, p.rows, first, last);
+    total += __builtin_amdgcn_readlane(sum_upto((int)((last - first + BM - 1) / BM)), 63);
+  }
+  return total;
+}
+__device__ inline void find_group(const Product& p, int BM, int ti, int& group, int64_t& first, int64_t& last) {
+  group = 0;
+  first = (int64_t)ti * BM;
+  last = p.rows;
+  if (!p.offsets) return;
+  int before = 0;
+  for (int e0 = 0; e0 < p.groups; e0 += 64) {
+    const int e = e0 + (threadIdx.x & 63);
+    int64_t f = 0, l = 0;
+    if (e < p.groups) group_rows(p.offsets + e, p.rows, f, l);
+    const int mine = (int)((l - f + BM - 1) / BM), upto = before + sum_upto(mine);
+    const uint64_t has = __ballot(ti >= upto - mine && ti < upto);
+    if (has) {
+      const int lane = __builtin_ctzll(has);
+      group = e0 + lane;
+      first = __builtin_amdgcn_readlane((int)f, lane) + (int64_t)(ti - __builtin_amdgcn_readlane(upto - mine, lane)) * BM;
+      last = __builtin_amdgcn_readlane((int)l, lane);
+      return;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  last = first = 0;       // (not reached: ti is below the number of tiles)
+}
+
+// The first n of a granule's elements, zeros behind them (n <= 0: none is read).
+template <typename T> __device__ inline u32x4 load_granule(const T* p, int n) {
+  constexpr int G = 16 / sizeof(T);
+  u32x4 r = {0, 0, 0, 0};
+  if (n >= G) {
+    r = load16(p);
+  } else if (n > 0) {
+#pragma unroll
+    for (int e = 0; e < G; ++e) {
+      if (e >= n) continue;
+      if (sizeof(T) == 4) r[e] = ((const uint32_t*)p)[e];
+      else r[e / 2] |= (uint32_t)((const uint16_t*)p)[e] << (16 * (e & 1));
+    }
+  }
+  return r;
+}
+
+// Slot of granule g in reduction row k of a turned tile with rows of `pitch` bytes: the rows that one read touches
+// at once fall into different banks (bf16: four neighbouring ones, 64 bytes of each; fp32: rows 4 apart, 128 bytes of each).
+template <typename T> __device__ constexpr int turned_swizzle(int k, int pitch) {
+  return sizeof(T) == 4 ? ((k >> 2) & 1) << 3 : pitch >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+}
+
+// LDS written by some lanes of a wave and read by others.
+__device__ inline void patch_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A tile of BM x BN results, WM x WN waves.  DUAL: two products with BN / 2 columns each, which share A; a wave has the same
+// columns of both.  Ep: what is done with 8 neighbouring results of a row.  SOON: of a stage's copies, eighths that are
+// issued in the last step of the stage that releases its buffer, and in the first step of the next.
+template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, bool DIRECT, class Ep>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs segs, Ep ep) {
+  constexpr bool TA = FORM == WEIGHTS, TB = FORM != ROWS_NT;
+  constexpr int G = 16 / sizeof(T), BK = 8 * G, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = DIRECT ? NB : 2;
+  constexpr int CA = BM / 8 / NW, CB = BN / 8 / NW, NC = CA + CB;   // copies of 1 KB per wave and stage
+  constexpr uint32_t STAGE = (BM + BN) * 128;
+  constexpr int CW = 32 * TN, EP = CW + 4;                          // a wave's columns, row pitch of its patch
+  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole copies");
+  static_assert(!DUAL || TN % 2 == 0, "a wave has columns of both products");
+  constexpr uint32_t AREA = NBUF * STAGE > NW * 32 * EP * 4 ? NBUF * STAGE : NW * 32 * EP * 4;   // (the patches come last)
+  static_assert(!TA || BM * (int)sizeof(T) >= 256, "a turned A has the wide swizzle");
+  __shared__ uint4 ring[AREA / 16];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int wm = wave % WM, wn = wave / WM, l31 = lane & 31, h = lane >> 5;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0];
+
+  // ---- which tile
+  int group, tj, depth;
+  int64_t i0, i_end, r0 = 0;              // output rows; WEIGHTS: first reduction row
+  const int tiles_j = (p.N + BNS - 1) / BNS;
+  if constexpr (FORM == WEIGHTS) {
+    const int tiles_i = (p.M + BM - 1) / BM;
+    const int64_t tiles = (int64_t)tiles_i * tiles_j;
+    const int64_t t = run_of_xcd(blockIdx.x, tiles * p.groups);
+    int ti;
+    group = (int)(t / tiles);
+    tile_of_place(t % tiles, tiles_i, tiles_j, ti, tj);
+    i0 = (int64_t)ti * BM;
+    i_end = p.M;
+    int64_t last;
+    if (p.segments) group_rows(p.segments + (int64_t)(group / p.workers) * (p.workers + 1) + group % p.workers, p.rows, r0, last);
+    else if (p.offsets) group_rows(p.offsets + group, p.rows, r0, last);
+    else r0 = segs.off[group], last = segs.off[group + 1];
+    r0 = uniform((int)r0);
+    depth = uniform((int)(last - r0));
+  } else {
+    const int tiles_i = uniform(row_tiles(p, BM));
+    const int64_t total = (int64_t)tiles_i * tiles_j;
+    if (blockIdx.x >= total) return;
+    int ti;
+    tile_of_place(run_of_xcd(blockIdx.x, total), tiles_i, tiles_j, ti, tj);
+    find_group(p, BM, ti, group, i0, i_end);
+    group = uniform(group);
+    i0 = uniform((int)i0);
+    i_end = uniform((int)i_end);
+    depth = p.K;
+  }
+  const int j0 = tj * BNS;
+
+  // ---- the stages of this workgroup
+  const int per_pair = (depth + BK - 1) / BK, all = FORM == WEIGHTS ? per_pair : per_pair * p.pairs;
+  const int part = (all + p.splits - 1) / p.splits;
+  const int s_begin = p.splits > 1 ? min((int)blockIdx.y * part, all) : 0;
+  const int s_end = p.splits > 1 ? min(s_begin + part, all) : all;
+  const int64_t stepA = TA ? (int64_t)BK * p.lda * sizeof(T) : 128, stepB = TB ? (int64_t)BK * p.ldb * sizeof(T) : 128;
+  // first byte of the tile in the operands of pair q
+  auto base_a = [&](int q) {
+    return (uint64_t)(uintptr_t)p.A[q] + (TA ? r0 * p.lda + i0 : i0 * p.lda) * sizeof(T);
+  };
+  auto base_b = [&](int q) {
+    return (uint64_t)(uintptr_t)p.B[q] +
+           (FORM == WEIGHTS ? r0 * p.ldb + j0 : group * p.b_stride + (TB ? (int64_t)j0 : j0 * p.ldb)) * sizeof(T);
+  };
+  int next = s_begin;                     // the stage that is copied next, where it stands, and what is left of the reduction
+  uint64_t from[3];                       // A, B, the other product's B
+  int left;
+  auto enter = [&](int q, int s) {        // stage s of pair q
+    from[0] = base_a(q) + s * stepA;
+    from[1] = base_b(q) + s * stepB;
+    if (DUAL) from[2] = base_b(1) + s * stepB;
+    left = depth - s * BK;
+  };
+  if (FORM != WEIGHTS && !DUAL && next >= per_pair && p.pairs == 2) enter(1, next - per_pair);
+  else enter(0, next);
+  if (next >= s_end) left = 0;
+  auto next_stage = [&]() {
+    ++next;
+    from[0] += stepA;
+    from[1] += stepB;
+    if (DUAL) from[2] += stepB;
+    left -= BK;
+    if (FORM != WEIGHTS && !DUAL && next == per_pair && p.pairs == 2) enter(1, 0);
+    if (next >= s_end) left = 0;          // (copies past the last stage keep the waits constant: zeros)
+  };
+
+  // ---- copies: block c of a tile is 64 granules, lane l's lands in slot 64 c + l
+  int64_t off[NC];                        // bytes from the stage's first (DIRECT: below 2^31, or PARKED)
+  int need[NC];                           // a granule is there where more than this is left of the reduction
+  int have[NC];                           // ... and so many of its elements (turned operands; the others: G or 0)
+#pragma unroll
+  for (int u = 0; u < NC; ++u) {
+    const bool isA = u < CA;
+    const int c = isA ? CA * wave + u : (CB * wave + u - CA) % (BNS / 8);      // (dual: block within its product's half)
+    const bool turned = isA ? TA : TB;
+    const int64_t ld = isA ? p.lda : p.ldb, limit = isA ? i_end - i0 : p.N - j0;
+    if (turned) {
+      const int row = isA ? BM / G : BNS / G, s = 64 * c + lane, k = s / row;
+      const int g = (s % row) ^ turned_swizzle<T>(k, row * 16);
+      off[u] = k * ld * (int64_t)sizeof(T) + g * 16;
+      need[u] = k;
+      have[u] = (int)max((int64_t)0, min((int64_t)G, limit - g * G));
+    } else {
+      const int r = 8 * c + (lane >> 3), g = (lane & 7) ^ swizzle128(r);
+      off[u] = r * ld * (int64_t)sizeof(T) + g * 16;
+      need[u] = g * G;
+      have[u] = r < limit ? G : 0;
+    }
+    if (DIRECT && have[u] == 0) need[u] = 0x7fffffff;
+  }
+  auto source = [&](int u) { return u < CA ? 0 : DUAL && (CB * wave + u - CA) >= BNS / 8 ? 2 : 1; };
+  auto slot_of = [&](int u) { return u < CA ? (CA * wave + u) * 1024u : BM * 128u + (CB * wave + u - CA) * 1024u; };
+  auto copy_one = [&](uint32_t buf, int u) {
+    const uint64_t a = from[source(u)];
+    const i32x4 r = {(int)(uint32_t)a, (int)((uint32_t)(a >> 32) & 0xffffu), (int)PARKED, BUFFER_32BIT};
+    async_copy_1k_buffer(r, need[u] < left ? (uint32_t)off[u] : PARKED, lds + buf + slot_of(u));
+  };
+
+  // ---- fragments: element (row or column l31, k of half h) of two granules
+  const char* const base = (const char*)&ring[0];
+  constexpr int PA = BM * sizeof(T), PB = BNS * sizeof(T);          // pitches of turned tiles
+  // turned bf16: 16 lanes fetch 4 reduction rows x 16 features with a transpose read (lane r supplies the address of
+  // features 4 (r % 4) .. of row r / 4 and receives feature r of the 4 rows)
+  const int tg = lane >> 4, tr = lane & 15;
+  auto turned_at = [&](int feat0, int pitch) {
+    if (sizeof(T) == 4) {
+      const int f = feat0 + l31;
+      return 4 * h * pitch + (((f >> 2) ^ (h << 3)) * 16) + (f & 3) * 4;
+    }
+    const int f = feat0 + 16 * (tg & 1) + 4 * (tr & 3), k = 8 * (tg >> 1) + (tr >> 2);
+    return k * pitch + (((f >> 3) ^ turned_swizzle<T>(k, pitch)) * 16) + (f & 7) * 2;
+  };
+  int at[4], atA[TA ? TM : 1], atB[TB ? TN : 1];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) at[kk] = l31 * 128 + (((2 * kk + h) ^ swizzle128(l31)) * 16);
+  if constexpr (TA) {
+#pragma unroll
+    for (int a = 0; a < TM; ++a) atA[a] = turned_at(wm * (BM / WM) + a * 32, PA);
+  }
+  auto sub_column = [&](int b) { return DUAL ? wn * (CW / 2) + b % (TN / 2 ? TN / 2 : 1) * 32 : wn * CW + b * 32; };
+  if constexpr (TB) {
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+      atB[b] = BM * 128 + (DUAL && b >= TN / 2 ? BNS * 128 : 0) + turned_at(sub_column(b), PB);
+  }
+  auto turned_fragment = [&](uint32_t where, int kk, int pitch) {
+    if constexpr (sizeof(T) == 4) {
+      f32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = *(const float*)(base + where + (kk * 8 + j) * pitch);
+      return __builtin_bit_cast(u32x4, v);
+    } else {
+      const s16x4 lo = lds_read_tr(lds + where + kk * 16 * pitch), hi = lds_read_tr(lds + where + (kk * 16 + 4) * pitch);
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      return __builtin_bit_cast(u32x4, v);
+    }
+  };
+  u32x4 fa[2][TM], fb[2][TN];             // [register set: the step's parity]
+  auto fetch_one = [&](uint32_t buf, int kk, int f) {
+    if (f < TM) {
+      if constexpr (TA) fa[kk & 1][f] = turned_fragment(buf + atA[f], kk, PA);
+      else fa[kk & 1][f] = *(const u32x4*)(base + buf + (wm * (BM / WM) + f * 32) * 128 + at[kk]);
+    } else {
+      const int b = f - TM;
+      if constexpr (TB) fb[kk & 1][b] = turned_fragment(buf + atB[b], kk, PB);
+      else fb[kk & 1][b] = *(const u32x4*)(base + buf + (BM + wn * CW + b * 32) * 128 + at[kk]);
+    }
+  };
+  static_assert(TB || !DUAL, "two products at a time: B turned");
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
+  // (B's columns as the instruction's rows: a lane then has 4 neighbouring columns of the output)
+  auto mma_one = [&](int set, int m) {
+    const int a = m % TM, b = m / TM;
+    if constexpr (sizeof(T) == 4) {
+      const f32x4 x = __builtin_bit_cast(f32x4, fa[set][a]), w = __builtin_bit_cast(f32x4, fb[set][b]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j], x[j], acc[a][b], 0, 0, 0);
+    } else {
+      acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[set][b]),
+                                                          __builtin_bit_cast(bf16x8, fa[set][a]), acc[a][b], 0, 0, 0);
+    }
+  };
+  constexpr int NM = TM * TN, NF = TM + TN;
+
+  if constexpr (DIRECT) {
+    // copies behind step 3 of the stage before, 0, 1, 2: up to Q[1], Q[2], ...
+    constexpr int Q[5] = {0, SOON * NC / 8, 2 * SOON * NC / 8, SOON * NC / 4 + (NC - SOON * NC / 4) / 2, NC};
+#pragma unroll 1
+    for (int s = 0; s < NB - 1; ++s) {
+#pragma unroll
+      for (int u = 0; u < NC; ++u) copy_one(s * STAGE, u);
+      next_stage();
+    }
+#pragma unroll
+    for (int u = 0; u < Q[1]; ++u) copy_one((NB - 1) * STAGE, u);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NC + Q[1]) : "memory");
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < NF; ++f) fetch_one(0, 0, f);
+    uint32_t slot = 0, fill = (NB - 1) * STAGE;
+#pragma unroll 1
+    for (int s = s_begin; s < s_end; ++s) {
+      const uint32_t after = slot + STAGE == NB * STAGE ? 0 : slot + STAGE;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        if (kk == 3) {
+          // this wave's copies of the next stage have landed (behind them, NB - 2 stages) and its reads of this one have
+          // returned, and so for every wave
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NC) : "memory");
+          __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0), the other counters at their limits
+          __syncthreads();
+          next_stage();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+          mma_one(kk & 1, m);
+          __builtin_amdgcn_sched_barrier(0);
+          const int first = Q[(kk + 1) & 3], items = NF + Q[((kk + 1) & 3) + 1] - first;
+#pragma unroll
+          for (int it = m * items / NM; it < (m + 1) * items / NM; ++it) {
+            if (it < NF) fetch_one(kk < 3 ? slot : after, (kk + 1) & 3, it);
+            else copy_one(kk < 3 ? fill : slot, first + it - NF);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      fill = slot;
+      slot = after;
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);      // (fetches past the last stage)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (no copy may land in the patches, or after the LDS has been given back)
+    __syncthreads();
+  } else {
+    u32x4 held[NC];
+    auto load_stage = [&]() {
+#pragma unroll
+      for (int u = 0; u < NC; ++u) {
+        const bool turned = u < CA ? TA : TB;
+        const int n = have[u] == 0 || need[u] >= left ? 0 : turned ? have[u] : min(G, left - need[u]);
+        held[u] = load_granule((const T*)(uintptr_t)(from[source(u)] + off[u]), n);
+      }
+    };
+    auto store_stage = [&](uint32_t buf) {
+#pragma unroll
+      for (int u = 0; u < NC; ++u) *(u32x4*)((char*)&ring[0] + buf + slot_of(u) + lane * 16) = held[u];
+    };
+    load_stage();
+    store_stage(0);
+    __syncthreads();
+    uint32_t slot = 0;
+#pragma unroll 1
+    for (int s = s_begin; s < s_end; ++s) {
+      next_stage();
+      load_stage();
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+        for (int f = 0; f < NF; ++f) fetch_one(slot, kk, f);
+#pragma unroll
+        for (int m = 0; m < NM; ++m) mma_one(kk & 1, m);
+      }
+      // (the other buffer: every wave has read it before the last barrier)
+      store_stage(STAGE - slot);
+      slot = STAGE - slot;
+      __syncthreads();
+    }
+  }
+
+  // ---- results: 32 rows at a time through a private patch, so that a lane has 8 neighbouring columns of a row
+  constexpr int LPR = BNS / WN / 8, RPI = 64 / LPR;
+  float* const patch = (float*)&ring[0] + wave * 32 * EP;
+  const int rrow = lane / LPR, rcol = (lane % LPR) * 8, hi4 = 4 * h;
+  const int col = j0 + wn * (BNS / WN) + rcol, n = min(p.N - col, 8);
+  const int wide = DUAL ? 2 * p.N : p.N;
+#pragma unroll
+  for (int a = 0; a < TM; ++a) {
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 o = {acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+        *(f32x4*)&patch[l31 * EP + b * 32 + 8 * q + hi4] = o;
+      }
+    patch_fence();
+#pragma unroll Ep::ROWS_AT_ONCE
+    for (int t = 0; t < 32 / RPI; ++t) {
+      const int r = rrow + RPI * t;
+      const int64_t i = i0 + wm * (BM / WM) + a * 32 + r;
+      float v[8], w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = patch[r * EP + rcol + e];
+        w[e] = DUAL ? patch[r * EP + CW / 2 + rcol + e] : 0.f;
+      }
+      if (i >= i_end || n <= 0) continue;
+      if (p.splits > 1) {
+        float* const to = p.partial + ((int64_t)blockIdx.y * p.partial_rows + (FORM == WEIGHTS ? (int64_t)group * p.M : 0) + i) * wide + col;
+        store_part(to, n, v);
+        if (DUAL) store_part(to + p.N, n, w);
+      } else {
+        ep.row(group, i, col, n, v, w);
+      }
+    }
+    patch_fence();
+  }
+}
+
+// The parts of a divided reduction, in order, and what follows the product.
+template <int FORM, bool DUAL, class Ep>
+__global__ __launch_bounds__(256) void joined_kernel(Product p, Ep ep) {
+  const int chunks = (p.N + 7) / 8, wide = DUAL ? 2 * p.N : p.N;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / chunks;
+  int64_t first = 0, rows = p.partial_rows;
+  if (FORM != WEIGHTS && p.offsets) {     // rows outside the groups have no parts
+    const int64_t end = p.offsets[p.groups];
+    rows = end < rows ? end : rows;
+    first = p.offsets[0];
+  }
+  if (row < first || row >= rows) return;
+  const int col = (int)(at % chunks) * 8, n = min(p.N - col, 8);
+  float v[8] = {}, w[8] = {}, x[8];
+  for (int s = 0; s < p.splits; ++s) {
+    const float* const from = p.partial + (s * p.partial_rows + row) * wide + col;
+    load_part(from, n, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
+    if (DUAL) {
+      load_part(from + p.N, n, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] += x[e];
+    }
+  }
+  if (FORM == WEIGHTS) ep.row((int)(row / p.M), row % p.M, col, n, v, w);
+  else ep.row(0, row, col, n, v, w);
+}
+
+}  // namespace
+}  // namespace dynb
+
+#endif
