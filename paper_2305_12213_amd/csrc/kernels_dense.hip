@@ -15,24 +15,34 @@ int64_t tiles_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
 int64_t row_tiles_of(int64_t rows, int groups, int size) {
   return groups == 1 ? tiles_of(rows, size) : rows / size + (std::min<int64_t>(groups, rows) + 1) / 2;
 }
-int parts(int64_t tiles, int64_t wanted, int64_t stages, int64_t least) {
-  const int64_t n = std::min({tiles_of(wanted, std::max<int64_t>(tiles, 1)), stages / least, (int64_t)16});
-  return tiles * 3 > wanted * 2 ? 1 : (int)std::max<int64_t>(n, 1);
+// Into how many parts a reduction of `stages` is divided: workgroups run `slots` at a time, each for its share of the stages;
+// a part more is worth it where that time falls by `worth` stages at least (what writing and joining it takes).
+int parts(int64_t tiles, int64_t slots, int64_t stages, int64_t worth) {
+  int best = 1;
+  int64_t least = tiles_of(tiles, slots) * stages;
+  for (int n = 2; n <= 16; ++n) {
+    const int64_t cost = tiles_of(tiles * n, slots) * tiles_of(stages, n) + worth * n;
+    if (cost < least) {
+      least = cost;
+      best = n;
+    }
+  }
+  return best;
 }
 
 ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduction, bool dual) {
   const int half = dual ? 2 : 1;
   const int64_t stages = tiles_of(reduction, dtype == DYNB_F32 ? 32 : 64);
   const int64_t each = rows / std::min<int64_t>(groups, std::max<int64_t>(rows, 1));
-  if (each <= 48) return {TILES_32, parts(row_tiles_of(rows, groups, 32) * tiles_of(N, 128 / half), 512, stages, 4)};
+  if (each <= 48) return {TILES_32, parts(row_tiles_of(rows, groups, 32) * tiles_of(N, 128 / half), 512, stages, 2)};
   if (dtype == DYNB_BF16 && each >= 160 && row_tiles_of(rows, groups, 256) * tiles_of(N, 256 / half) >= 192) return {TILES_256, 1};
-  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), 256, stages, 8)};
+  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), 256, stages, dtype == DYNB_F32 ? 1 : 4)};
 }
 ProductPlan plan_weights(int dtype, int64_t rows, int groups, int M, int N, bool dual) {
   const int half = dual ? 2 : 1;
   const int64_t stages = tiles_of(rows / groups, dtype == DYNB_F32 ? 32 : 64);
   if (dtype == DYNB_BF16 && tiles_of(M, 256) * tiles_of(N, 256 / half) * groups >= 192) return {TILES_256, 1};
-  return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128 / half) * groups, 256, stages, 8)};
+  return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128 / half) * groups, 256, stages, dtype == DYNB_F32 ? 2 : 6)};
 }
 // Bytes of Product::partial (0 where the plan has one part).
 size_t partial_bytes(const ProductPlan& plan, int64_t rows, int64_t columns) {
@@ -62,6 +72,7 @@ int check_workspace(const void* workspace, size_t bytes, size_t need, const char
 // ---- gradient of what an activation was taken of, and sums of its columns ------------------------------------------
 // dpre = dout act'(pre), and over the rows of each chunk its sums (fp32, the rows in order: four waves take every
 // fourth row each, their sums are added in turn).  Memory bounds it.
+constexpr int TOGETHER = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void dense_grad_kernel(const T* dout, int64_t ld_dout, const T* pre, int64_t ld_pre, int act,
                                                          T* dpre, int64_t ld_dpre, float* sums, int cols, Segs segs,
@@ -74,18 +85,33 @@ __global__ __launch_bounds__(256) void dense_grad_kernel(const T* dout, int64_t 
   const int64_t first = segs.off[k] + (int64_t)((int)blockIdx.x - ch.first[k]) * ch.rows;
   const int64_t last = min((int64_t)segs.off[k + 1], first + ch.rows);
   float s[8] = {};
-  for (int64_t r = first + wave; r < last; r += 4) {
-    float v[8];
-    load_part(dout + r * ld_dout + col, n, v);
-    if (act != DYNB_ACT_NONE) {
-      float z[8];
-      load_part(pre + r * ld_pre + col, n, z);
+  for (int64_t r0 = first + wave; r0 < last; r0 += 4 * TOGETHER) {
+    Raw<T> d[TOGETHER], z[TOGETHER];                  // (asked for together; rows past the last repeat it)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= slope(act, z[e]);
-      store_part(dpre + r * ld_dpre + col, n, v);
+    for (int u = 0; u < TOGETHER; ++u) {
+      const int64_t r = min(r0 + 4 * u, last - 1);
+      d[u] = load_raw(dout + r * ld_dout + col, n);
+      if (act != DYNB_ACT_NONE) z[u] = load_raw(pre + r * ld_pre + col, n);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] += v[e];
+    for (int u = 0; u < TOGETHER; ++u) {
+      if (r0 + 4 * u >= last) continue;
+      float v[8];
+      unpack(d[u], n, v);
+      if (act != DYNB_ACT_NONE) {
+        float x[8];
+        unpack(z[u], n, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float slope;
+          Curve<T>::both(act, x[e], slope);
+          v[e] *= slope;
+        }
+        store_part(dpre + (r0 + 4 * u) * ld_dpre + col, n, v);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += v[e];
+    }
   }
   if (!sums) return;                       // (uniform)
   if (wave) {

@@ -141,38 +141,88 @@ __global__ __launch_bounds__(THREADS) void digit_place_kernel(SortPass p, Segs s
 
 // ---- the sums ----------------------------------------------------------------------------------------------------
 // A token that appears often (a padding token may be all of them) would be one wave's long chain: the sorted tokens are cut
-// into chunks of 64, and one whose tokens are all the same is summed beforehand.  A run is then its first tokens up to a
-// chunk's end, its whole chunks, and the rest.
-constexpr int CHUNK = 64, SPAN = 64 * GRANULE;   // columns of a wave
-constexpr int AHEAD = 4;                         // rows asked for at once
+// into chunks of 32, and one whose tokens are all the same is summed beforehand.  A run is then its first tokens up to a
+// chunk's end, its whole chunks, and the rest.  A lane has four neighbouring columns twice, 256 apart, so that every access of a
+// wave is one stretch of memory; the numbers of 64 tokens are loaded at once and AHEAD of their rows are asked for together.
+constexpr int CHUNK = 32, QUAD = 4, HALF = 64 * QUAD, SPAN = 2 * HALF;   // SPAN: columns of a wave
+constexpr int AHEAD = 8;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 struct TableGrad {
   const int32_t* keys; const int32_t* tokens;    // sorted
   const void* dout; int64_t ld_dout;
   float* chunk_sums;                             // [chunks][cols]
   float* dtable; int64_t worker_stride;
-  int64_t n, vocabulary;
+  int64_t n; int vocabulary;
   int cols, workers;
   float scale;
 };
 
-// s += the rows of sorted tokens [from, to), in order
+// The first n of four elements (n <= 0: none is read), zeros for the others; as loaded, and as values.
+template <typename T> struct Quad;
+template <> struct Quad<float> { u32x4 v; };
+template <> struct Quad<bf16> { u32x2 v; };
+__device__ inline Quad<float> load_quad(const float* p, int n) {
+  Quad<float> q = {{0, 0, 0, 0}};
+  if (n >= QUAD) {
+    q.v = load16(p);
+  } else if (n > 0) {
+#pragma unroll
+    for (int e = 0; e < QUAD - 1; ++e)
+      if (e < n) q.v[e] = __float_as_uint(p[e]);
+  }
+  return q;
+}
+__device__ inline Quad<bf16> load_quad(const bf16* p, int n) {
+  Quad<bf16> q = {{0, 0}};
+  if (n >= QUAD) {
+    q.v = *(const u32x2_any*)p;
+  } else if (n > 0) {
+    q.v[0] = ((const uint16_t*)p)[0];
+    if (n > 1) q.v[0] |= (uint32_t)((const uint16_t*)p)[1] << 16;
+    if (n > 2) q.v[1] = ((const uint16_t*)p)[2];
+  }
+  return q;
+}
+__device__ inline f32x4_any values(const Quad<float>& q) {
+  return f32x4_any{__uint_as_float(q.v[0]), __uint_as_float(q.v[1]), __uint_as_float(q.v[2]), __uint_as_float(q.v[3])};
+}
+__device__ inline f32x4_any values(const Quad<bf16>& q) {
+  return f32x4_any{__uint_as_float(q.v[0] << 16), __uint_as_float(q.v[0] & 0xffff0000u), __uint_as_float(q.v[1] << 16),
+                   __uint_as_float(q.v[1] & 0xffff0000u)};
+}
+template <bool PAST> __device__ inline void store_quad(float* p, int n, const f32x4_any& v) {
+  if (n >= QUAD) {
+    if (PAST) __builtin_nontemporal_store(v, (f32x4_any*)p);
+    else *(f32x4_any*)p = v;
+  } else if (n > 0) {
+#pragma unroll
+    for (int e = 0; e < QUAD - 1; ++e)
+      if (e < n) p[e] = v[e];
+  }
+}
+
+// s += the rows of sorted tokens [from, to), in order (from and to the same in the whole wave)
 template <typename T>
-__device__ inline void add_rows(const TableGrad& p, int64_t from, int64_t to, int c, int n, float (&s)[GRANULE]) {
-  for (int64_t i = from; i < to; i += AHEAD) {
-    Raw<T> r[AHEAD];
+__device__ inline void add_rows(const TableGrad& p, int64_t from, int64_t to, int c, f32x4_any (&s)[2]) {
+  const int n0 = p.cols - c, n1 = n0 - HALF;
+  for (int64_t i0 = from; i0 < to; i0 += 64) {
+    const int count = (int)min((int64_t)64, to - i0), lane = threadIdx.x & 63;
+    const int mine = p.tokens[i0 + (lane < count ? lane : count - 1)];
+    for (int i = 0; i < count; i += AHEAD) {
+      Quad<T> q[AHEAD][2];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int64_t at = i + u < to ? i + u : to - 1;
-      r[u] = load_raw((const T*)p.dout + (int64_t)p.tokens[at] * p.ld_dout + c, n);
-    }
+      for (int u = 0; u < AHEAD; ++u) {
+        if (i + u >= count) continue;                  // (uniform)
+        const T* const row = (const T*)p.dout + (int64_t)__builtin_amdgcn_readlane(mine, i + u) * p.ld_dout + c;
+        q[u][0] = load_quad(row, n0);
+        q[u][1] = load_quad(row + HALF, n1);
+      }
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      float v[GRANULE];
-      unpack(r[u], n, v);
-      if (i + u < to) {
-#pragma unroll
-        for (int e = 0; e < GRANULE; ++e) s[e] += v[e];
+      for (int u = 0; u < AHEAD; ++u) {
+        if (i + u >= count) continue;
+        s[0] += values(q[u][0]);
+        s[1] += values(q[u][1]);
       }
     }
   }
@@ -180,18 +230,20 @@ __device__ inline void add_rows(const TableGrad& p, int64_t from, int64_t to, in
 
 template <typename T>
 __global__ __launch_bounds__(256) void chunk_rows_kernel(TableGrad p) {
-  const int64_t chunk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), first = chunk * CHUNK;
+  const int64_t chunk = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = chunk * CHUNK;
   if (first + CHUNK > p.n) return;
   const int key = p.keys[first];
   if (key != p.keys[first + CHUNK - 1] || key >= p.workers * p.vocabulary) return;
-  const int c = blockIdx.y * SPAN + (threadIdx.x & 63) * GRANULE, n = min(p.cols - c, GRANULE);
-  float s[GRANULE] = {};
-  add_rows<T>(p, first, first + CHUNK, c, n, s);
-  store_part(p.chunk_sums + chunk * p.cols + c, n, s);
+  const int c = blockIdx.y * SPAN + (threadIdx.x & 63) * QUAD;
+  f32x4_any s[2] = {};
+  add_rows<T>(p, first, first + CHUNK, c, s);
+  float* const to = p.chunk_sums + chunk * p.cols + c;
+  store_quad<false>(to, p.cols - c, s[0]);
+  store_quad<false>(to + HALF, p.cols - c - HALF, s[1]);
 }
 
 // Sorted tokens with keys below `key` (the whole wave takes part): 64 places at a time.
-__device__ inline int64_t keys_below(const int32_t* keys, int64_t n, int64_t key) {
+__device__ inline int64_t keys_below(const int32_t* keys, int64_t n, int key) {
   const int lane = threadIdx.x & 63;
   int64_t low = 0, high = n;                     // the answer is in [low, high]
   while (high > low) {
@@ -209,15 +261,14 @@ __device__ inline int64_t keys_below(const int32_t* keys, int64_t n, int64_t key
 constexpr int PER = 8;
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
-  const int lane = threadIdx.x & 63;
-  const int64_t all = p.workers * p.vocabulary;
-  const int64_t first = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * PER;
+  const int lane = threadIdx.x & 63, all = p.workers * p.vocabulary;
+  const int first = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * PER;
   if (first >= all) return;
-  const int c = blockIdx.y * SPAN + lane * GRANULE, n = min(p.cols - c, GRANULE);
+  const int c = blockIdx.y * SPAN + lane * QUAD, n0 = p.cols - c, n1 = n0 - HALF;
   int64_t at = keys_below(p.keys, p.n, first);
   int mine = at + lane < p.n ? p.keys[at + lane] : 0x7fffffff;      // the 64 keys from `at` on
-  for (int r = 0; r < PER && first + r < all; ++r) {
-    const int64_t row = first + r;
+  int worker = first / p.vocabulary, id = first % p.vocabulary;
+  for (int row = first; row < first + PER && row < all; ++row) {
     // this row's run begins at `begin`, the first of the 64 that is not below it
     const int less = __builtin_popcountll(__ballot(mine < row)), same = __builtin_popcountll(__ballot(mine == row));
     int64_t begin = at + less, end = begin + same;
@@ -227,23 +278,31 @@ __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
       at = end;
       mine = at + lane < p.n ? p.keys[at + lane] : 0x7fffffff;
     }
-    float s[GRANULE] = {};
-    const int64_t chunk = (begin + CHUNK - 1) / CHUNK, last = end / CHUNK;
-    if (chunk < last) {
-      add_rows<T>(p, begin, chunk * CHUNK, c, n, s);
-      for (int64_t q = chunk; q < last; ++q) {
-        float v[GRANULE];
-        load_part(p.chunk_sums + q * p.cols + c, n, v);
-#pragma unroll
-        for (int e = 0; e < GRANULE; ++e) s[e] += v[e];
+    f32x4_any s[2] = {};
+    if (begin < end) {
+      const int64_t chunk = (begin + CHUNK - 1) / CHUNK, last = end / CHUNK;
+      if (chunk < last) {
+        add_rows<T>(p, begin, chunk * CHUNK, c, s);
+#pragma unroll 4
+        for (int64_t q = chunk; q < last; ++q) {
+          const float* const from = p.chunk_sums + q * p.cols + c;
+          s[0] += values(load_quad(from, n0));
+          s[1] += values(load_quad(from + HALF, n1));
+        }
+        add_rows<T>(p, last * CHUNK, end, c, s);
+      } else {
+        add_rows<T>(p, begin, end, c, s);
       }
-      add_rows<T>(p, last * CHUNK, end, c, n, s);
-    } else {
-      add_rows<T>(p, begin, end, c, n, s);
+      s[0] *= p.scale;
+      s[1] *= p.scale;
     }
-#pragma unroll
-    for (int e = 0; e < GRANULE; ++e) s[e] *= p.scale;
-    store_part<PAST>(p.dtable + row / p.vocabulary * p.worker_stride + row % p.vocabulary * p.cols + c, n, s);
+    float* const to = p.dtable + worker * p.worker_stride + (int64_t)id * p.cols + c;
+    store_quad<PAST>(to, n0, s[0]);
+    store_quad<PAST>(to + HALF, n1, s[1]);
+    if (++id == p.vocabulary) {
+      id = 0;
+      ++worker;
+    }
   }
 }
 
@@ -281,7 +340,7 @@ void launch_table_grad(const TableGrad& p, hipStream_t st) {
   const unsigned spans = (p.cols + SPAN - 1) / SPAN;
   if (p.n >= CHUNK)
     hipLaunchKernelGGL(chunk_rows_kernel<T>, dim3((unsigned)((p.n / CHUNK + 3) / 4), spans), dim3(256), 0, st, p);
-  const int64_t rows = p.workers * p.vocabulary;
+  const int64_t rows = (int64_t)p.workers * p.vocabulary;
   const dim3 grid((unsigned)((rows + 4 * PER - 1) / (4 * PER)), spans);
   if (past_caches(4.0 * rows * p.cols)) hipLaunchKernelGGL((table_grad_kernel<T, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((table_grad_kernel<T, false>), grid, dim3(256), 0, st, p);
@@ -357,7 +416,7 @@ extern "C" int dynb_embedding_backward(const dynb_embedding_desc* d, const int32
     }
   }
   const TableGrad p = {keys[cur], tokens[cur], dout, d->ld_dout ? d->ld_dout : d->cols, (float*)(ws + w.sums), dtable,
-                       worker_stride, d->tokens, d->vocabulary, d->cols, K, d->scale};
+                       worker_stride, d->tokens, (int)d->vocabulary, d->cols, K, d->scale};
   if (d->dtype == DYNB_F32) launch_table_grad<float>(p, st);
   else launch_table_grad<bf16>(p, st);
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "embedding_backward launch failed");

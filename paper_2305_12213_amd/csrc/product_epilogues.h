@@ -7,28 +7,49 @@
 namespace dynb {
 
 // act(v) and its derivative, in fp32.
-//   silu  v p, p = 1 / (1 + e^-v);          p (1 + v (1 - p))
+//   silu  v p, p = 1 / (1 + e^-v);             p (1 + v (1 - p))
 //   gelu  v P, P = (1 + erf(v / sqrt 2)) / 2;  P + v e^(-v^2 / 2) / sqrt(2 pi)
-// (where v's magnitude is beyond an exponential's range p and P are 0 or 1, and the products with 0 vanish)
-__device__ inline float activate(int act, float v) {
-  switch (act) {
-    case DYNB_ACT_RELU: return v < 0.f ? 0.f : v;      // (a NaN stays one)
-    case DYNB_ACT_SILU: return v * (1.f / (1.f + expf(-v)));
-    case DYNB_ACT_GELU: return v * (0.5f + 0.5f * erff(v * 0.70710678f));
-    default: return v;
+// (where v's magnitude is beyond an exponential's range p and P are 0 or 1, and the products with 0 vanish.)  Values that are
+// rounded to 16 bits take the hardware's exponential and reciprocal and erf by Abramowitz and Stegun 7.1.26
+// (off by 1.5e-7 at most), which shares its exponential with gelu's derivative.
+template <typename T> struct Curve {
+  static constexpr bool SHORT = sizeof(T) == 2;
+  static __device__ float power(float v) { return SHORT ? __expf(v) : expf(v); }
+  static __device__ float inverse(float v) { return SHORT ? __builtin_amdgcn_rcpf(v) : 1.f / v; }
+  // P, and e^(-v^2 / 2)
+  static __device__ float normal(float v, float& bell) {
+    bell = power(-0.5f * v * v);
+    if (!SHORT) return 0.5f + 0.5f * erff(v * 0.70710678f);
+    const float t = inverse(1.f + 0.3275911f * 0.70710678f * fabsf(v));
+    const float tail = 0.5f * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))) * bell;
+    return v < 0.f ? tail : 1.f - tail;
   }
-}
-__device__ inline float slope(int act, float v) {
-  switch (act) {
-    case DYNB_ACT_RELU: return v > 0.f ? 1.f : 0.f;
-    case DYNB_ACT_SILU: {
-      const float p = 1.f / (1.f + expf(-v));
-      return p * (1.f + v * (1.f - p));
+  static __device__ float value(int act, float v) {
+    float slope;
+    return both(act, v, slope);
+  }
+  static __device__ float both(int act, float v, float& slope) {
+    switch (act) {
+      case DYNB_ACT_RELU:
+        slope = v > 0.f ? 1.f : 0.f;
+        return v < 0.f ? 0.f : v;            // (a NaN stays one)
+      case DYNB_ACT_SILU: {
+        const float p = inverse(1.f + power(-v));
+        slope = p * (1.f + v * (1.f - p));
+        return v * p;
+      }
+      case DYNB_ACT_GELU: {
+        float bell;
+        const float p = normal(v, bell);
+        slope = p + v * bell * 0.39894228f;
+        return v * p;
+      }
+      default:
+        slope = 1.f;
+        return v;
     }
-    case DYNB_ACT_GELU: return 0.5f + 0.5f * erff(v * 0.70710678f) + v * expf(-0.5f * v * v) * 0.39894228f;
-    default: return 1.f;
   }
-}
+};
 
 // out = act(v + bias) + residual; what the activation is taken of can be kept
 template <typename T> struct LinearOut {
@@ -48,7 +69,7 @@ template <typename T> struct LinearOut {
     if (pre) store_part(pre + i * ld_pre + col, n, v);
     if (act != DYNB_ACT_NONE) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = activate(act, v[e]);
+      for (int e = 0; e < 8; ++e) v[e] = Curve<T>::value(act, v[e]);
     }
     if (residual) {
       float r[8];
@@ -73,7 +94,7 @@ template <typename T> struct GatedOut {
       store_part(up + i * ld_kept + col, n, w);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = activate(act, v[e]) * w[e];
+    for (int e = 0; e < 8; ++e) v[e] = Curve<T>::value(act, v[e]) * w[e];
     store_part(hidden + i * ld_hidden + col, n, v);
   }
 };
@@ -92,8 +113,10 @@ template <typename T> struct GatedGrad {
     load_part(up + i * ld_kept + col, n, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      a[e] = v[e] * u[e] * slope(act, g[e]);
-      g[e] = activate(act, g[e]);
+      float slope;
+      const float value = Curve<T>::both(act, g[e], slope);
+      a[e] = v[e] * u[e] * slope;
+      g[e] = value;
       b[e] = v[e] * g[e];
       u[e] *= g[e];
     }
@@ -145,15 +168,15 @@ template <typename T> bool direct_ok(const Product& p, int form) {
          (form == WEIGHTS ? whole_granules<T>(p.M) : whole_granules<T>(p.K));
 }
 
-template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, bool DIRECT, class Ep>
+template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, Access ACCESS, class Ep>
 int launch_tiles(const Product& p, const Segs& s, const Ep& ep, hipStream_t st) {
   constexpr int BNS = DUAL ? BN / 2 : BN;
   const int64_t tiles_j = (p.N + BNS - 1) / BNS;
   int64_t blocks;
-  if (FORM == WEIGHTS) blocks = (p.M + BM - 1) / BM * tiles_j * p.groups;
+  if (FORM == WEIGHTS) blocks = weight_places((p.M + BM - 1) / BM * tiles_j) * p.groups;
   else blocks = (p.offsets ? p.rows / BM + (p.rows < p.groups ? p.rows : p.groups) : (p.rows + BM - 1) / BM) * tiles_j;
   if (blocks > INT32_MAX / 64) return fail(DYNB_ERR_UNSUPPORTED, "a product of more than 2^25 tiles");
-  hipLaunchKernelGGL((product_kernel<T, FORM, DUAL, BM, BN, WM, WN, NB, SOON, DIRECT, Ep>), dim3((unsigned)blocks, p.splits),
+  hipLaunchKernelGGL((product_kernel<T, FORM, DUAL, BM, BN, WM, WN, NB, SOON, ACCESS, Ep>), dim3((unsigned)blocks, p.splits),
                      dim3(WM * WN * 64), 0, st, p, s, ep);
   if (p.splits > 1) {
     const int64_t n = p.partial_rows * ((p.N + 7) / 8);
@@ -166,17 +189,21 @@ template <typename T, int FORM, bool DUAL, class Ep>
 int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* stream) {
   const hipStream_t st = (hipStream_t)stream;
   const bool direct = direct_ok<T>(p, FORM);
+  // (rows of less than a granule: nothing to shift)
+  const bool singly = (FORM == WEIGHTS ? p.M : p.K) < 16 / (int)sizeof(T) || (FORM != ROWS_NT && p.N < 16 / (int)sizeof(T));
   if constexpr (FORM != WEIGHTS) {
-    if (tiles == TILES_32) {
-      constexpr int WN = DUAL ? 2 : 4;
-      return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, true>(p, s, ep, st)
-                    : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, false>(p, s, ep, st);
-    }
+    constexpr int WN = DUAL ? 2 : 4;
+    if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, SINGLY>(p, s, ep, st);
+    if (tiles == TILES_32)
+      return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, DIRECT>(p, s, ep, st)
+                    : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, SHIFTED>(p, s, ep, st);
+  } else {
+    if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, SINGLY>(p, s, ep, st);
   }
-  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, false>(p, s, ep, st);
+  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, SHIFTED>(p, s, ep, st);
   if constexpr (sizeof(T) == 2)
-    if (tiles == TILES_256) return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 2, 4, true>(p, s, ep, st);
-  return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, true>(p, s, ep, st);
+    if (tiles == TILES_256) return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 2, 4, DIRECT>(p, s, ep, st);
+  return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, DIRECT>(p, s, ep, st);
 }
 
 }  // namespace

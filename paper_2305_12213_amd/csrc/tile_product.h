@@ -10,9 +10,9 @@
 // transpose reads, fp32 element by element.  One step is two granules: a 32 x 32 x 16 matrix instruction in bf16, four of
 // 32 x 32 x 2 in fp32, whose k are numbered so that both operands' lanes hold the same ones.
 //
-// DIRECT: copies go from memory straight to LDS, a ring of NB stages, a step's fragments are fetched one step ahead, and
-// fetches and copies stand between the matrix instructions (as in the dense layers' products).  Otherwise (rows that are
-// no multiple of 16 bytes) they pass through registers, which can fill up partial granules with zeros.
+// Copies go from memory straight to LDS, a ring of NB stages, a step's fragments are fetched one step ahead, and
+// fetches and copies stand between the matrix instructions (as in the dense layers' products).  Rows that are no
+// multiple of 16 bytes pass through registers, which can fill up partial granules with zeros.
 #ifndef DYNB_TILE_PRODUCT_H
 #define DYNB_TILE_PRODUCT_H
 
@@ -57,6 +57,11 @@ __device__ inline int64_t run_of_xcd(int64_t pid, int64_t total) {
   const int64_t per = total / 8, extra = total % 8, xcd = pid % 8;
   return xcd * per + (xcd < extra ? xcd : extra) + pid / 8;
 }
+// Gradients of weights: every group's tiles are spread over all XCDs (groups differ in their rows, so that whole groups to
+// an XCD left seven of them waiting: 32 groups of 16384 rows, 2048 x 2048, 545 us), in runs where there are enough of them: places
+// for a multiple of 8 tiles, some of them empty.
+constexpr int64_t XCD_RUNS = 32;
+__host__ __device__ inline int64_t weight_places(int64_t tiles) { return tiles < XCD_RUNS ? tiles : (tiles + 7) / 8 * 8; }
 // Place -> tile, in bands of 8 tile rows, so that a run covers a compact rectangle.
 __device__ inline void tile_of_place(int64_t t, int tiles_i, int tiles_j, int& ti, int& tj) {
   const int64_t bsz = (int64_t)8 * tiles_j;
@@ -119,21 +124,30 @@ __device__ inline void find_group(const Product& p, int BM, int ti, int& group, 
   last = first = 0;       // (not reached: ti is below the number of tiles)
 }
 
-// The first n of a granule's elements, zeros behind them (n <= 0: none is read).
-template <typename T> __device__ inline u32x4 load_granule(const T* p, int n) {
-  constexpr int G = 16 / sizeof(T);
+// How an operand's granules reach LDS.  DIRECT: copied, all of them whole and at multiples of 16 bytes.  SHIFTED: through
+// registers; the last granule of a row is loaded so that it ends with the row and shifted into its place, which needs rows of
+// a granule at least and keeps every load unconditional and in flight until it is stored.  SINGLY: element by element.
+enum Access { DIRECT, SHIFTED, SINGLY };
+
+template <typename T> __device__ inline u32x4 load_singly(const T* p, int n) {
   u32x4 r = {0, 0, 0, 0};
-  if (n >= G) {
-    r = load16(p);
-  } else if (n > 0) {
 #pragma unroll
-    for (int e = 0; e < G; ++e) {
-      if (e >= n) continue;
-      if (sizeof(T) == 4) r[e] = ((const uint32_t*)p)[e];
-      else r[e / 2] |= (uint32_t)((const uint16_t*)p)[e] << (16 * (e & 1));
-    }
+  for (int e = 0; e < 16 / (int)sizeof(T); ++e) {
+    if (e >= n) continue;
+    if (sizeof(T) == 4) r[e] = ((const uint32_t*)p)[e];
+    else r[e / 2] |= (uint32_t)((const uint16_t*)p)[e] << (16 * (e & 1));
   }
   return r;
+}
+// The last n of a granule's elements first, zeros behind them (n <= 0: zeros).
+template <typename T> __device__ inline u32x4 shifted(u32x4 v, int n) {
+  constexpr int G = 16 / (int)sizeof(T);
+  if (n >= G) return v;
+  const int bytes = (G - max(n, 0)) * (int)sizeof(T);
+  if (bytes & 8) v = u32x4{v[2], v[3], 0, 0};
+  if (bytes & 4) v = u32x4{v[1], v[2], v[3], 0};
+  if (bytes & 2) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+  return n > 0 ? v : u32x4{0, 0, 0, 0};
 }
 
 // Slot of granule g in reduction row k of a turned tile with rows of `pitch` bytes: the rows that one read touches
@@ -151,11 +165,11 @@ __device__ inline void patch_fence() {
 // A tile of BM x BN results, WM x WN waves.  DUAL: two products with BN / 2 columns each, which share A; a wave has the same
 // columns of both.  Ep: what is done with 8 neighbouring results of a row.  SOON: of a stage's copies, eighths that are
 // issued in the last step of the stage that releases its buffer, and in the first step of the next.
-template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, bool DIRECT, class Ep>
+template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, Access ACCESS, class Ep>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs segs, Ep ep) {
   constexpr bool TA = FORM == WEIGHTS, TB = FORM != ROWS_NT;
   constexpr int G = 16 / sizeof(T), BK = 8 * G, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = DIRECT ? NB : 2;
+  constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = ACCESS == DIRECT ? NB : 2;
   constexpr int CA = BM / 8 / NW, CB = BN / 8 / NW, NC = CA + CB;   // copies of 1 KB per wave and stage
   constexpr uint32_t STAGE = (BM + BN) * 128;
   constexpr int CW = 32 * TN, EP = CW + 4;                          // a wave's columns, row pitch of its patch
@@ -175,10 +189,13 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   if constexpr (FORM == WEIGHTS) {
     const int tiles_i = (p.M + BM - 1) / BM;
     const int64_t tiles = (int64_t)tiles_i * tiles_j;
-    const int64_t t = run_of_xcd(blockIdx.x, tiles * p.groups);
+    const int64_t places = weight_places(tiles);
+    int64_t place = blockIdx.x % places;
+    if (places >= XCD_RUNS) place = place % 8 * (places / 8) + place / 8;
+    if (place >= tiles) return;
     int ti;
-    group = (int)(t / tiles);
-    tile_of_place(t % tiles, tiles_i, tiles_j, ti, tj);
+    group = (int)(blockIdx.x / places);
+    tile_of_place(place, tiles_i, tiles_j, ti, tj);
     i0 = (int64_t)ti * BM;
     i_end = p.M;
     int64_t last;
@@ -259,7 +276,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
       need[u] = g * G;
       have[u] = r < limit ? G : 0;
     }
-    if (DIRECT && have[u] == 0) need[u] = 0x7fffffff;
+    if (ACCESS == DIRECT && have[u] == 0) need[u] = 0x7fffffff;
   }
   auto source = [&](int u) { return u < CA ? 0 : DUAL && (CB * wave + u - CA) >= BNS / 8 ? 2 : 1; };
   auto slot_of = [&](int u) { return u < CA ? (CA * wave + u) * 1024u : BM * 128u + (CB * wave + u - CA) * 1024u; };
@@ -342,7 +359,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   };
   constexpr int NM = TM * TN, NF = TM + TN;
 
-  if constexpr (DIRECT) {
+  if constexpr (ACCESS == DIRECT) {
     // copies behind step 3 of the stage before, 0, 1, 2: up to Q[1], Q[2], ...
     constexpr int Q[5] = {0, SOON * NC / 8, 2 * SOON * NC / 8, SOON * NC / 4 + (NC - SOON * NC / 4) / 2, NC};
 #pragma unroll 1
@@ -393,20 +410,38 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     __syncthreads();
   } else {
     u32x4 held[NC];
+    auto count_of = [&](int u, int l) {    // elements of granule u where l are left of the reduction
+      return have[u] == 0 || need[u] >= l ? 0 : (u < CA ? TA : TB) ? have[u] : min(G, l - need[u]);
+    };
+    int left_held;
     auto load_stage = [&]() {
+      left_held = left;
 #pragma unroll
       for (int u = 0; u < NC; ++u) {
-        const bool turned = u < CA ? TA : TB;
-        const int n = have[u] == 0 || need[u] >= left ? 0 : turned ? have[u] : min(G, left - need[u]);
-        held[u] = load_granule((const T*)(uintptr_t)(from[source(u)] + off[u]), n);
+        const int n = count_of(u, left);
+        const uint64_t at = from[source(u)] + off[u];
+        if constexpr (ACCESS == SINGLY) {
+          held[u] = load_singly((const T*)(uintptr_t)at, n);
+        } else {
+          const uint64_t back = (uint64_t)(n < G ? G - n : 0) * sizeof(T);
+          held[u] = load16((const void*)(uintptr_t)(n > 0 ? at - back : (uint64_t)(uintptr_t)(u < CA ? p.A[0] : p.B[0])));
+        }
       }
     };
     auto store_stage = [&](uint32_t buf) {
 #pragma unroll
-      for (int u = 0; u < NC; ++u) *(u32x4*)((char*)&ring[0] + buf + slot_of(u) + lane * 16) = held[u];
+      for (int u = 0; u < NC; ++u) {
+        if constexpr (ACCESS == SHIFTED) {
+          const int n = count_of(u, left_held);
+          if (__any(n < G)) held[u] = shifted<T>(held[u], n);
+        }
+        *(u32x4*)((char*)&ring[0] + buf + slot_of(u) + lane * 16) = held[u];
+      }
     };
-    load_stage();
-    store_stage(0);
+    if (s_begin < s_end) {                 // (no rows: there may be no memory either)
+      load_stage();
+      store_stage(0);
+    }
     __syncthreads();
     uint32_t slot = 0;
 #pragma unroll 1
@@ -480,6 +515,7 @@ __global__ __launch_bounds__(256) void joined_kernel(Product p, Ep ep) {
   if (row < first || row >= rows) return;
   const int col = (int)(at % chunks) * 8, n = min(p.N - col, 8);
   float v[8] = {}, w[8] = {}, x[8];
+#pragma unroll 4
   for (int s = 0; s < p.splits; ++s) {
     const float* const from = p.partial + (s * p.partial_rows + row) * wide + col;
     load_part(from, n, x);
