@@ -15,6 +15,8 @@ int64_t tiles_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
 int64_t row_tiles_of(int64_t rows, int groups, int size) {
   return groups == 1 ? tiles_of(rows, size) : rows / size + (std::min<int64_t>(groups, rows) + 1) / 2;
 }
+// (sizes alone: rows of other pitches or places take the same parts)
+bool whole_granules(int dtype, int64_t n) { return n % (dtype == DYNB_F32 ? 4 : 8) == 0; }
 // Into how many parts a reduction of `stages` is divided: workgroups run `slots` at a time, each for its share of the stages;
 // a part more is worth it where that time falls by `worth` stages at least (what writing and joining it takes).
 int parts(int64_t tiles, int64_t slots, int64_t stages, int64_t worth) {
@@ -34,15 +36,19 @@ ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduct
   const int half = dual ? 2 : 1;
   const int64_t stages = tiles_of(reduction, dtype == DYNB_F32 ? 32 : 64);
   const int64_t each = rows / std::min<int64_t>(groups, std::max<int64_t>(rows, 1));
-  if (each <= 48) return {TILES_32, parts(row_tiles_of(rows, groups, 32) * tiles_of(N, 128 / half), 512, stages, 2)};
+  if (each <= 48) {                        // (memory bounds these: parts only until every compute unit has work)
+    const int64_t tiles = row_tiles_of(rows, groups, 32) * tiles_of(N, 128 / half);
+    return {TILES_32, (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(tiles, 1), stages / 4, (int64_t)16}))};
+  }
   if (dtype == DYNB_BF16 && each >= 160 && row_tiles_of(rows, groups, 256) * tiles_of(N, 256 / half) >= 192) return {TILES_256, 1};
-  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), 256, stages, dtype == DYNB_F32 ? 1 : 4)};
+  const bool whole = whole_granules(dtype, N) && whole_granules(dtype, reduction);
+  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), whole ? 256 : 512, stages, dtype == DYNB_F32 ? 1 : 4)};
 }
-ProductPlan plan_weights(int dtype, int64_t rows, int groups, int M, int N, bool dual) {
-  const int half = dual ? 2 : 1;
+ProductPlan plan_weights(int dtype, int64_t rows, int groups, int M, int N, int matrices) {
   const int64_t stages = tiles_of(rows / groups, dtype == DYNB_F32 ? 32 : 64);
-  if (dtype == DYNB_BF16 && tiles_of(M, 256) * tiles_of(N, 256 / half) * groups >= 192) return {TILES_256, 1};
-  return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128 / half) * groups, 256, stages, dtype == DYNB_F32 ? 2 : 6)};
+  if (dtype == DYNB_BF16 && tiles_of(M, 256) * tiles_of(N, 256) * groups * matrices >= 192) return {TILES_256, 1};
+  const bool whole = whole_granules(dtype, N) && whole_granules(dtype, M);
+  return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128) * groups * matrices, whole ? 256 : 512, stages, dtype == DYNB_F32 ? 2 : 6)};
 }
 // Bytes of Product::partial (0 where the plan has one part).
 size_t partial_bytes(const ProductPlan& plan, int64_t rows, int64_t columns) {
@@ -53,6 +59,9 @@ void cut(Product& p, const ProductPlan& plan, int64_t partial_rows, void* partia
   p.partial = (float*)partial;
   p.partial_rows = partial_rows;
 }
+
+// Whether rows of weights' gradients are whole lines: others are not sent past the caches, which put the pieces together.
+template <typename O> bool whole_lines(int cols) { return cols * sizeof(O) % 128 == 0; }
 
 size_t size_of(int dtype) { return dtype == DYNB_F32 ? 4 : 2; }
 int64_t padded(int64_t cols, int dtype) { return round_up(cols, 16 / (int)size_of(dtype)); }
@@ -186,7 +195,7 @@ LinearBackward layout(const dynb_linear_desc* d, const Segs& s) {
   at += (size_t)round_up((int64_t)bias_chunks(s).first[s.K] * d->n_out * 4, 16);
   w.partial = at;
   const size_t dx = partial_bytes(plan_rows(d->dtype, T, 1, d->n_in, d->n_out, false), T, d->n_in);
-  const size_t dw = partial_bytes(plan_weights(d->dtype, T, s.K, d->n_in, d->n_out, false), (int64_t)s.K * d->n_in, d->n_out);
+  const size_t dw = partial_bytes(plan_weights(d->dtype, T, s.K, d->n_in, d->n_out, 1), (int64_t)s.K * d->n_in, d->n_out);
   w.end = at + std::max(dx, dw);
   return w;
 }
@@ -244,9 +253,9 @@ int linear_gradients(const dynb_linear_desc* d, const Segs& s, const void* x, co
     p.pairs = 1;
     p.groups = p.workers = s.K;
     p.rows = rows;
-    const ProductPlan plan = plan_weights(d->dtype, rows, s.K, n, m, false);
+    const ProductPlan plan = plan_weights(d->dtype, rows, s.K, n, m, 1);
     cut(p, plan, (int64_t)s.K * n, workspace + w.partial);
-    const WeightOut<O> ep = {{(O*)dweight, nullptr}, dweight_stride, 0, s.K, m};
+    const WeightOut<O> ep = {{(O*)dweight, nullptr}, dweight_stride, 0, s.K, m, s.K, past_caches((double)sizeof(O) * s.K * n * m) && whole_lines<O>(m)};
     return launch_weights<T, O>(p, plan.tiles, s, ep, stream);
   }
   return DYNB_OK;
@@ -275,10 +284,10 @@ ProductPlan plan_dx(const dynb_gated_block_desc* d) {
   return plan_rows(d->dtype, d->rows, d->n_experts, d->cols, 2 * (int64_t)d->hidden, false);
 }
 ProductPlan plan_dup(const dynb_gated_block_desc* d, int K) {
-  return plan_weights(d->dtype, d->rows, d->n_experts * K, d->cols, d->hidden, true);
+  return plan_weights(d->dtype, d->rows, d->n_experts * K, d->cols, d->hidden, 2);
 }
 ProductPlan plan_ddown(const dynb_gated_block_desc* d, int K) {
-  return plan_weights(d->dtype, d->rows, d->n_experts * K, d->hidden, d->cols, false);
+  return plan_weights(d->dtype, d->rows, d->n_experts * K, d->hidden, d->cols, 1);
 }
 
 Product by_expert(const dynb_gated_block_desc* d, const int32_t* offsets) {
@@ -376,9 +385,11 @@ int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offset
   p.M = H;
   p.N = F;
   ProductPlan plan = plan_dup(d, K);
-  cut(p, plan, (int64_t)p.groups * H, partial);
+  p.pairs = 2;
+  cut(p, plan, 2 * (int64_t)p.groups * H, partial);
   const int64_t matrix = (int64_t)H * F;
-  const WeightOut<O> ep = {{(O*)dw_gate, (O*)dw_up}, worker_stride, matrix, K, F};
+  const bool past = past_caches((double)sizeof(O) * p.groups * matrix);
+  const WeightOut<O> ep = {{(O*)dw_gate, (O*)dw_up}, worker_stride, matrix, K, F, p.groups, past && whole_lines<O>(F)};
   if (int rc = launch_weights<T, O>(p, plan.tiles, whole, ep, stream)) return rc;
   p.A[0] = p.A[1] = hidden;
   p.B[0] = p.B[1] = dy;
@@ -386,9 +397,10 @@ int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offset
   p.ldb = ld_dy;
   p.M = F;
   p.N = H;
+  p.pairs = 1;
   plan = plan_ddown(d, K);
   cut(p, plan, (int64_t)p.groups * F, partial);
-  const WeightOut<O> down = {{(O*)dw_down, nullptr}, worker_stride, matrix, K, H};
+  const WeightOut<O> down = {{(O*)dw_down, nullptr}, worker_stride, matrix, K, H, p.groups, past && whole_lines<O>(H)};
   return launch_weights<T, O>(p, plan.tiles, whole, down, stream);
 }
 
@@ -482,7 +494,7 @@ extern "C" size_t dynb_gated_block_backward_workspace_bytes(const dynb_gated_blo
   const int64_t groups = (int64_t)d->n_experts * K;
   return 3 * (size_t)hidden_bytes(d) +
          std::max({partial_bytes(plan_dhidden(d), d->rows, d->hidden), partial_bytes(plan_dx(d), d->rows, d->cols),
-                   partial_bytes(plan_dup(d, K), groups * d->cols, 2 * (int64_t)d->hidden),
+                   partial_bytes(plan_dup(d, K), 2 * groups * d->cols, d->hidden),
                    partial_bytes(plan_ddown(d, K), groups * d->hidden, d->cols)});
 }
 

@@ -2,6 +2,8 @@
 #ifndef DYNB_PRODUCT_EPILOGUES_H
 #define DYNB_PRODUCT_EPILOGUES_H
 
+#include <algorithm>
+
 #include "tile_product.h"
 
 namespace dynb {
@@ -51,15 +53,26 @@ template <typename T> struct Curve {
   }
 };
 
+// ask() loads what an epilogue reads for 8 results (n of them, none where n <= 0), row() uses it.  PACKS: where packed() says so,
+// results are only rounded to 16 bits, and put() stores 8 of them (of the first or the second product).
+
 // out = act(v + bias) + residual; what the activation is taken of can be kept
 template <typename T> struct LinearOut {
-  static constexpr int ROWS_AT_ONCE = 4;
+  static constexpr bool PACKS = sizeof(T) == 2;
   const float* bias;
   const T* residual; int64_t ld_residual;
   T* pre; int64_t ld_pre;
   T* out; int64_t ld_out;
   int act;
-  __device__ void row(int, int64_t i, int col, int n, float (&v)[8], float (&)[8]) const {
+  struct Held {
+    Raw<T> residual;
+  };
+  __device__ Held ask(int64_t i, int col, int n) const {
+    Held h = {};
+    if (residual) h.residual = load_raw(residual + i * ld_residual + col, n);
+    return h;
+  }
+  __device__ void row(int, int64_t i, int col, int n, float (&v)[8], float (&)[8], const Held& h) const {
     if (bias) {
       float b[8];
       load_part(bias + col, n, b);
@@ -73,22 +86,30 @@ template <typename T> struct LinearOut {
     }
     if (residual) {
       float r[8];
-      load_part(residual + i * ld_residual + col, n, r);
+      unpack(h.residual, n, r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
     store_part(out + i * ld_out + col, n, v);
   }
+  __device__ bool packed() const { return !bias && !residual && !pre && act == DYNB_ACT_NONE; }
+  __device__ void put(int, int64_t i, int col, int n, const u32x4& v, int) const {
+    store_packed((bf16*)out + i * ld_out + col, n, v);
+  }
 };
+
+struct Nothing {};
 
 // hidden = act(gate) * up, from the sums before they are rounded
 template <typename T> struct GatedOut {
-  static constexpr int ROWS_AT_ONCE = 4;
+  static constexpr bool PACKS = false;
   T* gate; T* up;             // or null: not kept
   int64_t ld_kept;
   T* hidden; int64_t ld_hidden;
   int act;
-  __device__ void row(int, int64_t i, int col, int n, float (&v)[8], float (&w)[8]) const {
+  typedef Nothing Held;
+  __device__ Held ask(int64_t, int, int) const { return {}; }
+  __device__ void row(int, int64_t i, int col, int n, float (&v)[8], float (&w)[8], Held) const {
     if (gate) {
       store_part(gate + i * ld_kept + col, n, v);
       store_part(up + i * ld_kept + col, n, w);
@@ -101,24 +122,29 @@ template <typename T> struct GatedOut {
 
 // from v = gradient of hidden: dgate = v up act'(gate), dup = v act(gate), and hidden once more
 template <typename T> struct GatedGrad {
-  static constexpr int ROWS_AT_ONCE = 1;
+  static constexpr bool PACKS = false;
   const T* gate; const T* up;
   int64_t ld_kept;
   T* dgate; T* dup; T* hidden;
   int64_t ld_hidden;
   int act;
-  __device__ void row(int, int64_t i, int col, int n, float (&v)[8], float (&)[8]) const {
+  struct Held {
+    Raw<T> gate, up;
+  };
+  __device__ Held ask(int64_t i, int col, int n) const {
+    return {load_raw(gate + i * ld_kept + col, n), load_raw(up + i * ld_kept + col, n)};
+  }
+  __device__ void row(int, int64_t i, int col, int n, float (&v)[8], float (&)[8], const Held& h) const {
     float g[8], u[8], a[8], b[8];
-    load_part(gate + i * ld_kept + col, n, g);
-    load_part(up + i * ld_kept + col, n, u);
+    unpack(h.gate, n, g);
+    unpack(h.up, n, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float slope;
       const float value = Curve<T>::both(act, g[e], slope);
       a[e] = v[e] * u[e] * slope;
-      g[e] = value;
-      b[e] = v[e] * g[e];
-      u[e] *= g[e];
+      b[e] = v[e] * value;
+      u[e] *= value;
     }
     store_part(dgate + i * ld_hidden + col, n, a);
     store_part(dup + i * ld_hidden + col, n, b);
@@ -126,16 +152,29 @@ template <typename T> struct GatedGrad {
   }
 };
 
-// gradients of one or two weights: group e * workers + k is worker k's of matrix e
+// gradients of one or two weights: group e * workers + k is worker k's of matrix e; the second weight's groups follow (row) or are
+// named by `product` (put)
 template <typename O> struct WeightOut {
-  static constexpr int ROWS_AT_ONCE = 4;
+  static constexpr bool PACKS = sizeof(O) == 2;
   O* out[2];
   int64_t worker_stride, matrix;
-  int workers, cols;
-  __device__ void row(int group, int64_t i, int col, int n, float (&v)[8], float (&w)[8]) const {
-    const int64_t to = group % workers * worker_stride + group / workers * matrix + i * cols + col;
-    store_part(out[0] + to, n, v);
-    if (out[1]) store_part(out[1] + to, n, w);
+  int workers, cols, groups;
+  bool past;                  // more than the caches keep until it is read: past them
+  typedef Nothing Held;
+  __device__ Held ask(int64_t, int, int) const { return {}; }
+  __device__ void row(int group, int64_t i, int col, int n, float (&v)[8], float (&)[8], Held) const {
+    O* const to = out[group / groups] + place(group % groups, i, col);
+    if (past) store_part<true>(to, n, v);
+    else store_part(to, n, v);
+  }
+  __device__ bool packed() const { return true; }
+  __device__ void put(int group, int64_t i, int col, int n, const u32x4& v, int product) const {
+    O* const to = out[product] + place(group, i, col);
+    if (past) store_packed<true>((bf16*)to, n, v);
+    else store_packed((bf16*)to, n, v);
+  }
+  __device__ int64_t place(int group, int64_t i, int col) const {
+    return group % workers * worker_stride + group / workers * matrix + i * cols + col;
   }
 };
 
@@ -168,15 +207,19 @@ template <typename T> bool direct_ok(const Product& p, int form) {
          (form == WEIGHTS ? whole_granules<T>(p.M) : whole_granules<T>(p.K));
 }
 
-template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, Access ACCESS, class Ep>
+template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
 int launch_tiles(const Product& p, const Segs& s, const Ep& ep, hipStream_t st) {
   constexpr int BNS = DUAL ? BN / 2 : BN;
   const int64_t tiles_j = (p.N + BNS - 1) / BNS;
-  int64_t blocks;
-  if (FORM == WEIGHTS) blocks = weight_places((p.M + BM - 1) / BM * tiles_j) * p.groups;
-  else blocks = (p.offsets ? p.rows / BM + (p.rows < p.groups ? p.rows : p.groups) : (p.rows + BM - 1) / BM) * tiles_j;
-  if (blocks > INT32_MAX / 64) return fail(DYNB_ERR_UNSUPPORTED, "a product of more than 2^25 tiles");
-  hipLaunchKernelGGL((product_kernel<T, FORM, DUAL, BM, BN, WM, WN, NB, SOON, ACCESS, Ep>), dim3((unsigned)blocks, p.splits),
+  int64_t units;
+  if (FORM == WEIGHTS) {
+    const int64_t tiles = (p.M + BM - 1) / BM * tiles_j;
+    units = tiles < 1 << 24 ? (int64_t)weight_places((int)tiles) * p.groups * p.pairs : tiles * p.groups;
+  } else {
+    units = (p.offsets ? p.rows / BM + (p.rows < p.groups ? p.rows : p.groups) : (p.rows + BM - 1) / BM) * tiles_j;
+  }
+  if (units * p.splits > INT32_MAX / 64) return fail(DYNB_ERR_UNSUPPORTED, "a product of more than 2^25 tiles");
+  hipLaunchKernelGGL((product_kernel<T, FORM, DUAL, BM, BN, WM, WN, DEPTH, NB, SOON, ACCESS, Ep>), dim3((unsigned)units, p.splits),
                      dim3(WM * WN * 64), 0, st, p, s, ep);
   if (p.splits > 1) {
     const int64_t n = p.partial_rows * ((p.N + 7) / 8);
@@ -193,17 +236,20 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
   const bool singly = (FORM == WEIGHTS ? p.M : p.K) < 16 / (int)sizeof(T) || (FORM != ROWS_NT && p.N < 16 / (int)sizeof(T));
   if constexpr (FORM != WEIGHTS) {
     constexpr int WN = DUAL ? 2 : 4;
-    if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, SINGLY>(p, s, ep, st);
+    if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SINGLY>(p, s, ep, st);
     if (tiles == TILES_32)
-      return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, DIRECT>(p, s, ep, st)
-                    : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 4, 2, SHIFTED>(p, s, ep, st);
+      return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, DIRECT>(p, s, ep, st)
+                    : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SHIFTED>(p, s, ep, st);
   } else {
-    if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, SINGLY>(p, s, ep, st);
+    if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
   }
-  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, SHIFTED>(p, s, ep, st);
+  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SHIFTED>(p, s, ep, st);
   if constexpr (sizeof(T) == 2)
-    if (tiles == TILES_256) return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 2, 4, DIRECT>(p, s, ep, st);
-  return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 4, 2, DIRECT>(p, s, ep, st);
+    if (tiles == TILES_256) {
+      if constexpr (FORM == WEIGHTS) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);
+      else return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 8, 2, 4, DIRECT>(p, s, ep, st);
+    }
+  return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 4, 2, DIRECT>(p, s, ep, st);
 }
 
 }  // namespace

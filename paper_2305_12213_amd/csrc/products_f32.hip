@@ -14,8 +14,7 @@ template <> int launch_gated_grad<float>(const Product& p, Tiles tiles, const Ga
   return launch_as<float, ROWS_NT, false>(p, tiles, Segs{}, ep, stream);
 }
 template <> int launch_weights<float, float>(const Product& p, Tiles tiles, const Segs& s, const WeightOut<float>& ep, void* stream) {
-  return ep.out[1] ? launch_as<float, WEIGHTS, true>(p, tiles, s, ep, stream)
-                   : launch_as<float, WEIGHTS, false>(p, tiles, s, ep, stream);
+  return launch_as<float, WEIGHTS, false>(p, tiles, s, ep, stream);
 }
 
 }  // namespace dynb

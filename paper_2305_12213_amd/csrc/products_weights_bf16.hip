@@ -4,12 +4,10 @@
 namespace dynb {
 
 template <> int launch_weights<bf16, float>(const Product& p, Tiles tiles, const Segs& s, const WeightOut<float>& ep, void* stream) {
-  return ep.out[1] ? launch_as<bf16, WEIGHTS, true>(p, tiles, s, ep, stream)
-                   : launch_as<bf16, WEIGHTS, false>(p, tiles, s, ep, stream);
+  return launch_as<bf16, WEIGHTS, false>(p, tiles, s, ep, stream);
 }
 template <> int launch_weights<bf16, bf16>(const Product& p, Tiles tiles, const Segs& s, const WeightOut<bf16>& ep, void* stream) {
-  return ep.out[1] ? launch_as<bf16, WEIGHTS, true>(p, tiles, s, ep, stream)
-                   : launch_as<bf16, WEIGHTS, false>(p, tiles, s, ep, stream);
+  return launch_as<bf16, WEIGHTS, false>(p, tiles, s, ep, stream);
 }
 
 }  // namespace dynb

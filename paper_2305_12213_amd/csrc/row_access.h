@@ -103,10 +103,7 @@ __device__ inline void unpack(Raw<float> r, int n, float (&f)[GRANULE]) {
     f[4 + e] = __uint_as_float(r.b[e]);
   }
 }
-template <bool PAST = false> __device__ inline void store_part(bf16* p, int n, const float (&f)[GRANULE]) {
-  u32x4 a;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) a[e] = two_bf16(f[2 * e], f[2 * e + 1]);
+template <bool PAST = false> __device__ inline void store_packed(bf16* p, int n, const u32x4& a) {   // (8 elements as bits)
   if (n >= GRANULE) {
     store16<PAST>(p, a);
   } else if (n > 0) {
@@ -115,6 +112,12 @@ template <bool PAST = false> __device__ inline void store_part(bf16* p, int n, c
     if (n & 2) *(u32_any*)(p + (n & 4)) = low;
     if (n & 1) *(u16_any*)(p + n - 1) = (uint16_t)(n & 2 ? high : low);
   }
+}
+template <bool PAST = false> __device__ inline void store_part(bf16* p, int n, const float (&f)[GRANULE]) {
+  u32x4 a;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) a[e] = two_bf16(f[2 * e], f[2 * e + 1]);
+  store_packed<PAST>(p, n, a);
 }
 template <bool PAST = false> __device__ inline void store_part(float* p, int n, const float (&f)[GRANULE]) {
   u32x4 a, b;

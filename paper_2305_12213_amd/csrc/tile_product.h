@@ -29,12 +29,12 @@ enum Form { ROWS_NN, ROWS_NT, WEIGHTS };
 
 struct Product {
   const void* A[2];
-  const void* B[2];          // of two products that share A (dual), or of two whose sum is wanted (pairs = 2)
+  const void* B[2];          // of two products that share A (dual), or see pairs
   int64_t lda, ldb;          // elements
   int64_t b_stride;          // elements from one group's B to the next (ROWS_*)
   int M, N;                  // WEIGHTS: output rows; output columns of one product
   int K;                     // ROWS_*: reduction length of one pair
-  int pairs;
+  int pairs;                 // 2: both A and both B (ROWS_*); both B, each with a result of its own (WEIGHTS)
   int64_t rows;              // rows there are (ROWS_*: of A; WEIGHTS: of both)
   const int32_t* offsets;    // ROWS_*: device [groups + 1], or null: one group of all rows.  WEIGHTS: see `segments`
   const int32_t* segments;   // WEIGHTS: device [groups / workers][workers + 1]; null: `offsets`, or the launch's Segs
@@ -52,20 +52,19 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr uint32_t PARKED = 0x80000000u;   // an offset past the end of a buffer: the copy writes zeros
 
 // Workgroup -> place in the tile sequence: consecutive workgroups go round the 8 XCDs, each of which gets a run of it.
-__device__ inline int64_t run_of_xcd(int64_t pid, int64_t total) {
+__device__ inline int run_of_xcd(int pid, int total) {
   if (total < 16) return pid;
-  const int64_t per = total / 8, extra = total % 8, xcd = pid % 8;
+  const int per = total / 8, extra = total % 8, xcd = pid % 8;
   return xcd * per + (xcd < extra ? xcd : extra) + pid / 8;
 }
 // Gradients of weights: every group's tiles are spread over all XCDs (groups differ in their rows, so that whole groups to
 // an XCD left seven of them waiting: 32 groups of 16384 rows, 2048 x 2048, 545 us), in runs where there are enough of them: places
 // for a multiple of 8 tiles, some of them empty.
-constexpr int64_t XCD_RUNS = 32;
-__host__ __device__ inline int64_t weight_places(int64_t tiles) { return tiles < XCD_RUNS ? tiles : (tiles + 7) / 8 * 8; }
+constexpr int XCD_RUNS = 32;
+__host__ __device__ inline int weight_places(int tiles) { return tiles < XCD_RUNS ? tiles : (tiles + 7) / 8 * 8; }
 // Place -> tile, in bands of 8 tile rows, so that a run covers a compact rectangle.
-__device__ inline void tile_of_place(int64_t t, int tiles_i, int tiles_j, int& ti, int& tj) {
-  const int64_t bsz = (int64_t)8 * tiles_j;
-  const int b0 = (int)(t / bsz), r = (int)(t % bsz);
+__device__ inline void tile_of_place(int t, int tiles_i, int tiles_j, int& ti, int& tj) {
+  const int bsz = 8 * tiles_j, b0 = t / bsz, r = t % bsz;
   const int rows = tiles_i - b0 * 8 < 8 ? tiles_i - b0 * 8 : 8;
   ti = b0 * 8 + r % rows;
   tj = r / rows;
@@ -156,6 +155,12 @@ template <typename T> __device__ constexpr int turned_swizzle(int k, int pitch) 
   return sizeof(T) == 4 ? ((k >> 2) & 1) << 3 : pitch >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
 }
 
+// ... of granule g of row r of a tile whose rows run along the reduction, DEPTH granules each: 16 neighbouring rows, read at one
+// granule, fall into 64 different banks.
+template <int DEPTH> __device__ constexpr int along_swizzle(int r) {
+  return DEPTH == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+}
+
 // LDS written by some lanes of a wave and read by others.
 __device__ inline void patch_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -165,15 +170,15 @@ __device__ inline void patch_fence() {
 // A tile of BM x BN results, WM x WN waves.  DUAL: two products with BN / 2 columns each, which share A; a wave has the same
 // columns of both.  Ep: what is done with 8 neighbouring results of a row.  SOON: of a stage's copies, eighths that are
 // issued in the last step of the stage that releases its buffer, and in the first step of the next.
-template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int NB, int SOON, Access ACCESS, class Ep>
-__global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs segs, Ep ep) {
+template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
+__global__ __launch_bounds__(WM * WN * 64, WM * WN < 8 ? 2 : 1) void product_kernel(Product p, Segs segs, Ep ep) {
   constexpr bool TA = FORM == WEIGHTS, TB = FORM != ROWS_NT;
-  constexpr int G = 16 / sizeof(T), BK = 8 * G, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int G = 16 / sizeof(T), BK = DEPTH * G, STEPS = DEPTH / 2, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = ACCESS == DIRECT ? NB : 2;
-  constexpr int CA = BM / 8 / NW, CB = BN / 8 / NW, NC = CA + CB;   // copies of 1 KB per wave and stage
-  constexpr uint32_t STAGE = (BM + BN) * 128;
+  constexpr int CA = BM * DEPTH / 64 / NW, CB = BN * DEPTH / 64 / NW, NC = CA + CB;   // copies of 1 KB per wave and stage
+  constexpr uint32_t STAGE_A = BM * DEPTH * 16, STAGE = (BM + BN) * DEPTH * 16;
   constexpr int CW = 32 * TN, EP = CW + 4;                          // a wave's columns, row pitch of its patch
-  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole copies");
+  static_assert(BM * DEPTH % (64 * NW) == 0 && BN * DEPTH % (64 * NW) == 0 && (DEPTH == 4 || DEPTH == 8), "whole copies");
   static_assert(!DUAL || TN % 2 == 0, "a wave has columns of both products");
   constexpr uint32_t AREA = NBUF * STAGE > NW * 32 * EP * 4 ? NBUF * STAGE : NW * 32 * EP * 4;   // (the patches come last)
   static_assert(!TA || BM * (int)sizeof(T) >= 256, "a turned A has the wide swizzle");
@@ -183,18 +188,22 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0];
 
   // ---- which tile
-  int group, tj, depth;
+  int group, tj, depth, second = 0;
   int64_t i0, i_end, r0 = 0;              // output rows; WEIGHTS: first reduction row
   const int tiles_j = (p.N + BNS - 1) / BNS;
   if constexpr (FORM == WEIGHTS) {
     const int tiles_i = (p.M + BM - 1) / BM;
-    const int64_t tiles = (int64_t)tiles_i * tiles_j;
-    const int64_t places = weight_places(tiles);
-    int64_t place = blockIdx.x % places;
-    if (places >= XCD_RUNS) place = place % 8 * (places / 8) + place / 8;
+    const int tiles = tiles_i * tiles_j, places = weight_places(tiles);
+    int place = blockIdx.x % places, ti;
+    group = blockIdx.x / places;
+    second = group / p.groups;            // (pairs = 2: the other B, the other result)
+    group %= p.groups;
+    if (places >= XCD_RUNS) {
+      // (every XCD at other groups: tiles of one are stored while those of another are computed)
+      group = (group + place % 8 * p.groups / 8) % p.groups;
+      place = place % 8 * (places / 8) + place / 8;
+    }
     if (place >= tiles) return;
-    int ti;
-    group = (int)(blockIdx.x / places);
     tile_of_place(place, tiles_i, tiles_j, ti, tj);
     i0 = (int64_t)ti * BM;
     i_end = p.M;
@@ -206,8 +215,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     depth = uniform((int)(last - r0));
   } else {
     const int tiles_i = uniform(row_tiles(p, BM));
-    const int64_t total = (int64_t)tiles_i * tiles_j;
-    if (blockIdx.x >= total) return;
+    const int total = tiles_i * tiles_j;
+    if ((int)blockIdx.x >= total) return;
     int ti;
     tile_of_place(run_of_xcd(blockIdx.x, total), tiles_i, tiles_j, ti, tj);
     find_group(p, BM, ti, group, i0, i_end);
@@ -223,13 +232,13 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   const int part = (all + p.splits - 1) / p.splits;
   const int s_begin = p.splits > 1 ? min((int)blockIdx.y * part, all) : 0;
   const int s_end = p.splits > 1 ? min(s_begin + part, all) : all;
-  const int64_t stepA = TA ? (int64_t)BK * p.lda * sizeof(T) : 128, stepB = TB ? (int64_t)BK * p.ldb * sizeof(T) : 128;
+  const int64_t stepA = TA ? (int64_t)BK * p.lda * sizeof(T) : DEPTH * 16, stepB = TB ? (int64_t)BK * p.ldb * sizeof(T) : DEPTH * 16;
   // first byte of the tile in the operands of pair q
   auto base_a = [&](int q) {
     return (uint64_t)(uintptr_t)p.A[q] + (TA ? r0 * p.lda + i0 : i0 * p.lda) * sizeof(T);
   };
   auto base_b = [&](int q) {
-    return (uint64_t)(uintptr_t)p.B[q] +
+    return (uint64_t)(uintptr_t)p.B[FORM == WEIGHTS ? second : q] +
            (FORM == WEIGHTS ? r0 * p.ldb + j0 : group * p.b_stride + (TB ? (int64_t)j0 : j0 * p.ldb)) * sizeof(T);
   };
   int next = s_begin;                     // the stage that is copied next, where it stands, and what is left of the reduction
@@ -241,7 +250,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     if (DUAL) from[2] = base_b(1) + s * stepB;
     left = depth - s * BK;
   };
-  if (FORM != WEIGHTS && !DUAL && next >= per_pair && p.pairs == 2) enter(1, next - per_pair);
+  const int turn_at = FORM != WEIGHTS && !DUAL && p.pairs == 2 ? per_pair : -1;      // where the second pair begins
+  const uint64_t other[2] = {base_a(1), base_b(1)};
+  if (turn_at >= 0 && next >= turn_at) enter(1, next - turn_at);
   else enter(0, next);
   if (next >= s_end) left = 0;
   auto next_stage = [&]() {
@@ -250,8 +261,13 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     from[1] += stepB;
     if (DUAL) from[2] += stepB;
     left -= BK;
-    if (FORM != WEIGHTS && !DUAL && next == per_pair && p.pairs == 2) enter(1, 0);
-    if (next >= s_end) left = 0;          // (copies past the last stage keep the waits constant: zeros)
+    if (FORM != WEIGHTS && !DUAL) {       // (selects: no branch in the inner loop)
+      const bool turn = next == turn_at;
+      from[0] = turn ? other[0] : from[0];
+      from[1] = turn ? other[1] : from[1];
+      left = turn ? depth : left;
+    }
+    left = next >= s_end ? 0 : left;      // (copies past the last stage keep the waits constant: zeros)
   };
 
   // ---- copies: block c of a tile is 64 granules, lane l's lands in slot 64 c + l
@@ -261,7 +277,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
 #pragma unroll
   for (int u = 0; u < NC; ++u) {
     const bool isA = u < CA;
-    const int c = isA ? CA * wave + u : (CB * wave + u - CA) % (BNS / 8);      // (dual: block within its product's half)
+    const int c = isA ? CA * wave + u : (CB * wave + u - CA) % (BNS * DEPTH / 64);      // (dual: block within its product's half)
     const bool turned = isA ? TA : TB;
     const int64_t ld = isA ? p.lda : p.ldb, limit = isA ? i_end - i0 : p.N - j0;
     if (turned) {
@@ -271,15 +287,15 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
       need[u] = k;
       have[u] = (int)max((int64_t)0, min((int64_t)G, limit - g * G));
     } else {
-      const int r = 8 * c + (lane >> 3), g = (lane & 7) ^ swizzle128(r);
+      const int r = 64 / DEPTH * c + lane / DEPTH, g = lane % DEPTH ^ along_swizzle<DEPTH>(r);
       off[u] = r * ld * (int64_t)sizeof(T) + g * 16;
       need[u] = g * G;
       have[u] = r < limit ? G : 0;
     }
     if (ACCESS == DIRECT && have[u] == 0) need[u] = 0x7fffffff;
   }
-  auto source = [&](int u) { return u < CA ? 0 : DUAL && (CB * wave + u - CA) >= BNS / 8 ? 2 : 1; };
-  auto slot_of = [&](int u) { return u < CA ? (CA * wave + u) * 1024u : BM * 128u + (CB * wave + u - CA) * 1024u; };
+  auto source = [&](int u) { return u < CA ? 0 : DUAL && (CB * wave + u - CA) >= BNS * DEPTH / 64 ? 2 : 1; };
+  auto slot_of = [&](int u) { return u < CA ? (CA * wave + u) * 1024u : STAGE_A + (CB * wave + u - CA) * 1024u; };
   auto copy_one = [&](uint32_t buf, int u) {
     const uint64_t a = from[source(u)];
     const i32x4 r = {(int)(uint32_t)a, (int)((uint32_t)(a >> 32) & 0xffffu), (int)PARKED, BUFFER_32BIT};
@@ -300,9 +316,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     const int f = feat0 + 16 * (tg & 1) + 4 * (tr & 3), k = 8 * (tg >> 1) + (tr >> 2);
     return k * pitch + (((f >> 3) ^ turned_swizzle<T>(k, pitch)) * 16) + (f & 7) * 2;
   };
-  int at[4], atA[TA ? TM : 1], atB[TB ? TN : 1];
+  int at[STEPS], atA[TA ? TM : 1], atB[TB ? TN : 1];
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk) at[kk] = l31 * 128 + (((2 * kk + h) ^ swizzle128(l31)) * 16);
+  for (int kk = 0; kk < STEPS; ++kk) at[kk] = (l31 * DEPTH + ((2 * kk + h) ^ along_swizzle<DEPTH>(l31))) * 16;
   if constexpr (TA) {
 #pragma unroll
     for (int a = 0; a < TM; ++a) atA[a] = turned_at(wm * (BM / WM) + a * 32, PA);
@@ -311,7 +327,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   if constexpr (TB) {
 #pragma unroll
     for (int b = 0; b < TN; ++b)
-      atB[b] = BM * 128 + (DUAL && b >= TN / 2 ? BNS * 128 : 0) + turned_at(sub_column(b), PB);
+      atB[b] = STAGE_A + (DUAL && b >= TN / 2 ? BNS * DEPTH * 16 : 0) + turned_at(sub_column(b), PB);
   }
   auto turned_fragment = [&](uint32_t where, int kk, int pitch) {
     if constexpr (sizeof(T) == 4) {
@@ -330,11 +346,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   auto fetch_one = [&](uint32_t buf, int kk, int f) {
     if (f < TM) {
       if constexpr (TA) fa[kk & 1][f] = turned_fragment(buf + atA[f], kk, PA);
-      else fa[kk & 1][f] = *(const u32x4*)(base + buf + (wm * (BM / WM) + f * 32) * 128 + at[kk]);
+      else fa[kk & 1][f] = *(const u32x4*)(base + buf + (wm * (BM / WM) + f * 32) * DEPTH * 16 + at[kk]);
     } else {
       const int b = f - TM;
       if constexpr (TB) fb[kk & 1][b] = turned_fragment(buf + atB[b], kk, PB);
-      else fb[kk & 1][b] = *(const u32x4*)(base + buf + (BM + wn * CW + b * 32) * 128 + at[kk]);
+      else fb[kk & 1][b] = *(const u32x4*)(base + buf + (BM + wn * CW + b * 32) * DEPTH * 16 + at[kk]);
     }
   };
   static_assert(TB || !DUAL, "two products at a time: B turned");
@@ -360,8 +376,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
   constexpr int NM = TM * TN, NF = TM + TN;
 
   if constexpr (ACCESS == DIRECT) {
-    // copies behind step 3 of the stage before, 0, 1, 2: up to Q[1], Q[2], ...
-    constexpr int Q[5] = {0, SOON * NC / 8, 2 * SOON * NC / 8, SOON * NC / 4 + (NC - SOON * NC / 4) / 2, NC};
+    // copies behind the last step of the stage before, the first, the second ...: up to Q[1], Q[2], ...
+    constexpr int Q[5] = {0, SOON * NC / 8, STEPS == 2 ? NC : 2 * SOON * NC / 8, SOON * NC / 4 + (NC - SOON * NC / 4) / 2, NC};
 #pragma unroll 1
     for (int s = 0; s < NB - 1; ++s) {
 #pragma unroll
@@ -379,8 +395,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     for (int s = s_begin; s < s_end; ++s) {
       const uint32_t after = slot + STAGE == NB * STAGE ? 0 : slot + STAGE;
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        if (kk == 3) {
+      for (int kk = 0; kk < STEPS; ++kk) {
+        constexpr int LAST = STEPS - 1;
+        if (kk == LAST) {
           // this wave's copies of the next stage have landed (behind them, NB - 2 stages) and its reads of this one have
           // returned, and so for every wave
           asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NC) : "memory");
@@ -389,15 +406,16 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
           next_stage();
           __builtin_amdgcn_sched_barrier(0);
         }
+        const int step = (kk + 1) % STEPS;
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
           mma_one(kk & 1, m);
           __builtin_amdgcn_sched_barrier(0);
-          const int first = Q[(kk + 1) & 3], items = NF + Q[((kk + 1) & 3) + 1] - first;
+          const int first = Q[step], items = NF + Q[step + 1] - first;
 #pragma unroll
           for (int it = m * items / NM; it < (m + 1) * items / NM; ++it) {
-            if (it < NF) fetch_one(kk < 3 ? slot : after, (kk + 1) & 3, it);
-            else copy_one(kk < 3 ? fill : slot, first + it - NF);
+            if (it < NF) fetch_one(kk < LAST ? slot : after, step, it);
+            else copy_one(kk < LAST ? fill : slot, first + it - NF);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -449,7 +467,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
       next_stage();
       load_stage();
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
+      for (int kk = 0; kk < STEPS; ++kk) {
 #pragma unroll
         for (int f = 0; f < NF; ++f) fetch_one(slot, kk, f);
 #pragma unroll
@@ -462,14 +480,50 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
     }
   }
 
-  // ---- results: 32 rows at a time through a private patch, so that a lane has 8 neighbouring columns of a row
-  constexpr int LPR = BNS / WN / 8, RPI = 64 / LPR;
+  // ---- results, through a private patch of LDS, so that one access of the wave covers whole lines
+  if constexpr (CW == 64 && Ep::PACKS) {
+    if (p.splits == 1 && ep.packed()) {
+      // nothing but a rounding, done before the patches: all of the wave's results at once, 4 KB for 32 rows.  Granule g of row r
+      // is at g ^ (r / 2): two rows share a pass over the banks.
+      static_assert(NW * TM * 4096 <= AREA, "the patches fit in the ring");
+      char* const bits = (char*)&ring[0] + wave * TM * 4096;
+      const int c = lane & 7, product = DUAL ? c / 4 : 0;
+      const int col = j0 + wn * (BNS / WN) + (DUAL ? c % 4 : c) * 8, n = min(p.N - col, 8);
+#pragma unroll
+      for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *(u32x2*)(bits + a * 4096 + l31 * 128 + ((4 * b + q) ^ (l31 / 2 & 7)) * 16 + h * 8) =
+                u32x2{two_bf16(acc[a][b][4 * q], acc[a][b][4 * q + 1]), two_bf16(acc[a][b][4 * q + 2], acc[a][b][4 * q + 3])};
+      patch_fence();
+#pragma unroll
+      for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = u * 8 + lane / 8;
+          const int64_t i = i0 + wm * (BM / WM) + a * 32 + r;
+          const u32x4 v = *(const u32x4*)(bits + a * 4096 + r * 128 + (c ^ (r / 2 & 7)) * 16);
+          if (i < i_end) ep.put(group, i, col, n, v, FORM == WEIGHTS ? second : product);
+        }
+      return;
+    }
+  }
+  // 32 rows in fp32 at a time
+  constexpr int LPR = BNS / WN / 8, RPI = 64 / LPR, TIMES = 32 / RPI;
   float* const patch = (float*)&ring[0] + wave * 32 * EP;
   const int rrow = lane / LPR, rcol = (lane % LPR) * 8, hi4 = 4 * h;
   const int col = j0 + wn * (BNS / WN) + rcol, n = min(p.N - col, 8);
   const int wide = DUAL ? 2 * p.N : p.N;
 #pragma unroll
   for (int a = 0; a < TM; ++a) {
+    const int64_t first = i0 + wm * (BM / WM) + a * 32 + rrow;
+    typename Ep::Held held[TIMES];
+    if (p.splits == 1) {
+#pragma unroll
+      for (int t = 0; t < TIMES; ++t) held[t] = ep.ask(first + RPI * t, col, first + RPI * t < i_end ? n : 0);
+    }
 #pragma unroll
     for (int b = 0; b < TN; ++b)
 #pragma unroll
@@ -478,26 +532,31 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product p, Segs s
         *(f32x4*)&patch[l31 * EP + b * 32 + 8 * q + hi4] = o;
       }
     patch_fence();
-#pragma unroll Ep::ROWS_AT_ONCE
-    for (int t = 0; t < 32 / RPI; ++t) {
+#pragma unroll
+    for (int t = 0; t < TIMES; ++t) {
       const int r = rrow + RPI * t;
-      const int64_t i = i0 + wm * (BM / WM) + a * 32 + r;
+      const int64_t i = first + RPI * t;
       float v[8], w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = patch[r * EP + rcol + e];
-        w[e] = DUAL ? patch[r * EP + CW / 2 + rcol + e] : 0.f;
+      for (int g = 0; g < 2; ++g) {
+        const f32x4 x = *(const f32x4*)&patch[r * EP + rcol + 4 * g], y = *(const f32x4*)&patch[r * EP + (DUAL ? CW / 2 : 0) + rcol + 4 * g];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[4 * g + e] = x[e];
+          w[4 * g + e] = DUAL ? y[e] : 0.f;
+        }
       }
       if (i >= i_end || n <= 0) continue;
       if (p.splits > 1) {
-        float* const to = p.partial + ((int64_t)blockIdx.y * p.partial_rows + (FORM == WEIGHTS ? (int64_t)group * p.M : 0) + i) * wide + col;
+        float* const to = p.partial + ((int64_t)blockIdx.y * p.partial_rows + (FORM == WEIGHTS ? (int64_t)(second * p.groups + group) * p.M : 0) + i) * wide + col;
         store_part(to, n, v);
         if (DUAL) store_part(to + p.N, n, w);
       } else {
-        ep.row(group, i, col, n, v, w);
+        ep.row(FORM == WEIGHTS ? second * p.groups + group : group, i, col, n, v, w, held[t]);
       }
     }
     patch_fence();
+    __builtin_amdgcn_sched_barrier(0);      // (or registers run out)
   }
 }
 
@@ -527,8 +586,8 @@ __global__ __launch_bounds__(256) void joined_kernel(Product p, Ep ep) {
       for (int e = 0; e < 8; ++e) w[e] += x[e];
     }
   }
-  if (FORM == WEIGHTS) ep.row((int)(row / p.M), row % p.M, col, n, v, w);
-  else ep.row(0, row, col, n, v, w);
+  const int64_t i = FORM == WEIGHTS ? row % p.M : row;
+  ep.row(FORM == WEIGHTS ? (int)(row / p.M) : 0, i, col, n, v, w, ep.ask(i, col, n));
 }
 
 }  // namespace
