@@ -37,12 +37,15 @@ ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduct
   const int64_t stages = tiles_of(reduction, dtype == DYNB_F32 ? 32 : 64);
   const int64_t each = rows / std::min<int64_t>(groups, std::max<int64_t>(rows, 1));
   if (each <= 48) {                        // (memory bounds these: parts only until every compute unit has work)
-    const int64_t tiles = row_tiles_of(rows, groups, 32) * tiles_of(N, 128 / half);
-    return {TILES_32, (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(tiles, 1), stages / 4, (int64_t)16}))};
+    const int64_t row_tiles = row_tiles_of(rows, groups, 32);
+    const bool narrow = !dual && row_tiles * tiles_of(N, 128) < 256;
+    const int64_t tiles = row_tiles * tiles_of(N, narrow ? 64 : 128 / half);
+    const int n = (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(tiles, 1), stages / 4, (int64_t)16}));
+    return {narrow ? TILES_32X64 : TILES_32, narrow && tiles >= 192 ? 1 : n};
   }
   if (dtype == DYNB_BF16 && each >= 160 && row_tiles_of(rows, groups, 256) * tiles_of(N, 256 / half) >= 192) return {TILES_256, 1};
   const bool whole = whole_granules(dtype, N) && whole_granules(dtype, reduction);
-  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), whole ? 256 : 512, stages, dtype == DYNB_F32 ? 1 : 4)};
+  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), whole ? 256 : 512, stages, dtype == DYNB_F32 ? 3 : 4)};
 }
 ProductPlan plan_weights(int dtype, int64_t rows, int groups, int M, int N, int matrices) {
   const int64_t stages = tiles_of(rows / groups, dtype == DYNB_F32 ? 32 : 64);

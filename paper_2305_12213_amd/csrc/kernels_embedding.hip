@@ -71,9 +71,7 @@ __global__ __launch_bounds__(THREADS) void digit_count_kernel(SortPass p, Segs s
   for (int e = threadIdx.x; e < 1 << p.bits; e += THREADS) p.counts[((int64_t)blockIdx.x << p.bits) + e] = count[e];
 }
 
-__global__ __launch_bounds__(THREADS) void digit_place_kernel(SortPass p, Segs s) {
-  __shared__ int place[WAVES][DIGITS];    // counts, then the next places
-  __shared__ int wave_total[DIGITS / 64];
+__device__ inline void place_digits(const SortPass& p, const Segs& s, int (*place)[DIGITS], int* wave_total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, digits = 1 << p.bits, mask = digits - 1;
   for (int i = threadIdx.x; i < WAVES * DIGITS; i += THREADS) ((int*)place)[i] = 0;
   __syncthreads();
@@ -139,12 +137,31 @@ __global__ __launch_bounds__(THREADS) void digit_place_kernel(SortPass p, Segs s
   }
 }
 
+// (one workgroup alone goes on with `more` further passes, from what it wrote to where it read)
+__global__ __launch_bounds__(THREADS) void digit_place_kernel(SortPass p, Segs s, int more, int all_bits) {
+  __shared__ int place[WAVES][DIGITS];    // counts, then the next places
+  __shared__ int wave_total[DIGITS / 64];
+  for (;; --more) {
+    place_digits(p, s, place, wave_total);
+    if (more == 0) return;
+    __syncthreads();
+    int32_t *const keys = p.keys_out, *const tokens = p.tokens_out;
+    p.keys_out = const_cast<int32_t*>(p.keys);
+    p.tokens_out = const_cast<int32_t*>(p.tokens);
+    p.keys = keys;
+    p.tokens = tokens;
+    p.ids = nullptr;
+    p.shift += p.bits;
+    p.bits = min(p.bits, all_bits - p.shift);
+  }
+}
+
 // ---- the sums ----------------------------------------------------------------------------------------------------
 // A token that appears often (a padding token may be all of them) would be one wave's long chain: the sorted tokens are cut
-// into chunks of 32, and one whose tokens are all the same is summed beforehand.  A run is then its first tokens up to a
+// into chunks of 16, and one whose tokens are all the same is summed beforehand.  A run is then its first tokens up to a
 // chunk's end, its whole chunks, and the rest.  A lane has four neighbouring columns twice, 256 apart, so that every access of a
 // wave is one stretch of memory; the numbers of 64 tokens are loaded at once and AHEAD of their rows are asked for together.
-constexpr int CHUNK = 32, QUAD = 4, HALF = 64 * QUAD, SPAN = 2 * HALF;   // SPAN: columns of a wave
+constexpr int CHUNK = 16, QUAD = 4, HALF = 64 * QUAD, SPAN = 2 * HALF;   // SPAN: columns of a wave
 constexpr int AHEAD = 8;
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -154,7 +171,7 @@ struct TableGrad {
   float* chunk_sums;                             // [chunks][cols]
   float* dtable; int64_t worker_stride;
   int64_t n; int vocabulary;
-  int cols, workers;
+  int cols, workers, per;
   float scale;
 };
 
@@ -257,18 +274,21 @@ __device__ inline int64_t keys_below(const int32_t* keys, int64_t n, int key) {
   return low;
 }
 
-// PER neighbouring rows of the gradients to a wave.
-constexpr int PER = 8;
+// p.per neighbouring rows of the gradients to a wave: MOST_PER, which share a search, or fewer where waves are few (the
+// first rows of a vocabulary are often those of its most frequent tokens).
+constexpr int MOST_PER = 8, ENOUGH_WAVES = 8192;
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
   const int lane = threadIdx.x & 63, all = p.workers * p.vocabulary;
-  const int first = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * PER;
+  // (the spans of a row are neighbours in time too: in launches of their own they would each meet a part of the memory channels)
+  const int spans = (p.cols + SPAN - 1) / SPAN;
+  const int first = (blockIdx.x / spans * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * p.per;
   if (first >= all) return;
-  const int c = blockIdx.y * SPAN + lane * QUAD, n0 = p.cols - c, n1 = n0 - HALF;
+  const int c = blockIdx.x % spans * SPAN + lane * QUAD, n0 = p.cols - c, n1 = n0 - HALF;
   int64_t at = keys_below(p.keys, p.n, first);
   int mine = at + lane < p.n ? p.keys[at + lane] : 0x7fffffff;      // the 64 keys from `at` on
   int worker = first / p.vocabulary, id = first % p.vocabulary;
-  for (int row = first; row < first + PER && row < all; ++row) {
+  for (int row = first; row < first + p.per && row < all; ++row) {
     // this row's run begins at `begin`, the first of the 64 that is not below it
     const int less = __builtin_popcountll(__ballot(mine < row)), same = __builtin_popcountll(__ballot(mine == row));
     int64_t begin = at + less, end = begin + same;
@@ -283,7 +303,7 @@ __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
       const int64_t chunk = (begin + CHUNK - 1) / CHUNK, last = end / CHUNK;
       if (chunk < last) {
         add_rows<T>(p, begin, chunk * CHUNK, c, s);
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t q = chunk; q < last; ++q) {
           const float* const from = p.chunk_sums + q * p.cols + c;
           s[0] += values(load_quad(from, n0));
@@ -335,14 +355,16 @@ Parts parts_of(const dynb_embedding_desc* d) {
   return w;
 }
 
+int64_t table_grad_blocks(const TableGrad& p) {
+  return ((int64_t)p.workers * p.vocabulary + 4 * p.per - 1) / (4 * p.per) * ((p.cols + SPAN - 1) / SPAN);
+}
+
 template <typename T>
 void launch_table_grad(const TableGrad& p, hipStream_t st) {
-  const unsigned spans = (p.cols + SPAN - 1) / SPAN;
   if (p.n >= CHUNK)
-    hipLaunchKernelGGL(chunk_rows_kernel<T>, dim3((unsigned)((p.n / CHUNK + 3) / 4), spans), dim3(256), 0, st, p);
-  const int64_t rows = (int64_t)p.workers * p.vocabulary;
-  const dim3 grid((unsigned)((rows + 4 * PER - 1) / (4 * PER)), spans);
-  if (past_caches(4.0 * rows * p.cols)) hipLaunchKernelGGL((table_grad_kernel<T, true>), grid, dim3(256), 0, st, p);
+    hipLaunchKernelGGL(chunk_rows_kernel<T>, dim3((unsigned)((p.n / CHUNK + 3) / 4), (p.cols + SPAN - 1) / SPAN), dim3(256), 0, st, p);
+  const dim3 grid((unsigned)table_grad_blocks(p));
+  if (past_caches(4.0 * p.workers * p.vocabulary * p.cols)) hipLaunchKernelGGL((table_grad_kernel<T, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((table_grad_kernel<T, false>), grid, dim3(256), 0, st, p);
 }
 
@@ -393,6 +415,10 @@ extern "C" int dynb_embedding_backward(const dynb_embedding_desc* d, const int32
   const Parts w = parts_of(d);
   if (w.end && (!workspace || workspace_bytes < (size_t)w.end || off_by(workspace, 16)))
     return fail(DYNB_ERR_BADARG, "embedding_backward: workspace is null, too small or not 16-byte aligned");
+  const int per = (int)std::max<int64_t>(1, std::min<int64_t>(MOST_PER, K * d->vocabulary / ENOUGH_WAVES));
+  TableGrad grad = {nullptr, nullptr, dout, d->ld_dout ? d->ld_dout : d->cols, (float*)((char*)workspace + w.sums), dtable,
+                       worker_stride, d->tokens, (int)d->vocabulary, d->cols, K, per, d->scale};
+  if (table_grad_blocks(grad) > 1 << 23) return fail(DYNB_ERR_UNSUPPORTED, "embedding_backward: more than 2^37 elements");
   const hipStream_t st = (hipStream_t)stream;
   Timed t(KC_EMBEDDING, stream, (double)d->tokens * d->cols,
           4.0 * K * d->vocabulary * d->cols + (double)size * d->tokens * d->cols);
@@ -410,14 +436,19 @@ extern "C" int dynb_embedding_backward(const dynb_embedding_desc* d, const int32
     for (int i = 0; i < passes; ++i) {
       SortPass p = {i ? nullptr : ids, keys[cur], tokens[cur], keys[1 - cur], tokens[1 - cur], d->tokens, per, d->vocabulary,
                     i * per_pass, std::min(per_pass, bits - i * per_pass), (int32_t*)(ws + w.counts)};
-      if (grid.x > 1) hipLaunchKernelGGL(digit_count_kernel, grid, dim3(THREADS), 0, st, p, s);
-      hipLaunchKernelGGL(digit_place_kernel, grid, dim3(THREADS), 0, st, p, s);
+      if (grid.x == 1) {
+        hipLaunchKernelGGL(digit_place_kernel, grid, dim3(THREADS), 0, st, p, s, passes - 1, bits);
+        cur = passes & 1;
+        break;
+      }
+      hipLaunchKernelGGL(digit_count_kernel, grid, dim3(THREADS), 0, st, p, s);
+      hipLaunchKernelGGL(digit_place_kernel, grid, dim3(THREADS), 0, st, p, s, 0, bits);
       cur = 1 - cur;
     }
   }
-  const TableGrad p = {keys[cur], tokens[cur], dout, d->ld_dout ? d->ld_dout : d->cols, (float*)(ws + w.sums), dtable,
-                       worker_stride, d->tokens, (int)d->vocabulary, d->cols, K, d->scale};
-  if (d->dtype == DYNB_F32) launch_table_grad<float>(p, st);
-  else launch_table_grad<bf16>(p, st);
+  grad.keys = keys[cur];
+  grad.tokens = tokens[cur];
+  if (d->dtype == DYNB_F32) launch_table_grad<float>(grad, st);
+  else launch_table_grad<bf16>(grad, st);
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "embedding_backward launch failed");
 }

@@ -179,7 +179,7 @@ template <typename O> struct WeightOut {
 };
 
 // How a product is cut into tiles and its reduction into parts.
-enum Tiles { TILES_256, TILES_128, TILES_32 };
+enum Tiles { TILES_256, TILES_128, TILES_32, TILES_32X64 };
 struct ProductPlan {
   Tiles tiles;
   int splits;
@@ -237,13 +237,17 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
   if constexpr (FORM != WEIGHTS) {
     constexpr int WN = DUAL ? 2 : 4;
     if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SINGLY>(p, s, ep, st);
-    if (tiles == TILES_32)
+    if constexpr (!DUAL)
+      if (tiles == TILES_32X64 && direct) return launch_tiles<T, FORM, DUAL, 32, 64, 1, 2, 8, 6, 2, DIRECT>(p, s, ep, st);
+    if (tiles == TILES_32 || tiles == TILES_32X64)
       return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, DIRECT>(p, s, ep, st)
                     : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SHIFTED>(p, s, ep, st);
   } else {
     if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
   }
-  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SHIFTED>(p, s, ep, st);
+  // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends)
+  constexpr bool SHORT = FORM == WEIGHTS;
+  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
   if constexpr (sizeof(T) == 2)
     if (tiles == TILES_256) {
       if constexpr (FORM == WEIGHTS) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);

@@ -171,7 +171,7 @@ __device__ inline void patch_fence() {
 // columns of both.  Ep: what is done with 8 neighbouring results of a row.  SOON: of a stage's copies, eighths that are
 // issued in the last step of the stage that releases its buffer, and in the first step of the next.
 template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
-__global__ __launch_bounds__(WM * WN * 64, WM * WN < 8 ? 2 : 1) void product_kernel(Product p, Segs segs, Ep ep) {
+__global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED && BM == 128 ? 3 : 2) void product_kernel(Product p, Segs segs, Ep ep) {
   constexpr bool TA = FORM == WEIGHTS, TB = FORM != ROWS_NT;
   constexpr int G = 16 / sizeof(T), BK = DEPTH * G, STEPS = DEPTH / 2, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = ACCESS == DIRECT ? NB : 2;
