@@ -17,14 +17,16 @@ int64_t row_tiles_of(int64_t rows, int groups, int size) {
 }
 // (sizes alone: rows of other pitches or places take the same parts)
 bool whole_granules(int dtype, int64_t n) { return n % (dtype == DYNB_F32 ? 4 : 8) == 0; }
-// Into how many parts a reduction of `stages` is divided: workgroups run `slots` at a time, each for its share of the stages;
-// a part more is worth it where that time falls by `worth` stages at least (what writing and joining it takes).
-int parts(int64_t tiles, int64_t slots, int64_t stages, int64_t worth) {
+// Into how many parts a reduction of `stages` is divided.  A workgroup takes about its share of the stages; where two share a
+// compute unit (paired) they take twice as long, one alone there 1.5 times.  `worth`: what a part costs to be written and
+// joined, in halves of a stage.
+int parts(int64_t tiles, int64_t stages, bool paired, int worth) {
   int best = 1;
-  int64_t least = tiles_of(tiles, slots) * stages;
-  for (int n = 2; n <= 16; ++n) {
-    const int64_t cost = tiles_of(tiles * n, slots) * tiles_of(stages, n) + worth * n;
-    if (cost < least) {
+  int64_t least = 0;
+  for (int n = 1; n <= 16; ++n) {
+    const int64_t blocks = tiles * n, share = tiles_of(stages, n);
+    const int64_t cost = (paired ? blocks <= 256 ? 3 : 4 * tiles_of(blocks, 512) : 2 * tiles_of(blocks, 256)) * share + (n > 1 ? worth * n : 0);
+    if (n == 1 || cost < least) {
       least = cost;
       best = n;
     }
@@ -44,14 +46,14 @@ ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduct
     return {narrow ? TILES_32X64 : TILES_32, narrow && tiles >= 192 ? 1 : n};
   }
   if (dtype == DYNB_BF16 && each >= 160 && row_tiles_of(rows, groups, 256) * tiles_of(N, 256 / half) >= 192) return {TILES_256, 1};
-  const bool whole = whole_granules(dtype, N) && whole_granules(dtype, reduction);
-  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), whole ? 256 : 512, stages, dtype == DYNB_F32 ? 3 : 4)};
+  const bool paired = dtype == DYNB_F32 || !whole_granules(dtype, N) || !whole_granules(dtype, reduction);
+  return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), stages, paired, dtype == DYNB_F32 ? groups == 1 ? 6 : 12 : 8)};
 }
 ProductPlan plan_weights(int dtype, int64_t rows, int groups, int M, int N, int matrices) {
   const int64_t stages = tiles_of(rows / groups, dtype == DYNB_F32 ? 32 : 64);
   if (dtype == DYNB_BF16 && tiles_of(M, 256) * tiles_of(N, 256) * groups * matrices >= 192) return {TILES_256, 1};
-  const bool whole = whole_granules(dtype, N) && whole_granules(dtype, M);
-  return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128) * groups * matrices, whole ? 256 : 512, stages, dtype == DYNB_F32 ? 2 : 6)};
+  const bool paired = dtype == DYNB_F32 || !whole_granules(dtype, N) || !whole_granules(dtype, M);
+  return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128) * groups * matrices, stages, paired, dtype == DYNB_F32 ? 6 : 12)};
 }
 // Bytes of Product::partial (0 where the plan has one part).
 size_t partial_bytes(const ProductPlan& plan, int64_t rows, int64_t columns) {

@@ -246,14 +246,17 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
     if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
   }
   // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends)
-  constexpr bool SHORT = FORM == WEIGHTS;
-  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
-  if constexpr (sizeof(T) == 2)
-    if (tiles == TILES_256) {
-      if constexpr (FORM == WEIGHTS) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);
-      else return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 8, 2, 4, DIRECT>(p, s, ep, st);
-    }
-  return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 4, 2, DIRECT>(p, s, ep, st);
+  constexpr bool SHORT = FORM == WEIGHTS, F32 = sizeof(T) == 4;
+  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT || F32 ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
+  // fp32: two workgroups of four waves on a compute unit, one's matrix instructions in the other's barriers (4096^3 1120 us with one
+  // of eight waves and a ring of four stages, 1057)
+  if constexpr (F32) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, st);
+  else if (tiles == TILES_256) {
+    if constexpr (FORM == WEIGHTS) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);
+    else return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 8, 2, 4, DIRECT>(p, s, ep, st);
+  } else {
+    return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 4, 2, DIRECT>(p, s, ep, st);
+  }
 }
 
 }  // namespace

@@ -171,7 +171,7 @@ __device__ inline void patch_fence() {
 // columns of both.  Ep: what is done with 8 neighbouring results of a row.  SOON: of a stage's copies, eighths that are
 // issued in the last step of the stage that releases its buffer, and in the first step of the next.
 template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
-__global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED && BM == 128 ? 3 : 2) void product_kernel(Product p, Segs segs, Ep ep) {
+__global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED && DEPTH == 4 ? 3 : 2) void product_kernel(Product p, Segs segs, Ep ep) {
   constexpr bool TA = FORM == WEIGHTS, TB = FORM != ROWS_NT;
   constexpr int G = 16 / sizeof(T), BK = DEPTH * G, STEPS = DEPTH / 2, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = ACCESS == DIRECT ? NB : 2;
@@ -362,18 +362,20 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
   // (B's columns as the instruction's rows: a lane then has 4 neighbouring columns of the output)
+  // (fp32: the four instructions of a step go round the tiles, so that neighbours do not wait for each other's sums)
+  constexpr int NM = TM * TN * (sizeof(T) == 4 ? 4 : 1), NF = TM + TN;
   auto mma_one = [&](int set, int m) {
-    const int a = m % TM, b = m / TM;
+    const int a = m % TM, b = m / TM % TN;
     if constexpr (sizeof(T) == 4) {
+      const int j = m / (TM * TN);
       const f32x4 x = __builtin_bit_cast(f32x4, fa[set][a]), w = __builtin_bit_cast(f32x4, fb[set][b]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j], x[j], acc[a][b], 0, 0, 0);
+      acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j], x[j], acc[a][b], 0, 0, 0);
     } else {
       acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[set][b]),
                                                           __builtin_bit_cast(bf16x8, fa[set][a]), acc[a][b], 0, 0, 0);
     }
   };
-  constexpr int NM = TM * TN, NF = TM + TN;
+
 
   if constexpr (ACCESS == DIRECT) {
     // copies behind the last step of the stage before, the first, the second ...: up to Q[1], Q[2], ...
