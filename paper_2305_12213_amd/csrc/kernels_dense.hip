@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256) void chunk_sum_kernel(const float* sums, int c
 }
 
 RowChunks bias_chunks(const Segs& s) {     // (a hundred or two of them, so that a column's sum is no long chain)
-  return make_row_chunks(s, (int)std::max<int64_t>(64, round_up(s.off[s.K] / 128, 16)));
+  return make_row_chunks(s, (int)std::max<int64_t>(32, round_up(s.off[s.K] / 128, 16)));
 }
 
 // ---- dense layers -----------------------------------------------------------------------------------------------

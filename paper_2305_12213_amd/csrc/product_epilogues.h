@@ -58,6 +58,7 @@ template <typename T> struct Curve {
 
 // out = act(v + bias) + residual; what the activation is taken of can be kept
 template <typename T> struct LinearOut {
+  static constexpr bool HEAVY = false;
   static constexpr bool PACKS = sizeof(T) == 2;
   const float* bias;
   const T* residual; int64_t ld_residual;
@@ -102,6 +103,7 @@ struct Nothing {};
 
 // hidden = act(gate) * up, from the sums before they are rounded
 template <typename T> struct GatedOut {
+  static constexpr bool HEAVY = false;
   static constexpr bool PACKS = false;
   T* gate; T* up;             // or null: not kept
   int64_t ld_kept;
@@ -122,6 +124,7 @@ template <typename T> struct GatedOut {
 
 // from v = gradient of hidden: dgate = v up act'(gate), dup = v act(gate), and hidden once more
 template <typename T> struct GatedGrad {
+  static constexpr bool HEAVY = true;
   static constexpr bool PACKS = false;
   const T* gate; const T* up;
   int64_t ld_kept;
@@ -155,6 +158,7 @@ template <typename T> struct GatedGrad {
 // gradients of one or two weights: group e * workers + k is worker k's of matrix e; the second weight's groups follow (row) or are
 // named by `product` (put)
 template <typename O> struct WeightOut {
+  static constexpr bool HEAVY = false;
   static constexpr bool PACKS = sizeof(O) == 2;
   O* out[2];
   int64_t worker_stride, matrix;
@@ -252,7 +256,9 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
   // of eight waves and a ring of four stages, 1057)
   if constexpr (F32) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, st);
   else if (tiles == TILES_256) {
-    if constexpr (FORM == WEIGHTS) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);
+    // (results that come with more bytes than operations: two workgroups to a compute unit, one computes while the other stores.
+    // 16384 rows of 8 experts, 2048 x 2048: gradients of hidden 281 us on 256 x 256 tiles, 267; other rows 4 to 20 % slower)
+    if constexpr (FORM == WEIGHTS || Ep::HEAVY) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);
     else return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 8, 2, 4, DIRECT>(p, s, ep, st);
   } else {
     return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 4, 2, DIRECT>(p, s, ep, st);

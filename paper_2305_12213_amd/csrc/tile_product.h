@@ -87,38 +87,59 @@ __device__ inline int sum_upto(int v) {
   }
   return v;
 }
-// Tiles of BM rows over all groups; and the group that has tile `ti` of them, its rows from that tile on.
-__device__ inline int row_tiles(const Product& p, int BM) {
-  if (!p.offsets) return (int)((p.rows + BM - 1) / BM);
-  int total = 0;
-  for (int e0 = 0; e0 < p.groups; e0 += 64) {
-    const int e = e0 + (threadIdx.x & 63);
-    int64_t first = 0, last = 0;
-    if (e < p.groups) group_rows(p.offsets + e, p.rows, first, last);
-    total += __builtin_amdgcn_readlane(sum_upto((int)((last - first + BM - 1) / BM)), 63);
-  }
-  return total;
+// The groups' tiles of BM rows: how many there are, and which group has tile `ti`, with its rows from that tile on.  The bounds of
+// up to 256 groups are asked for at once and stay in registers, those of more are read again in the search.
+struct RowTiles {
+  static constexpr int HELD = 4;
+  int first[HELD], last[HELD];            // rows of group 64 c + lane
+  int total;
+};
+__device__ inline void rows_of(const Product& p, int e, int& first, int& last) {
+  int64_t f = 0, l = 0;
+  if (e < p.groups) group_rows(p.offsets + e, p.rows, f, l);
+  first = (int)f;
+  last = (int)l;
 }
-__device__ inline void find_group(const Product& p, int BM, int ti, int& group, int64_t& first, int64_t& last) {
+__device__ inline void count_tiles(const Product& p, int BM, RowTiles& t) {
+  t.total = (int)((p.rows + BM - 1) / BM);
+  if (!p.offsets) return;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < RowTiles::HELD; ++c) rows_of(p, 64 * c + lane, t.first[c], t.last[c]);
+  int mine = 0;
+#pragma unroll
+  for (int c = 0; c < RowTiles::HELD; ++c) mine += (t.last[c] - t.first[c] + BM - 1) / BM;
+  for (int e = 64 * RowTiles::HELD + lane; e < p.groups; e += 64) {
+    int f, l;
+    rows_of(p, e, f, l);
+    mine += (l - f + BM - 1) / BM;
+  }
+  t.total = __builtin_amdgcn_readlane(sum_upto(mine), 63);
+}
+__device__ inline void find_group(const Product& p, int BM, const RowTiles& t, int ti, int& group, int64_t& first, int64_t& last) {
   group = 0;
   first = (int64_t)ti * BM;
   last = p.rows;
   if (!p.offsets) return;
   int before = 0;
-  for (int e0 = 0; e0 < p.groups; e0 += 64) {
-    const int e = e0 + (threadIdx.x & 63);
-    int64_t f = 0, l = 0;
-    if (e < p.groups) group_rows(p.offsets + e, p.rows, f, l);
-    const int mine = (int)((l - f + BM - 1) / BM), upto = before + sum_upto(mine);
+  auto look = [&](int c, int f, int l) {
+    const int mine = (l - f + BM - 1) / BM, upto = before + sum_upto(mine);
     const uint64_t has = __ballot(ti >= upto - mine && ti < upto);
-    if (has) {
-      const int lane = __builtin_ctzll(has);
-      group = e0 + lane;
-      first = __builtin_amdgcn_readlane((int)f, lane) + (int64_t)(ti - __builtin_amdgcn_readlane(upto - mine, lane)) * BM;
-      last = __builtin_amdgcn_readlane((int)l, lane);
-      return;
-    }
     before = __builtin_amdgcn_readlane(upto, 63);
+    if (!has) return false;
+    const int lane = __builtin_ctzll(has);
+    group = 64 * c + lane;
+    first = __builtin_amdgcn_readlane(f, lane) + (int64_t)(ti - __builtin_amdgcn_readlane(upto - mine, lane)) * BM;
+    last = __builtin_amdgcn_readlane(l, lane);
+    return true;
+  };
+#pragma unroll
+  for (int c = 0; c < RowTiles::HELD; ++c)
+    if (64 * c < p.groups && look(c, t.first[c], t.last[c])) return;
+  for (int c = RowTiles::HELD; 64 * c < p.groups; ++c) {
+    int f, l;
+    rows_of(p, 64 * c + (threadIdx.x & 63), f, l);
+    if (look(c, f, l)) return;
   }
   last = first = 0;       // (not reached: ti is below the number of tiles)
 }
@@ -214,12 +235,14 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
     r0 = uniform((int)r0);
     depth = uniform((int)(last - r0));
   } else {
-    const int tiles_i = uniform(row_tiles(p, BM));
+    RowTiles rt;
+    count_tiles(p, BM, rt);
+    const int tiles_i = uniform(rt.total);
     const int total = tiles_i * tiles_j;
     if ((int)blockIdx.x >= total) return;
     int ti;
     tile_of_place(run_of_xcd(blockIdx.x, total), tiles_i, tiles_j, ti, tj);
-    find_group(p, BM, ti, group, i0, i_end);
+    find_group(p, BM, rt, ti, group, i0, i_end);
     group = uniform(group);
     i0 = uniform((int)i0);
     i_end = uniform((int)i_end);
