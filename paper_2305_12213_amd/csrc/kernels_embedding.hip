@@ -247,16 +247,18 @@ __device__ inline void add_rows(const TableGrad& p, int64_t from, int64_t to, in
 
 template <typename T>
 __global__ __launch_bounds__(256) void chunk_rows_kernel(TableGrad p) {
-  const int64_t chunk = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = chunk * CHUNK;
-  if (first + CHUNK > p.n) return;
-  const int key = p.keys[first];
-  if (key != p.keys[first + CHUNK - 1] || key >= p.workers * p.vocabulary) return;
   const int c = blockIdx.y * SPAN + (threadIdx.x & 63) * QUAD;
-  f32x4_any s[2] = {};
-  add_rows<T>(p, first, first + CHUNK, c, s);
-  float* const to = p.chunk_sums + chunk * p.cols + c;
-  store_quad<false>(to, p.cols - c, s[0]);
-  store_quad<false>(to + HALF, p.cols - c - HALF, s[1]);
+  for (int64_t chunk = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); (chunk + 1) * CHUNK <= p.n;
+       chunk += (int64_t)gridDim.x * 4) {
+    const int64_t first = chunk * CHUNK;
+    const int key = p.keys[first];
+    if (key != p.keys[first + CHUNK - 1] || key >= p.workers * p.vocabulary) continue;
+    f32x4_any s[2] = {};
+    add_rows<T>(p, first, first + CHUNK, c, s);
+    float* const to = p.chunk_sums + chunk * p.cols + c;
+    store_quad<false>(to, p.cols - c, s[0]);
+    store_quad<false>(to + HALF, p.cols - c - HALF, s[1]);
+  }
 }
 
 // Sorted tokens with keys below `key` (the whole wave takes part): 64 places at a time.
@@ -362,7 +364,7 @@ int64_t table_grad_blocks(const TableGrad& p) {
 template <typename T>
 void launch_table_grad(const TableGrad& p, hipStream_t st) {
   if (p.n >= CHUNK)
-    hipLaunchKernelGGL(chunk_rows_kernel<T>, dim3((unsigned)((p.n / CHUNK + 3) / 4), (p.cols + SPAN - 1) / SPAN), dim3(256), 0, st, p);
+    hipLaunchKernelGGL(chunk_rows_kernel<T>, dim3((unsigned)std::min<int64_t>((p.n / CHUNK + 3) / 4, 1 << 20), (p.cols + SPAN - 1) / SPAN), dim3(256), 0, st, p);
   const dim3 grid((unsigned)table_grad_blocks(p));
   if (past_caches(4.0 * p.workers * p.vocabulary * p.cols)) hipLaunchKernelGGL((table_grad_kernel<T, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((table_grad_kernel<T, false>), grid, dim3(256), 0, st, p);

@@ -218,11 +218,11 @@ int launch_tiles(const Product& p, const Segs& s, const Ep& ep, hipStream_t st) 
   int64_t units;
   if (FORM == WEIGHTS) {
     const int64_t tiles = (p.M + BM - 1) / BM * tiles_j;
-    units = tiles < 1 << 24 ? (int64_t)weight_places((int)tiles) * p.groups * p.pairs : tiles * p.groups;
+    units = (tiles < 1 << 24 ? weight_places((int)tiles) : tiles) * (int64_t)p.groups * p.pairs;
   } else {
     units = (p.offsets ? p.rows / BM + (p.rows < p.groups ? p.rows : p.groups) : (p.rows + BM - 1) / BM) * tiles_j;
   }
-  if (units * p.splits > INT32_MAX / 64) return fail(DYNB_ERR_UNSUPPORTED, "a product of more than 2^25 tiles");
+  if (units * p.splits > INT32_MAX / (WM * WN * 64)) return fail(DYNB_ERR_UNSUPPORTED, "a product of more than 2^22 tiles");
   hipLaunchKernelGGL((product_kernel<T, FORM, DUAL, BM, BN, WM, WN, DEPTH, NB, SOON, ACCESS, Ep>), dim3((unsigned)units, p.splits),
                      dim3(WM * WN * 64), 0, st, p, s, ep);
   if (p.splits > 1) {

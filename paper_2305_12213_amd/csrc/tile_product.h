@@ -100,6 +100,7 @@ __device__ inline void rows_of(const Product& p, int e, int& first, int& last) {
   first = (int)f;
   last = (int)l;
 }
+__device__ inline int tiles_between(int first, int last, int BM) { return (int)(((uint32_t)(last - first) + BM - 1) / BM); }
 __device__ inline void count_tiles(const Product& p, int BM, RowTiles& t) {
   t.total = (int)((p.rows + BM - 1) / BM);
   if (!p.offsets) return;
@@ -108,11 +109,11 @@ __device__ inline void count_tiles(const Product& p, int BM, RowTiles& t) {
   for (int c = 0; c < RowTiles::HELD; ++c) rows_of(p, 64 * c + lane, t.first[c], t.last[c]);
   int mine = 0;
 #pragma unroll
-  for (int c = 0; c < RowTiles::HELD; ++c) mine += (t.last[c] - t.first[c] + BM - 1) / BM;
+  for (int c = 0; c < RowTiles::HELD; ++c) mine += tiles_between(t.first[c], t.last[c], BM);
   for (int e = 64 * RowTiles::HELD + lane; e < p.groups; e += 64) {
     int f, l;
     rows_of(p, e, f, l);
-    mine += (l - f + BM - 1) / BM;
+    mine += tiles_between(f, l, BM);
   }
   t.total = __builtin_amdgcn_readlane(sum_upto(mine), 63);
 }
@@ -123,7 +124,7 @@ __device__ inline void find_group(const Product& p, int BM, const RowTiles& t, i
   if (!p.offsets) return;
   int before = 0;
   auto look = [&](int c, int f, int l) {
-    const int mine = (l - f + BM - 1) / BM, upto = before + sum_upto(mine);
+    const int mine = tiles_between(f, l, BM), upto = before + sum_upto(mine);
     const uint64_t has = __ballot(ti >= upto - mine && ti < upto);
     before = __builtin_amdgcn_readlane(upto, 63);
     if (!has) return false;
@@ -251,7 +252,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
   const int j0 = tj * BNS;
 
   // ---- the stages of this workgroup
-  const int per_pair = (depth + BK - 1) / BK, all = FORM == WEIGHTS ? per_pair : per_pair * p.pairs;
+  const int per_pair = (int)(((uint32_t)depth + BK - 1) / BK), all = FORM == WEIGHTS ? per_pair : per_pair * p.pairs;
   const int part = (all + p.splits - 1) / p.splits;
   const int s_begin = p.splits > 1 ? min((int)blockIdx.y * part, all) : 0;
   const int s_end = p.splits > 1 ? min(s_begin + part, all) : all;

@@ -96,6 +96,26 @@ def test_large_vocabulary(dynb):
     assert bool(((got.reshape(-1, H).double() - want).abs() <= (most + 2) * EPS * size).all())
 
 
+def test_table_of_more_than_32_bits(dynb):
+    """2^21 tokens of 1100 columns: the last rows are 2^31 elements from the first."""
+    import torch
+    V, H = (1 << 21) + 3, 1100
+    table = torch.empty(V, H, device="cuda", dtype=torch.bfloat16)
+    ids = torch.tensor([V - 1, 0, V // 2, V - 1, V, 7], device="cuda", dtype=torch.int32)
+    some = ids[[0, 1, 2, 5]].long()
+    table[some] = torch.randn(4, H, device="cuda").to(torch.bfloat16)
+    out = torch.empty(6, H, device="cuda", dtype=torch.bfloat16)
+    d = binding.embedding_desc("bf16", H, V, 6)
+    binding.embedding(d, ids, table, out)
+    assert torch.equal(out[[0, 1, 2, 3, 5]], table[ids[[0, 1, 2, 3, 5]].long()]) and not bool(out[4].any())
+    g = torch.empty(V * H, device="cuda")
+    n = binding.embedding_backward_workspace_bytes(d, 1)
+    binding.embedding_backward(d, [6], ids, out, g, V * H, torch.empty(n + 16, device="cuda", dtype=torch.uint8), n)
+    g = g.view(V, H)
+    assert torch.equal(g[V - 1], out[0].float() + out[3].float()) and torch.equal(g[V // 2], out[2].float())
+    assert int((g != 0).any(1).sum()) == 4
+
+
 def test_no_tokens(dynb):
     import torch
     d = binding.embedding_desc("bf16", 16, 10, 0)

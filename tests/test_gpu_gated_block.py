@@ -184,6 +184,51 @@ def test_many_groups_of_weights(dynb):
     Case(rng.integers(0, 60, (12, 9)), 512, 264, "bf16").check_backward("f32")
 
 
+def test_more_experts_than_registers_hold(dynb):
+    """The bounds of 256 groups stay in registers, the others' are read again."""
+    rng = np.random.default_rng(6)
+    counts = np.where(rng.random((700, 2)) < 0.5, 0, rng.integers(0, 5, (700, 2)))
+    counts[-1] = 3, 0
+    Case(counts, 64, 40, "bf16", behind=2).check_forward()
+    Case(counts, 40, 24, "f32").check_backward()
+
+
+def test_weights_of_more_than_32_bits(dynb):
+    """600 experts of 2048 x 2048: the last ones are 2^31 elements and 2^32 bytes from the first."""
+    import torch
+    E, H = 600, 2048
+    w = torch.empty(E, H, H, device="cuda", dtype=torch.bfloat16)
+    g = torch.Generator("cuda").manual_seed(4)
+    used = {0: 3, 512: 2, 599: 4}
+    for e in used:
+        w[e] = torch.randn(H, H, generator=g, device="cuda") / H ** 0.5
+    counts = np.array([used.get(e, 0) for e in range(E)])
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    x = torch.randn(9, H, generator=g, device="cuda").to(torch.bfloat16)
+    d = binding.gated_block_desc("bf16", H, H, E, 9, "silu", "bf16")
+    y, gate, up = (torch.empty_like(x) for _ in range(3))
+    n = binding.gated_block_workspace_bytes(d)
+    dev = torch.from_numpy(offsets).cuda()
+    binding.gated_block(d, dev, x, w, w, w, gate, up, y, room(n), n)
+    dy, dx = torch.randn(9, H, generator=g, device="cuda").to(torch.bfloat16), torch.empty_like(x)
+    dg, du, dw = (torch.empty_like(w) for _ in range(3))
+    n = binding.gated_block_backward_workspace_bytes(d, 1)
+    binding.gated_block_backward(d, 1, dev, None, x, w, w, w, gate, up, dy, dx, dg, du, dw, 0, room(n), n)
+    torch.cuda.synchronize()
+    for e in used:
+        r = slice(offsets[e], offsets[e + 1])
+        hw, hx, hy = host(w[e]), host(x[r]), host(dy[r])
+        a = hx @ hw
+        assert_within(host(gate)[r], a, stored("bf16", a, summed(hx, hw)), "gate")
+        s = op.activate("silu", host(gate)[r]) * host(up)[r]
+        off = stored("bf16", s, 32 * EPS * np.abs(s))
+        assert_within(host(dw[e]), s.T @ hy, stored("bf16", s.T @ hy, summed(s.T, hy, off.T)), "w_down's gradient")
+        dup = (hy @ hw.T) * op.activate("silu", host(gate)[r])
+        off = stored("bf16", dup, summed(hy, hw.T) * np.abs(op.activate("silu", host(gate)[r])) + 32 * EPS * np.abs(dup))
+        assert_within(host(du[e]), hx.T @ dup, stored("bf16", hx.T @ dup, summed(hx.T, dup) + 1.01 * (np.abs(hx.T) @ off)), "w_up's gradient")
+    assert not any(bool(t[e].any()) for t in (dg, du, dw) for e in (1, 598))
+
+
 def test_gradients_are_differences(dynb):
     """fp32, against differences of the call itself: a loss <y, c> whose central difference of step 2^-6 has an error of about
     its square times the third derivative, 3e-4 of the gradients' size, and 4e-5 of rounding."""

@@ -111,6 +111,29 @@ def test_large_tiles(dynb):
     check([500, 200], 2048, 1600, 8, 0, "bf16", "none", True, False, "f32")
 
 
+def test_pitches_and_rows_of_more_than_32_bits(dynb):
+    """Rows 2^22 elements apart (256 of them are 2^31 bytes), 600 of them: the last ones are 2^32 bytes from the first."""
+    import torch
+    rows, n, m, ld = 600, 72, 40, 1 << 22
+    g = torch.Generator("cuda").manual_seed(2)
+    wide = torch.empty(rows * ld, device="cuda", dtype=torch.bfloat16)
+    x = wide.view(rows, ld)[:, :n]
+    x.copy_(torch.randn(rows, n, generator=g, device="cuda"))
+    near, w = x.contiguous(), torch.randn(n, m, generator=g, device="cuda").to(torch.bfloat16)
+    dout = torch.randn(rows, m, generator=g, device="cuda").to(torch.bfloat16)
+    found = []
+    for t, pitch in ((x, ld), (near, 0)):
+        d = binding.linear_desc("bf16", n, m, "none", "f32", ld_x=pitch)
+        out, dw = torch.empty(rows, m, device="cuda", dtype=torch.bfloat16), torch.empty(n * m, device="cuda")
+        nb = max(binding.linear_workspace_bytes(d, rows), binding.linear_backward_workspace_bytes(d, [rows]))
+        binding.linear(d, rows, t, w, None, None, None, out, room(nb), nb)
+        binding.linear_backward(d, [rows], t, w, None, dout, None, dw, 0, None, 0, room(nb), nb)
+        torch.cuda.synchronize()
+        hx, hw, hd = host(near), host(w), host(dout)
+        assert_within(host(out), hx @ hw, stored("bf16", hx @ hw, summed(hx, hw)), "out")
+        assert_within(host(dw).reshape(n, m), hx.T @ hd, summed(hx.T, hd) + EPS * np.abs(hx.T @ hd), "dw")
+
+
 def test_no_rows_and_idle_workers(dynb):
     import torch
     d = binding.linear_desc("bf16", 40, 24, "silu")
