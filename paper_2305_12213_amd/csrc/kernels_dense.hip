@@ -34,6 +34,22 @@ int parts(int64_t tiles, int64_t stages, bool paired, int worth) {
   return best;
 }
 
+// The same for fp32 on 64 x 64 tiles (64 x 128 for two products): matrix instructions bound several workgroups on a compute unit
+// together, fewer than three leave them waiting.
+int parts_of_small(int64_t tiles, int64_t stages) {
+  int best = 1;
+  int64_t least = 0;
+  for (int n = 1; n <= 8; ++n) {
+    const int64_t cost = std::max<int64_t>(tiles_of(tiles * n, 256), 3) * tiles_of(stages, n) + (n > 1 ? 6 * n : 0);
+    if (n == 1 || cost < least) {
+      least = cost;
+      best = n;
+    }
+  }
+  return best;
+}
+constexpr int64_t FEW_TILES = 768;         // 128 x 128 tiles, three rounds of them: below, smaller ones
+
 ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduction, bool dual) {
   const int half = dual ? 2 : 1;
   const int64_t stages = tiles_of(reduction, dtype == DYNB_F32 ? 32 : 64);
@@ -46,12 +62,16 @@ ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduct
     return {narrow ? TILES_32X64 : TILES_32, narrow && tiles >= 192 ? 1 : n};
   }
   if (dtype == DYNB_BF16 && each >= 160 && row_tiles_of(rows, groups, 256) * tiles_of(N, 256 / half) >= 192) return {TILES_256, 1};
+  if (dtype == DYNB_F32 && row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half) < FEW_TILES)
+    return {TILES_64, parts_of_small(row_tiles_of(rows, groups, 64) * tiles_of(N, 64), stages)};
   const bool paired = dtype == DYNB_F32 || !whole_granules(dtype, N) || !whole_granules(dtype, reduction);
   return {TILES_128, parts(row_tiles_of(rows, groups, 128) * tiles_of(N, 128 / half), stages, paired, dtype == DYNB_F32 ? groups == 1 ? 6 : 12 : 8)};
 }
 ProductPlan plan_weights(int dtype, int64_t rows, int groups, int M, int N, int matrices) {
   const int64_t stages = tiles_of(rows / groups, dtype == DYNB_F32 ? 32 : 64);
   if (dtype == DYNB_BF16 && tiles_of(M, 256) * tiles_of(N, 256) * groups * matrices >= 192) return {TILES_256, 1};
+  if (dtype == DYNB_F32 && (stages < 8 || tiles_of(M, 128) * tiles_of(N, 128) * groups * matrices < FEW_TILES))
+    return {TILES_64, parts_of_small(tiles_of(M, 64) * tiles_of(N, 64) * groups * matrices, stages)};
   const bool paired = dtype == DYNB_F32 || !whole_granules(dtype, N) || !whole_granules(dtype, M);
   return {TILES_128, parts(tiles_of(M, 128) * tiles_of(N, 128) * groups * matrices, stages, paired, dtype == DYNB_F32 ? 6 : 12)};
 }

@@ -183,7 +183,7 @@ template <typename O> struct WeightOut {
 };
 
 // How a product is cut into tiles and its reduction into parts.
-enum Tiles { TILES_256, TILES_128, TILES_32, TILES_32X64 };
+enum Tiles { TILES_256, TILES_128, TILES_64, TILES_32, TILES_32X64 };
 struct ProductPlan {
   Tiles tiles;
   int splits;
@@ -248,6 +248,14 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
                     : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SHIFTED>(p, s, ep, st);
   } else {
     if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
+  }
+  // fp32 with few tiles: smaller ones, of which several share a compute unit and leave less of it idle at the end
+  if constexpr (sizeof(T) == 4) {
+    if (tiles == TILES_64) {
+      constexpr int BN = DUAL ? 128 : 64;
+      if (direct) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, st);
+      return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, FORM == WEIGHTS ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
+    }
   }
   // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends)
   constexpr bool SHORT = FORM == WEIGHTS, F32 = sizeof(T) == 4;
