@@ -303,7 +303,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
   };
 
   // ---- copies: block c of a tile is 64 granules, lane l's lands in slot 64 c + l
-  int64_t off[NC];                        // bytes from the stage's first (DIRECT: below 2^31, or PARKED)
+  int64_t off[NC];                        // bytes from the stage's first (DIRECT: below 2^31)
   int need[NC];                           // a granule is there where more than this is left of the reduction
   int have[NC];                           // ... and so many of its elements (turned operands; the others: G or 0)
 #pragma unroll
@@ -393,8 +393,8 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
     for (int b = 0; b < TN; ++b)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.f;
-  // (B's columns as the instruction's rows: a lane then has 4 neighbouring columns of the output)
-  // (fp32: the four instructions of a step go round the tiles, so that neighbours do not wait for each other's sums)
+  // B's columns as the instruction's rows: a lane then has 4 neighbouring columns of the output.  fp32: the four instructions of a
+  // step go round the tiles, so that neighbours do not wait for each other's sums.
   constexpr int NM = TM * TN * (sizeof(T) == 4 ? 4 : 1), NF = TM + TN;
   auto mma_one = [&](int set, int m) {
     const int a = m % TM, b = m / TM % TN;
@@ -407,7 +407,6 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
                                                           __builtin_bit_cast(bf16x8, fa[set][a]), acc[a][b], 0, 0, 0);
     }
   };
-
 
   if constexpr (ACCESS == DIRECT) {
     // copies behind the last step of the stage before, the first, the second ...: up to Q[1], Q[2], ...

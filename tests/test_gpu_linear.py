@@ -144,14 +144,15 @@ def test_no_rows_and_idle_workers(dynb):
     assert not bool(dw.isnan().any() | dw.any()) and not bool(db.isnan().any() | db.any())
 
 
-def test_extreme_pre_activations(dynb):
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_extreme_pre_activations(dynb, dtype):
     """Where exponentials overflow or vanish, activations and slopes have their limits; a NaN stays one."""
     import torch
-    v = torch.tensor([-3e38, -1e4, -200.0, -90.0, 90.0, 200.0, 1e4, 3e38, float("nan")], device="cuda")
-    x, one = v[:, None].contiguous(), torch.ones(1, 1, device="cuda")
+    v = torch.tensor([-3e38, -1e4, -200.0, -90.0, 90.0, 200.0, 1e4, 3e38, float("nan")], device="cuda").to(torch_type(dtype))
+    x, one = v[:, None].contiguous(), torch.ones(1, 1, device="cuda", dtype=v.dtype)
     for act in ("relu", "silu", "gelu"):
-        d = binding.linear_desc("f32", 1, 1, act)
-        out, pre, dx = (torch.empty(9, 1, device="cuda") for _ in range(3))
+        d = binding.linear_desc(dtype, 1, 1, act)
+        out, pre, dx = (torch.empty(9, 1, device="cuda", dtype=v.dtype) for _ in range(3))
         binding.linear(d, 9, x, one, None, None, pre, out, room(64), binding.linear_workspace_bytes(d, 9))
         n = binding.linear_backward_workspace_bytes(d, [9])
         binding.linear_backward(d, [9], x, one, pre, torch.ones_like(x), dx, None, 0, None, 0, room(n), n)
