@@ -49,6 +49,13 @@ __device__ inline void async_copy_1k_buffer(i32x4 rsrc, uint32_t voffset, uint32
                : "memory", "m0");
 }
 
+// The same 4 bytes at a time, from any multiple of 4: lane l's land at LDS byte address lds_base + 4 * l.
+__device__ inline void async_copy_256_buffer(i32x4 rsrc, uint32_t voffset, uint32_t lds_base) {
+  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_base);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(base), "v"(voffset), "s"(rsrc)
+               : "memory", "m0");
+}
+
 // n - 128, or 0: the bytes left of a buffer whose base moves on by a line.  (Assembly: the compiler takes a
 // vector instruction for a saturating difference, and a resource has to stay in scalar registers.)
 __device__ inline uint32_t less_128(uint32_t n) {

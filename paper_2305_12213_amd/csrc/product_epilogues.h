@@ -203,13 +203,13 @@ namespace {
 template <typename T> bool whole_granules(int64_t v) { return v % (16 / (int)sizeof(T)) == 0; }
 inline bool near(int64_t ld, size_t size) { return ld * (int64_t)size * 256 < ((int64_t)1 << 31); }
 
-// Whether all of an operand's copies are whole granules at multiples of 16 bytes, and 32-bit offsets reach a stage.
+// Whether 32-bit offsets reach a stage, and whether all of an operand's copies are whole granules at multiples of 16 bytes.
+template <typename T> bool copies_ok(const Product& p) { return near(p.lda, sizeof(T)) && near(p.ldb, sizeof(T)); }
 template <typename T> bool direct_ok(const Product& p, int form) {
   for (int q = 0; q < 2; ++q)
     if (off_by(p.A[q], 16) || off_by(p.B[q], 16)) return false;
-  return whole_granules<T>(p.lda) && whole_granules<T>(p.ldb) && whole_granules<T>(p.b_stride) && near(p.lda, sizeof(T)) &&
-         near(p.ldb, sizeof(T)) && (form == ROWS_NT || whole_granules<T>(p.N)) &&
-         (form == WEIGHTS ? whole_granules<T>(p.M) : whole_granules<T>(p.K));
+  return copies_ok<T>(p) && whole_granules<T>(p.lda) && whole_granules<T>(p.ldb) && whole_granules<T>(p.b_stride) &&
+         (form == ROWS_NT || whole_granules<T>(p.N)) && (form == WEIGHTS ? whole_granules<T>(p.M) : whole_granules<T>(p.K));
 }
 
 template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
@@ -252,16 +252,20 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
     if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
   }
   // fp32 with few tiles: smaller ones, of which several share a compute unit and leave less of it idle at the end (gradients of
-  // 1531 tokens, 3 of 11 experts, 777 x 301: 294 -> 252 us)
+  // 1531 tokens, 3 of 11 experts, 777 x 301: 294 -> 252 us).  Odd widths: single copies, of shorter stages for gradients of weights,
+  // took 1 to 12 % less than shifted granules in all of 30 products but one (odd sizes from 768 to 8192; 1531 x 2050 x 777 72 -> 64
+  // us, weights of 8192 tokens, 2047 x 2049 704 -> 627, but of 16 workers 786 -> 812)
   if constexpr (sizeof(T) == 4) {
+    constexpr int DEPTH = FORM == WEIGHTS ? 4 : 8;
     if (tiles == TILES_64) {
       constexpr int BN = DUAL ? 128 : 64;
       if (direct) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, st);
-      return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, FORM == WEIGHTS ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
+      if (copies_ok<T>(p)) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, DEPTH, 2, 4, SINGLES>(p, s, ep, st);
     }
+    if (!direct && copies_ok<T>(p)) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, DEPTH, 2, 4, SINGLES>(p, s, ep, st);
   }
   // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends; 77 groups of
-  // 48 rows, 777 x 301 in fp32, two weights: 119 -> 104 us)
+  // 48 rows, 777 x 301, shifted granules of fp32, two weights: 119 -> 104 us)
   constexpr bool SHORT = FORM == WEIGHTS, F32 = sizeof(T) == 4;
   if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT || F32 ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
   // fp32: two workgroups of four waves on a compute unit, one's matrix instructions in the other's barriers (4096^3 1120 us with one

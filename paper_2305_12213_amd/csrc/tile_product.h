@@ -12,7 +12,8 @@
 //
 // Copies go from memory straight to LDS, a ring of NB stages, a step's fragments are fetched one step ahead, and
 // fetches and copies stand between the matrix instructions (as in the dense layers' products).  Rows that are no
-// multiple of 16 bytes pass through registers, which can fill up partial granules with zeros.
+// multiple of 16 bytes are copied element by element in fp32, and in bf16 pass through registers, which can fill up
+// partial granules with zeros.
 //
 // What bounds it.  Long reductions in bf16: the matrix instructions at the clock that they leave (8192^3 915 us, 1200 TFLOP/s; the clock
 // falls to 1.8 GHz).  Short ones (gradients of weights from a few hundred rows): the stores, which all workgroups come to
@@ -153,10 +154,11 @@ __device__ inline void find_group(const Product& p, int BM, const RowTiles& t, i
   last = first = 0;       // (not reached: ti is below the number of tiles)
 }
 
-// How an operand's granules reach LDS.  DIRECT: copied, all of them whole and at multiples of 16 bytes.  SHIFTED: through
-// registers; the last granule of a row is loaded so that it ends with the row and shifted into its place, which needs rows of
-// a granule at least and keeps every load unconditional and in flight until it is stored.  SINGLY: element by element.
-enum Access { DIRECT, SHIFTED, SINGLY };
+// How an operand's granules reach LDS.  DIRECT: copied, all of them whole and at multiples of 16 bytes.  SINGLES (fp32): copied
+// element by element, four times the copies, wherever rows begin and end.  SHIFTED: through registers; the last granule of a row is
+// loaded so that it ends with the row and shifted into its place, which needs rows of a granule at least and keeps every load
+// unconditional and in flight until it is stored.  SINGLY: element by element.
+enum Access { DIRECT, SHIFTED, SINGLY, SINGLES };
 
 template <typename T> __device__ inline u32x4 load_singly(const T* p, int n) {
   u32x4 r = {0, 0, 0, 0};
@@ -201,10 +203,11 @@ __device__ inline void patch_fence() {
 // columns of both.  Ep: what is done with 8 neighbouring results of a row.  SOON: of a stage's copies, eighths that are
 // issued in the last step of the stage that releases its buffer, and in the first step of the next.
 template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
-__global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED && DEPTH == 4 ? 3 : 2) void product_kernel(Product p, Segs segs, Ep ep) {
+__global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : (ACCESS == SHIFTED || ACCESS == SINGLES) && DEPTH == 4 ? 3 : 2) void product_kernel(Product p, Segs segs, Ep ep) {
   constexpr bool TA = FORM == WEIGHTS, TB = FORM != ROWS_NT;
   constexpr int G = 16 / sizeof(T), BK = DEPTH * G, STEPS = DEPTH / 2, NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = ACCESS == DIRECT ? NB : 2;
+  constexpr bool COPIED = ACCESS == DIRECT || ACCESS == SINGLES;
+  constexpr int BNS = DUAL ? BN / 2 : BN, NBUF = COPIED ? NB : 2;
   constexpr int CA = BM * DEPTH / 64 / NW, CB = BN * DEPTH / 64 / NW, NC = CA + CB;   // copies of 1 KB per wave and stage
   constexpr uint32_t STAGE_A = BM * DEPTH * 16, STAGE = (BM + BN) * DEPTH * 16;
   constexpr int CW = 32 * TN, EP = CW + 4;                          // a wave's columns, row pitch of its patch
@@ -302,36 +305,44 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
     left = next >= s_end ? 0 : left;      // (copies past the last stage keep the waits constant: zeros)
   };
 
-  // ---- copies: block c of a tile is 64 granules, lane l's lands in slot 64 c + l
-  int64_t off[NC];                        // bytes from the stage's first (DIRECT: below 2^31)
-  int need[NC];                           // a granule is there where more than this is left of the reduction
-  int have[NC];                           // ... and so many of its elements (turned operands; the others: G or 0)
+  // ---- copies: block c of a tile is 64 granules, lane l's lands in slot 64 c + l.  SINGLES: a quarter of a block at a time, an
+  // element per lane.
+  constexpr int PER = ACCESS == SINGLES ? 4 : 1, NP = NC * PER, WIDTH = ACCESS == SINGLES ? 1 : G;   // WIDTH: elements of a lane
+  static_assert(ACCESS != SINGLES || sizeof(T) == 4, "copies of 4 bytes");
+  int64_t off[NP];                        // bytes from the stage's first (copied: below 2^31)
+  int need[NP];                           // a granule (SINGLES: an element) is there where more than this is left of the reduction
+  int have[NP];                           // ... and so many of its elements (turned operands; the others: all or none)
 #pragma unroll
-  for (int u = 0; u < NC; ++u) {
+  for (int v = 0; v < NP; ++v) {
+    const int u = v / PER;
     const bool isA = u < CA;
     const int c = isA ? CA * wave + u : (CB * wave + u - CA) % (BNS * DEPTH / 64);      // (dual: block within its product's half)
+    const int in = PER == 1 ? lane : 16 * (v % PER) + lane / 4, e = PER == 1 ? 0 : lane % 4;   // granule of the block, element of it
     const bool turned = isA ? TA : TB;
     const int64_t ld = isA ? p.lda : p.ldb, limit = isA ? i_end - i0 : p.N - j0;
     if (turned) {
-      const int row = isA ? BM / G : BNS / G, s = 64 * c + lane, k = s / row;
+      const int row = isA ? BM / G : BNS / G, s = 64 * c + in, k = s / row;
       const int g = (s % row) ^ turned_swizzle<T>(k, row * 16);
-      off[u] = k * ld * (int64_t)sizeof(T) + g * 16;
-      need[u] = k;
-      have[u] = (int)max((int64_t)0, min((int64_t)G, limit - g * G));
+      off[v] = k * ld * (int64_t)sizeof(T) + g * 16 + e * 4;
+      need[v] = k;
+      have[v] = (int)max((int64_t)0, min((int64_t)WIDTH, limit - g * G - e));
     } else {
-      const int r = 64 / DEPTH * c + lane / DEPTH, g = lane % DEPTH ^ along_swizzle<DEPTH>(r);
-      off[u] = r * ld * (int64_t)sizeof(T) + g * 16;
-      need[u] = g * G;
-      have[u] = r < limit ? G : 0;
+      const int r = 64 / DEPTH * c + in / DEPTH, g = in % DEPTH ^ along_swizzle<DEPTH>(r);
+      off[v] = r * ld * (int64_t)sizeof(T) + g * 16 + e * 4;
+      need[v] = g * G + e;
+      have[v] = r < limit ? WIDTH : 0;
     }
-    if (ACCESS == DIRECT && have[u] == 0) need[u] = 0x7fffffff;
+    if (COPIED && have[v] == 0) need[v] = 0x7fffffff;
   }
   auto source = [&](int u) { return u < CA ? 0 : DUAL && (CB * wave + u - CA) >= BNS * DEPTH / 64 ? 2 : 1; };
   auto slot_of = [&](int u) { return u < CA ? (CA * wave + u) * 1024u : STAGE_A + (CB * wave + u - CA) * 1024u; };
-  auto copy_one = [&](uint32_t buf, int u) {
+  auto copy_one = [&](uint32_t buf, int v) {
+    const int u = v / PER;
     const uint64_t a = from[source(u)];
     const i32x4 r = {(int)(uint32_t)a, (int)((uint32_t)(a >> 32) & 0xffffu), (int)PARKED, BUFFER_32BIT};
-    async_copy_1k_buffer(r, need[u] < left ? (uint32_t)off[u] : PARKED, lds + buf + slot_of(u));
+    const uint32_t at = need[v] < left ? (uint32_t)off[v] : PARKED, to = lds + buf + slot_of(u);
+    if constexpr (ACCESS == SINGLES) async_copy_256_buffer(r, at, to + v % PER * 256);
+    else async_copy_1k_buffer(r, at, to);
   };
 
   // ---- fragments: element (row or column l31, k of half h) of two granules
@@ -408,18 +419,19 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
     }
   };
 
-  if constexpr (ACCESS == DIRECT) {
+  if constexpr (COPIED) {
     // copies behind the last step of the stage before, the first, the second ...: up to Q[1], Q[2], ...
-    constexpr int Q[5] = {0, SOON * NC / 8, STEPS == 2 ? NC : 2 * SOON * NC / 8, SOON * NC / 4 + (NC - SOON * NC / 4) / 2, NC};
+    constexpr int Q[5] = {0, SOON * NP / 8, STEPS == 2 ? NP : 2 * SOON * NP / 8, SOON * NP / 4 + (NP - SOON * NP / 4) / 2, NP};
+    static_assert((NB - 2) * NP + Q[1] <= 63, "the counter of copies");
 #pragma unroll 1
     for (int s = 0; s < NB - 1; ++s) {
 #pragma unroll
-      for (int u = 0; u < NC; ++u) copy_one(s * STAGE, u);
+      for (int u = 0; u < NP; ++u) copy_one(s * STAGE, u);
       next_stage();
     }
 #pragma unroll
     for (int u = 0; u < Q[1]; ++u) copy_one((NB - 1) * STAGE, u);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NC + Q[1]) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NP + Q[1]) : "memory");
     __syncthreads();
 #pragma unroll
     for (int f = 0; f < NF; ++f) fetch_one(0, 0, f);
@@ -433,7 +445,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : ACCESS == SHIFTED 
         if (kk == LAST) {
           // this wave's copies of the next stage have landed (behind them, NB - 2 stages) and its reads of this one have
           // returned, and so for every wave
-          asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NC) : "memory");
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NP) : "memory");
           __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0), the other counters at their limits
           __syncthreads();
           next_stage();

@@ -179,6 +179,18 @@ def test_large_tiles(dynb, case):
     Case(**LARGE[case]).check_backward("bf16")
 
 
+@pytest.mark.parametrize("odd", [0, 1])
+def test_large_tiles_of_fp32(dynb, odd):
+    """768 tiles of 128 x 128 and more: of hidden, of the rows, of the weights."""
+    counts = [[700, 1000], [0, 0], [900, 401]]
+    pad = 4 - 3 * odd
+    Case(counts, 40 + odd, 2440 + odd, "f32", behind=3, pad=pad).check_forward()
+    Case(counts, 4100 + odd, 40 - odd, "f32", behind=3, pad=pad).check_forward()
+    Case(counts, 40 + odd, 3900 + odd, "f32", behind=3, pad=pad).check_backward()
+    Case(counts, 3900 + odd, 40 - odd, "f32", behind=3, pad=pad, act="gelu").check_backward()
+    Case(counts, 1500 - odd, 1300 + odd, "f32", behind=3, pad=pad).check_backward()
+
+
 def test_many_groups_of_weights(dynb):
     rng = np.random.default_rng(5)
     Case(rng.integers(0, 60, (12, 9)), 512, 264, "bf16").check_backward("f32")

@@ -111,6 +111,15 @@ def test_large_tiles(dynb):
     check([500, 200], 2048, 1600, 8, 0, "bf16", "none", True, False, "f32")
 
 
+@pytest.mark.parametrize("odd", [0, 1])
+def test_large_tiles_of_fp32(dynb, odd):
+    """768 tiles of 128 x 128 and more: of the outputs, of the inputs' gradients, of the weights'."""
+    pad = 4 - 3 * odd
+    check([5000, 0, 200], 40 + odd, 2440 + odd, pad, odd, "f32", "silu", True, True, "f32")
+    check([5000, 200], 2440 - odd, 40 + odd, pad, odd, "f32", "none", False, True, "f32")
+    check([700, 260], 2600 - odd, 2440 + odd, pad, odd, "f32", "none", True, False, "f32")
+
+
 def test_pitches_and_rows_of_more_than_32_bits(dynb):
     """Rows 2^22 elements apart (256 of them are 2^31 bytes), 600 of them: the last ones are 2^32 bytes from the first."""
     import torch
@@ -132,6 +141,26 @@ def test_pitches_and_rows_of_more_than_32_bits(dynb):
         hx, hw, hd = host(near), host(w), host(dout)
         assert_within(host(out), hx @ hw, stored("bf16", hx @ hw, summed(hx, hw)), "out")
         assert_within(host(dw).reshape(n, m), hx.T @ hd, summed(hx.T, hd) + EPS * np.abs(hx.T @ hd), "dw")
+
+
+def test_pitches_of_more_than_32_bits_in_fp32(dynb):
+    """Rows 2^21 + 1 elements apart (256 of them pass 2^31 bytes), 600 of them."""
+    import torch
+    rows, n, m, ld = 600, 72, 41, (1 << 21) + 1
+    g = torch.Generator("cuda").manual_seed(3)
+    x = torch.empty(rows * ld, device="cuda").view(rows, ld)[:, :n]
+    x.copy_(torch.randn(rows, n, generator=g, device="cuda"))
+    w = torch.randn(n, m, generator=g, device="cuda")
+    dout = torch.randn(rows, m, generator=g, device="cuda")
+    d = binding.linear_desc("f32", n, m, "none", "f32", ld_x=ld)
+    out, dw = torch.empty(rows, m, device="cuda"), torch.empty(n * m, device="cuda")
+    nb = max(binding.linear_workspace_bytes(d, rows), binding.linear_backward_workspace_bytes(d, [rows]))
+    binding.linear(d, rows, x, w, None, None, None, out, room(nb), nb)
+    binding.linear_backward(d, [rows], x, w, None, dout, None, dw, 0, None, 0, room(nb), nb)
+    torch.cuda.synchronize()
+    hx, hw, hd = host(x.contiguous()), host(w), host(dout)
+    assert_within(host(out), hx @ hw, stored("f32", hx @ hw, summed(hx, hw)), "out")
+    assert_within(host(dw).reshape(n, m), hx.T @ hd, summed(hx.T, hd) + EPS * np.abs(hx.T @ hd), "dw")
 
 
 def test_no_rows_and_idle_workers(dynb):
