@@ -217,7 +217,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : (ACCESS == SHIFTED
   static_assert(!TA || BM * (int)sizeof(T) >= 256, "a turned A has the wide swizzle");
   __shared__ uint4 ring[AREA / 16];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int wm = wave % WM, wn = wave / WM, l31 = lane & 31, h = lane >> 5;
+  const int wm = wave / WN, wn = wave % WN, l31 = lane & 31, h = lane >> 5;
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0];
 
   // ---- which tile
@@ -433,9 +433,29 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 8 ? 1 : (ACCESS == SHIFTED
     for (int u = 0; u < Q[1]; ++u) copy_one((NB - 1) * STAGE, u);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NP + Q[1]) : "memory");
     __syncthreads();
+    uint32_t slot = 0, fill = (NB - 1) * STAGE;
+    if (WM > 1 && i0 + wm * (BM / WM) >= i_end) {
+      // a wave without rows copies and waits alike, and leaves the matrix instructions to the others, one of which is on each SIMD (64
+      // experts of 320 rows on average, 2048 x 2048: forward 772 -> 710 us, gradients of rows 826 -> 812; 384 rows 798 -> 781, 873 -> 866)
+#pragma unroll 1
+      for (int s = s_begin; s < s_end; ++s) {
+        const uint32_t after = slot + STAGE == NB * STAGE ? 0 : slot + STAGE;
+#pragma unroll
+        for (int u = Q[1]; u < NP; ++u) copy_one(fill, u);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 2) * NP) : "memory");
+        __syncthreads();
+        next_stage();
+#pragma unroll
+        for (int u = 0; u < Q[1]; ++u) copy_one(slot, u);
+        fill = slot;
+        slot = after;
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      return;
+    }
 #pragma unroll
     for (int f = 0; f < NF; ++f) fetch_one(0, 0, f);
-    uint32_t slot = 0, fill = (NB - 1) * STAGE;
 #pragma unroll 1
     for (int s = s_begin; s < s_end; ++s) {
       const uint32_t after = slot + STAGE == NB * STAGE ? 0 : slot + STAGE;
