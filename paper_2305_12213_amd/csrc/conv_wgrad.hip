@@ -742,7 +742,7 @@ RowChunks make_row_chunks(const Segs& s, int rows) {
   ch.rows = rows;
   ch.first[0] = 0;
   for (int k = 0; k < s.K; ++k)
-    ch.first[k + 1] = ch.first[k] + (s.off[k + 1] - s.off[k] + rows - 1) / rows;
+    ch.first[k + 1] = ch.first[k] + (int)(((int64_t)s.off[k + 1] - s.off[k] + rows - 1) / rows);   // (a worker may have 2^31 - 1)
   for (int k = s.K + 1; k <= DYNB_MAX_WORKERS; ++k) ch.first[k] = ch.first[s.K];
   return ch;
 }

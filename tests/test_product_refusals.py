@@ -130,3 +130,15 @@ def test_embedding_arguments():
     refused(binding.embedding_backward, d, [4, 6], *A[:3], 6399, WS, BIG)
     for ws, n in ((None, need), (WS, need - 1), (WS + 8, need)):
         refused(binding.embedding_backward, d, [4, 6], *A[:3], 6400, ws, n)
+
+
+@pytest.mark.parametrize("dtype,n,activation", [("f32", 1, "none"), ("f32", 64, "none"), ("bf16", 1, "gelu"), ("bf16", 4096, "none")])
+def test_backward_workspace_of_the_most_rows(dtype, n, activation):
+    """About 128 chunks of rows have a sum of n each; parts of a weight's gradient are at most 16 (a row's gradient of so many
+    tiles has one); what belongs to an activation is a value per element, in rows of whole granules."""
+    for b in ([1 << 30], [2130000000], [2140000000], [(1 << 31) - 1], [(1 << 31) - 2, 1], [1 << 30, (1 << 30) - 1]):
+        K, T, size = len(b), sum(b), 2 if dtype == "bf16" else 4
+        got = binding.linear_backward_workspace_bytes(binding.linear_desc(dtype, n, n, activation=activation), b)
+        kept = T * -(-n * size // 16) * 16 if activation != "none" else 0
+        least, most = kept + 100 * n * 4, kept + (130 + K) * n * 4 + 16 * K * n * n * 4 + 64
+        assert least <= got <= most, (b, got, least, most)
