@@ -106,6 +106,12 @@ int check_workspace(const void* workspace, size_t bytes, size_t need, const char
   return DYNB_OK;
 }
 
+// A call of several products: all of them are looked at, then all are launched.
+template <class Products> int whole_call(void* stream, Products products) {
+  if (int rc = products(Target{(hipStream_t)stream, false})) return rc;
+  return products(Target{(hipStream_t)stream, true});
+}
+
 // ---- gradient of what an activation was taken of, and sums of its columns ------------------------------------------
 // dpre = dout act'(pre), and over the rows of each chunk its sums (fp32, the rows in order: four waves take every
 // fourth row each, their sums are added in turn).  Memory bounds it: 4096 x 4096 in bf16, 16 workers, 101 MB in 31 us.
@@ -191,7 +197,7 @@ int check(const dynb_linear_desc* d, const char* who) {
 
 template <typename T>
 int linear_forward(const dynb_linear_desc* d, int64_t rows, const void* x, const void* weight, const float* bias,
-                   const void* residual, void* pre, void* out, void* workspace, void* stream) {
+                   const void* residual, void* pre, void* out, void* workspace, Target to) {
   Product p = {};
   p.A[0] = p.A[1] = x;
   p.B[0] = p.B[1] = weight;
@@ -206,7 +212,7 @@ int linear_forward(const dynb_linear_desc* d, int64_t rows, const void* x, const
   const int64_t m = d->n_out;
   const LinearOut<T> ep = {bias, (const T*)residual, d->ld_residual ? d->ld_residual : m, (T*)pre, d->ld_pre ? d->ld_pre : m,
                            (T*)out, d->ld_out ? d->ld_out : m, d->activation};
-  return launch_linear<T>(p, plan.tiles, false, ep, stream);
+  return launch_linear<T>(p, plan.tiles, false, ep, to);
 }
 
 // Where the parts of a backward pass's workspace begin.
@@ -231,8 +237,7 @@ LinearBackward layout(const dynb_linear_desc* d, const Segs& s) {
 template <typename T, typename O>
 int linear_gradients(const dynb_linear_desc* d, const Segs& s, const void* x, const void* weight, const void* pre,
                      const void* dout, void* dx, void* dweight, int64_t dweight_stride, void* dbias, int64_t dbias_stride,
-                     char* workspace, void* stream) {
-  const hipStream_t st = (hipStream_t)stream;
+                     char* workspace, Target to) {
   const int64_t rows = s.off[s.K];
   const int n = d->n_in, m = d->n_out;
   const LinearBackward w = layout(d, s);
@@ -243,18 +248,19 @@ int linear_gradients(const dynb_linear_desc* d, const Segs& s, const void* x, co
   float* const sums = (float*)(workspace + w.sums);
   if (rows > 0 && (act || dbias)) {
     T* const dpre = (T*)(workspace + w.dpre);
-    hipLaunchKernelGGL(dense_grad_kernel<T>, dim3(ch.first[s.K], (unsigned)tiles_of(m, 512)), dim3(256), 0, st, g, ld_g,
-                       (const T*)pre, d->ld_pre ? d->ld_pre : m, d->activation, dpre, padded(m, d->dtype),
-                       dbias ? sums : nullptr, m, s, ch);
+    if (to.launch)
+      hipLaunchKernelGGL(dense_grad_kernel<T>, dim3(ch.first[s.K], (unsigned)tiles_of(m, 512)), dim3(256), 0, to.stream, g, ld_g,
+                         (const T*)pre, d->ld_pre ? d->ld_pre : m, d->activation, dpre, padded(m, d->dtype),
+                         dbias ? sums : nullptr, m, s, ch);
     if (act) {
       g = dpre;
       ld_g = padded(m, d->dtype);
     }
   }
-  if (dbias)
-    hipLaunchKernelGGL(chunk_sum_kernel<O>, dim3((unsigned)tiles_of(m, 256), s.K), dim3(256), 0, st, sums, m, ch, (O*)dbias,
+  if (dbias && to.launch)
+    hipLaunchKernelGGL(chunk_sum_kernel<O>, dim3((unsigned)tiles_of(m, 256), s.K), dim3(256), 0, to.stream, sums, m, ch, (O*)dbias,
                        dbias_stride);
-  if (hipGetLastError() != hipSuccess) return fail(DYNB_ERR_HIP, "linear_backward launch failed");
+  if (to.launch && hipGetLastError() != hipSuccess) return fail(DYNB_ERR_HIP, "linear_backward launch failed");
   if (dx && rows > 0) {
     Product p = {};
     p.A[0] = p.A[1] = g;
@@ -268,7 +274,7 @@ int linear_gradients(const dynb_linear_desc* d, const Segs& s, const void* x, co
     const ProductPlan plan = plan_rows(d->dtype, rows, 1, n, m, false);
     cut(p, plan, rows, workspace + w.partial);
     const LinearOut<T> ep = {nullptr, nullptr, 0, nullptr, 0, (T*)dx, d->ld_dx ? d->ld_dx : n, DYNB_ACT_NONE};
-    if (int rc = launch_linear<T>(p, plan.tiles, true, ep, stream)) return rc;
+    if (int rc = launch_linear<T>(p, plan.tiles, true, ep, to)) return rc;
   }
   if (dweight) {
     Product p = {};
@@ -284,7 +290,7 @@ int linear_gradients(const dynb_linear_desc* d, const Segs& s, const void* x, co
     const ProductPlan plan = plan_weights(d->dtype, rows, s.K, n, m, 1);
     cut(p, plan, (int64_t)s.K * n, workspace + w.partial);
     const WeightOut<O> ep = {{(O*)dweight, nullptr}, dweight_stride, 0, s.K, m, s.K, past_caches((double)sizeof(O) * s.K * n * m) && whole_lines<O>(m)};
-    return launch_weights<T, O>(p, plan.tiles, s, ep, stream);
+    return launch_weights<T, O>(p, plan.tiles, s, ep, to);
   }
   return DYNB_OK;
 }
@@ -330,7 +336,7 @@ Product by_expert(const dynb_gated_block_desc* d, const int32_t* offsets) {
 
 template <typename T>
 int gated_forward(const dynb_gated_block_desc* d, const int32_t* offsets, const void* x, const void* w_gate, const void* w_up,
-                  const void* w_down, void* gate, void* up, void* y, char* workspace, void* stream) {
+                  const void* w_down, void* gate, void* up, void* y, char* workspace, Target to) {
   const int H = d->cols, F = d->hidden;
   const int64_t ld_hidden = padded(F, d->dtype);
   T* const hidden = (T*)workspace;
@@ -346,7 +352,7 @@ int gated_forward(const dynb_gated_block_desc* d, const int32_t* offsets, const 
   ProductPlan plan = plan_up(d);
   cut(p, plan, d->rows, partial);
   const GatedOut<T> ep = {(T*)gate, (T*)up, d->ld_kept ? d->ld_kept : F, hidden, ld_hidden, d->activation};
-  if (int rc = launch_gated<T>(p, plan.tiles, ep, stream)) return rc;
+  if (int rc = launch_gated<T>(p, plan.tiles, ep, to)) return rc;
   p.A[0] = p.A[1] = hidden;
   p.B[0] = p.B[1] = w_down;
   p.lda = ld_hidden;
@@ -356,13 +362,13 @@ int gated_forward(const dynb_gated_block_desc* d, const int32_t* offsets, const 
   plan = plan_down(d);
   cut(p, plan, d->rows, partial);
   const LinearOut<T> out = {nullptr, nullptr, 0, nullptr, 0, (T*)y, d->ld_y ? d->ld_y : H, DYNB_ACT_NONE};
-  return launch_linear<T>(p, plan.tiles, false, out, stream);
+  return launch_linear<T>(p, plan.tiles, false, out, to);
 }
 
 template <typename T, typename O>
 int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offsets, const int32_t* segments, const void* x,
                     const void* w_gate, const void* w_up, const void* w_down, const void* gate, const void* up, const void* dy,
-                    void* dx, void* dw_gate, void* dw_up, void* dw_down, int64_t worker_stride, char* workspace, void* stream) {
+                    void* dx, void* dw_gate, void* dw_up, void* dw_down, int64_t worker_stride, char* workspace, Target to) {
   const int H = d->cols, F = d->hidden;
   const int64_t ld_hidden = padded(F, d->dtype), ld_dy = d->ld_dy ? d->ld_dy : H, each = hidden_bytes(d);
   T *const dgate = (T*)workspace, *const dup = (T*)(workspace + each), *const hidden = (T*)(workspace + 2 * each);
@@ -378,7 +384,7 @@ int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offset
     const ProductPlan plan = plan_dhidden(d);
     cut(p, plan, d->rows, partial);
     const GatedGrad<T> ep = {(const T*)gate, (const T*)up, d->ld_kept ? d->ld_kept : F, dgate, dup, hidden, ld_hidden, d->activation};
-    if (int rc = launch_gated_grad<T>(p, plan.tiles, ep, stream)) return rc;
+    if (int rc = launch_gated_grad<T>(p, plan.tiles, ep, to)) return rc;
   }
   if (dx && d->rows > 0) {
     Product p = by_expert(d, offsets);
@@ -394,7 +400,7 @@ int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offset
     const ProductPlan plan = plan_dx(d);
     cut(p, plan, d->rows, partial);
     const LinearOut<T> ep = {nullptr, nullptr, 0, nullptr, 0, (T*)dx, d->ld_dx ? d->ld_dx : H, DYNB_ACT_NONE};
-    if (int rc = launch_linear<T>(p, plan.tiles, true, ep, stream)) return rc;
+    if (int rc = launch_linear<T>(p, plan.tiles, true, ep, to)) return rc;
   }
   if (!dw_gate) return DYNB_OK;
   Product p = by_expert(d, offsets);
@@ -418,7 +424,7 @@ int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offset
   const int64_t matrix = (int64_t)H * F;
   const bool past = past_caches((double)sizeof(O) * p.groups * matrix);
   const WeightOut<O> ep = {{(O*)dw_gate, (O*)dw_up}, worker_stride, matrix, K, F, p.groups, past && whole_lines<O>(F)};
-  if (int rc = launch_weights<T, O>(p, plan.tiles, whole, ep, stream)) return rc;
+  if (int rc = launch_weights<T, O>(p, plan.tiles, whole, ep, to)) return rc;
   p.A[0] = p.A[1] = hidden;
   p.B[0] = p.B[1] = dy;
   p.lda = ld_hidden;
@@ -429,7 +435,7 @@ int gated_gradients(const dynb_gated_block_desc* d, int K, const int32_t* offset
   plan = plan_ddown(d, K);
   cut(p, plan, (int64_t)p.groups * F, partial);
   const WeightOut<O> down = {{(O*)dw_down, nullptr}, worker_stride, matrix, K, H, p.groups, past && whole_lines<O>(H)};
-  return launch_weights<T, O>(p, plan.tiles, whole, down, stream);
+  return launch_weights<T, O>(p, plan.tiles, whole, down, to);
 }
 
 }  // namespace
@@ -454,8 +460,9 @@ extern "C" int dynb_linear(const dynb_linear_desc* d, int64_t rows, const void* 
   if (int rc = check_workspace(workspace, workspace_bytes, dynb_linear_workspace_bytes(d, rows), "linear")) return rc;
   const double n = d->n_in, m = d->n_out;
   Timed t(KC_DENSE, stream, 2.0 * rows * n * m, size * (n * m + rows * (n + m * (1 + !!residual + !!pre))));
-  return d->dtype == DYNB_F32 ? linear_forward<float>(d, rows, x, weight, bias, residual, pre, out, workspace, stream)
-                              : linear_forward<bf16>(d, rows, x, weight, bias, residual, pre, out, workspace, stream);
+  const Target to = {(hipStream_t)stream, true};
+  return d->dtype == DYNB_F32 ? linear_forward<float>(d, rows, x, weight, bias, residual, pre, out, workspace, to)
+                              : linear_forward<bf16>(d, rows, x, weight, bias, residual, pre, out, workspace, to);
 }
 
 extern "C" size_t dynb_linear_backward_workspace_bytes(const dynb_linear_desc* d, const int32_t* b, int32_t K) {
@@ -484,8 +491,10 @@ extern "C" int dynb_linear_backward(const dynb_linear_desc* d, const int32_t* b,
   Timed t(KC_DENSE, stream, 2.0 * rows * n * m * (!!dx + !!dweight),
           size * (n * m + rows * (2 * n + 2 * m)) + gsize * K * n * m);
   auto call = [&](auto type, auto grad) {
-    return linear_gradients<decltype(type), decltype(grad)>(d, s, x, weight, pre, dout, dx, dweight, dweight_stride, dbias,
-                                                            dbias_stride, (char*)workspace, stream);
+    return whole_call(stream, [&](Target to) {
+      return linear_gradients<decltype(type), decltype(grad)>(d, s, x, weight, pre, dout, dx, dweight, dweight_stride, dbias,
+                                                              dbias_stride, (char*)workspace, to);
+    });
   };
   if (d->dtype == DYNB_F32) return call(float(), float());
   return d->grad_dtype == DYNB_F32 ? call(bf16(), float()) : call(bf16(), bf16());
@@ -512,9 +521,11 @@ extern "C" int dynb_gated_block(const dynb_gated_block_desc* d, const int32_t* o
   if (int rc = check_workspace(workspace, workspace_bytes, dynb_gated_block_workspace_bytes(d), "gated_block")) return rc;
   const double n = d->cols, m = d->hidden, rows = (double)d->rows;
   Timed t(KC_DENSE, stream, 6.0 * rows * n * m, size * (3.0 * std::min<double>(d->n_experts, rows) * n * m + rows * (2 * n + (gate ? 2 * m : 0))));
-  return d->dtype == DYNB_F32
-             ? gated_forward<float>(d, offsets, x, w_gate, w_up, w_down, gate, up, y, (char*)workspace, stream)
-             : gated_forward<bf16>(d, offsets, x, w_gate, w_up, w_down, gate, up, y, (char*)workspace, stream);
+  return whole_call(stream, [&](Target to) {
+    return d->dtype == DYNB_F32
+               ? gated_forward<float>(d, offsets, x, w_gate, w_up, w_down, gate, up, y, (char*)workspace, to)
+               : gated_forward<bf16>(d, offsets, x, w_gate, w_up, w_down, gate, up, y, (char*)workspace, to);
+  });
 }
 
 extern "C" size_t dynb_gated_block_backward_workspace_bytes(const dynb_gated_block_desc* d, int32_t K) {
@@ -552,8 +563,10 @@ extern "C" int dynb_gated_block_backward(const dynb_gated_block_desc* d, int32_t
   Timed t(KC_DENSE, stream, rows * n * m * (2.0 + (dx ? 4.0 : 0.0) + (dw_gate ? 6.0 : 0.0)),
           size * (3.0 * d->n_experts * n * m + rows * (3 * n + 2 * m)) + (dw_gate ? 3.0 * gsize * K * d->n_experts * n * m : 0.0));
   auto call = [&](auto type, auto grad) {
-    return gated_gradients<decltype(type), decltype(grad)>(d, K, offsets, segments, x, w_gate, w_up, w_down, gate, up, dy, dx,
-                                                           dw_gate, dw_up, dw_down, worker_stride, (char*)workspace, stream);
+    return whole_call(stream, [&](Target to) {
+      return gated_gradients<decltype(type), decltype(grad)>(d, K, offsets, segments, x, w_gate, w_up, w_down, gate, up, dy, dx,
+                                                             dw_gate, dw_up, dw_down, worker_stride, (char*)workspace, to);
+    });
   };
   if (d->dtype == DYNB_F32) return call(float(), float());
   return d->grad_dtype == DYNB_F32 ? call(bf16(), float()) : call(bf16(), bf16());

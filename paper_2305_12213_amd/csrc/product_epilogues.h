@@ -190,13 +190,19 @@ struct ProductPlan {
   int splits;
 };
 
-// (instantiated once per type and form: products_*.hip.  T: type of the rows and weights, O: of the weights' gradients)
-template <typename T> int launch_linear(const Product& p, Tiles tiles, bool turned, const LinearOut<T>& ep, void* stream);
-template <typename T> int launch_gated(const Product& p, Tiles tiles, const GatedOut<T>& ep, void* stream);
-template <typename T> int launch_gated_grad(const Product& p, Tiles tiles, const GatedGrad<T>& ep, void* stream);
-template <typename T, typename O>
-int launch_weights(const Product& p, Tiles tiles, const Segs& s, const WeightOut<O>& ep, void* stream);
+// Where a product goes.  launch false: it is only asked whether one launch holds it, so that a call of several products is refused
+// before the first of them has written anything.
+struct Target {
+  hipStream_t stream;
+  bool launch;
+};
 
+// (instantiated once per type and form: products_*.hip.  T: type of the rows and weights, O: of the weights' gradients)
+template <typename T> int launch_linear(const Product& p, Tiles tiles, bool turned, const LinearOut<T>& ep, Target to);
+template <typename T> int launch_gated(const Product& p, Tiles tiles, const GatedOut<T>& ep, Target to);
+template <typename T> int launch_gated_grad(const Product& p, Tiles tiles, const GatedGrad<T>& ep, Target to);
+template <typename T, typename O>
+int launch_weights(const Product& p, Tiles tiles, const Segs& s, const WeightOut<O>& ep, Target to);
 
 namespace {
 
@@ -213,7 +219,7 @@ template <typename T> bool direct_ok(const Product& p, int form) {
 }
 
 template <typename T, int FORM, bool DUAL, int BM, int BN, int WM, int WN, int DEPTH, int NB, int SOON, Access ACCESS, class Ep>
-int launch_tiles(const Product& p, const Segs& s, const Ep& ep, hipStream_t st) {
+int launch_tiles(const Product& p, const Segs& s, const Ep& ep, Target to) {
   constexpr int BNS = DUAL ? BN / 2 : BN;
   const int64_t tiles_j = (p.N + BNS - 1) / BNS;
   int64_t units;
@@ -224,32 +230,32 @@ int launch_tiles(const Product& p, const Segs& s, const Ep& ep, hipStream_t st) 
     units = (p.offsets ? p.rows / BM + (p.rows < p.groups ? p.rows : p.groups) : (p.rows + BM - 1) / BM) * tiles_j;
   }
   if (units * p.splits > INT32_MAX / (WM * WN * 64)) return fail(DYNB_ERR_UNSUPPORTED, "a product of more than 2^22 tiles");
+  if (!to.launch) return DYNB_OK;
   hipLaunchKernelGGL((product_kernel<T, FORM, DUAL, BM, BN, WM, WN, DEPTH, NB, SOON, ACCESS, Ep>), dim3((unsigned)units, p.splits),
-                     dim3(WM * WN * 64), 0, st, p, s, ep);
+                     dim3(WM * WN * 64), 0, to.stream, p, s, ep);
   if (p.splits > 1) {
     const int64_t n = p.partial_rows * ((p.N + 7) / 8);
-    hipLaunchKernelGGL((joined_kernel<FORM, DUAL, Ep>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, p, ep);
+    hipLaunchKernelGGL((joined_kernel<FORM, DUAL, Ep>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, to.stream, p, ep);
   }
   return hipGetLastError() == hipSuccess ? DYNB_OK : fail(DYNB_ERR_HIP, "launch of a product failed");
 }
 
 template <typename T, int FORM, bool DUAL, class Ep>
-int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* stream) {
-  const hipStream_t st = (hipStream_t)stream;
+int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, Target to) {
   const bool direct = direct_ok<T>(p, FORM);
   // (rows of less than a granule: nothing to shift)
   const bool singly = (FORM == WEIGHTS ? p.M : p.K) < 16 / (int)sizeof(T) || (FORM != ROWS_NT && p.N < 16 / (int)sizeof(T));
   if constexpr (FORM != WEIGHTS) {
     constexpr int WN = DUAL ? 2 : 4;
-    if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SINGLY>(p, s, ep, st);
+    if (singly) return launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SINGLY>(p, s, ep, to);
     if constexpr (!DUAL)
       // (one token through 4096 x 14336: 24.7 us; on tiles of 128 columns, in four parts and joined, 27.4)
-      if (tiles == TILES_32X64 && direct) return launch_tiles<T, FORM, DUAL, 32, 64, 1, 2, 8, 6, 2, DIRECT>(p, s, ep, st);
+      if (tiles == TILES_32X64 && direct) return launch_tiles<T, FORM, DUAL, 32, 64, 1, 2, 8, 6, 2, DIRECT>(p, s, ep, to);
     if (tiles == TILES_32 || tiles == TILES_32X64)
-      return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, DIRECT>(p, s, ep, st)
-                    : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SHIFTED>(p, s, ep, st);
+      return direct ? launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, DIRECT>(p, s, ep, to)
+                    : launch_tiles<T, FORM, DUAL, 32, 128, 1, WN, 8, 4, 2, SHIFTED>(p, s, ep, to);
   } else {
-    if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, st);
+    if (singly) return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 2, 4, SINGLY>(p, s, ep, to);
   }
   // fp32 with few tiles: smaller ones, of which several share a compute unit and leave less of it idle at the end (gradients of
   // 1531 tokens, 3 of 11 experts, 777 x 301: 294 -> 252 us).  Odd widths: single copies, of shorter stages for gradients of weights,
@@ -259,25 +265,25 @@ int launch_as(const Product& p, Tiles tiles, const Segs& s, const Ep& ep, void* 
     constexpr int DEPTH = FORM == WEIGHTS ? 4 : 8;
     if (tiles == TILES_64) {
       constexpr int BN = DUAL ? 128 : 64;
-      if (direct) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, st);
-      if (copies_ok<T>(p)) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, DEPTH, 2, 4, SINGLES>(p, s, ep, st);
+      if (direct) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, to);
+      if (copies_ok<T>(p)) return launch_tiles<T, FORM, DUAL, 64, BN, 2, 2, DEPTH, 2, 4, SINGLES>(p, s, ep, to);
     }
-    if (!direct && copies_ok<T>(p)) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, DEPTH, 2, 4, SINGLES>(p, s, ep, st);
+    if (!direct && copies_ok<T>(p)) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, DEPTH, 2, 4, SINGLES>(p, s, ep, to);
   }
   // (gradients of weights end after a few stages: more and smaller workgroups on a compute unit hide more of their ends; 77 groups of
   // 48 rows, 777 x 301, shifted granules of fp32, two weights: 119 -> 104 us)
   constexpr bool SHORT = FORM == WEIGHTS, F32 = sizeof(T) == 4;
-  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT || F32 ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, st);
+  if (!direct) return launch_tiles<T, FORM, DUAL, 128, 128, SHORT || F32 ? 2 : 4, 2, SHORT ? 4 : 8, 2, 4, SHIFTED>(p, s, ep, to);
   // fp32: two workgroups of four waves on a compute unit, one's matrix instructions in the other's barriers (4096^3 1120 us with one
   // of eight waves and a ring of four stages, 1057)
-  if constexpr (F32) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, st);
+  if constexpr (F32) return launch_tiles<T, FORM, DUAL, 128, 128, 2, 2, 8, 2, 4, DIRECT>(p, s, ep, to);
   else if (tiles == TILES_256) {
     // (results that come with more bytes than operations: two workgroups to a compute unit, one computes while the other stores.
     // 16384 rows of 8 experts, 2048 x 2048: gradients of hidden 281 us on 256 x 256 tiles, 267; other rows 4 to 20 % slower)
-    if constexpr (FORM == WEIGHTS || Ep::HEAVY) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, st);
-    else return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 8, 2, 4, DIRECT>(p, s, ep, st);
+    if constexpr (FORM == WEIGHTS || Ep::HEAVY) return launch_tiles<T, FORM, DUAL, 256, 128, 2, 2, 4, 3, 4, DIRECT>(p, s, ep, to);
+    else return launch_tiles<T, FORM, DUAL, 256, 256, 2, 4, 8, 2, 4, DIRECT>(p, s, ep, to);
   } else {
-    return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 4, 2, DIRECT>(p, s, ep, st);
+    return launch_tiles<T, FORM, DUAL, 128, 128, 4, 2, 8, 4, 2, DIRECT>(p, s, ep, to);
   }
 }
 

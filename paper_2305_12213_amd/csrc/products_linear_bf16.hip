@@ -3,9 +3,9 @@
 
 namespace dynb {
 
-template <> int launch_linear<bf16>(const Product& p, Tiles tiles, bool turned, const LinearOut<bf16>& ep, void* stream) {
-  return turned ? launch_as<bf16, ROWS_NT, false>(p, tiles, Segs{}, ep, stream)
-                : launch_as<bf16, ROWS_NN, false>(p, tiles, Segs{}, ep, stream);
+template <> int launch_linear<bf16>(const Product& p, Tiles tiles, bool turned, const LinearOut<bf16>& ep, Target to) {
+  return turned ? launch_as<bf16, ROWS_NT, false>(p, tiles, Segs{}, ep, to)
+                : launch_as<bf16, ROWS_NN, false>(p, tiles, Segs{}, ep, to);
 }
 
 }  // namespace dynb

@@ -142,3 +142,24 @@ def test_backward_workspace_of_the_most_rows(dtype, n, activation):
         kept = T * -(-n * size // 16) * 16 if activation != "none" else 0
         least, most = kept + 100 * n * 4, kept + (130 + K) * n * 4 + 16 * K * n * n * 4 + 64
         assert least <= got <= most, (b, got, least, most)
+
+
+UNSUPPORTED = -2
+
+
+def too_large(call, *args):
+    with pytest.raises(binding.DynbError) as e:
+        call(*args, stream=0)
+    assert e.value.code == UNSUPPORTED and str(e.value)
+
+
+def test_all_products_of_a_call_are_looked_at_before_its_first_launch():
+    """A later product of more tiles than one launch holds: the call is refused as a whole (without a GPU a launch would be
+    another error)."""
+    d = binding.linear_desc("bf16", 64, 4, "none", "f32")           # dx by tiles of 32 rows, 2^24 of them
+    too_large(binding.linear, d, 1 << 30, *A[:6], WS, BIG)
+    too_large(binding.linear_backward, d, [1 << 29], A[0], A[1], None, A[2], A[3], A[4], 256, A[5], 4, WS, BIG)
+    too_large(binding.linear_backward, d, [1 << 29], A[0], A[1], None, A[2], A[3], None, 0, A[5], 4, WS, BIG)
+    d = binding.gated_block_desc("bf16", 4096, 64, 1, 1 << 28)      # 2^20 tiles of hidden, 2^24 of y and dx
+    too_large(binding.gated_block, d, None, *A[:7], WS, BIG)
+    too_large(binding.gated_block_backward, d, 1, None, None, *A[:11], BIG, WS, BIG)
