@@ -434,7 +434,7 @@ int dynb_adamw_read_states(dynb_adamw* h, void* const* out1, void* const* out2, 
  * element's size.  Gradients of weights and biases are per worker, fp32 or (grad_dtype) of the rows' type.
  * Results are the same from run to run.  Calls may be captured into a graph; a workspace is used by one call at a time.
  * DYNB_ERR_UNSUPPORTED: more work than one launch holds (a product of 2^22 tiles, the smallest of which have 32 x 64 results;
- * 2^34 looked-up values, gradients of tables of 2^37 values).  A refused call has launched nothing.
+ * looked-up rows of more than 2^31 - 256 pieces of 8 columns).  A refused call has launched nothing.
  * Values past the rows, or between them, are neither read nor written. */
 enum { DYNB_ACT_NONE = 0, DYNB_ACT_RELU = 1, DYNB_ACT_SILU = 2, DYNB_ACT_GELU = 3 };
 /*   RELU max(v, 0);  SILU v / (1 + e^-v);  GELU v (1 + erf(v / sqrt 2)) / 2;  a NaN stays one */

@@ -279,8 +279,9 @@ __device__ inline int64_t keys_below(const int32_t* keys, int64_t n, int key) {
 }
 
 // p.per neighbouring rows of the gradients to a wave: MOST_PER, which share a search, or fewer where waves are few (the
-// first rows of a vocabulary are often those of its most frequent tokens).
-constexpr int MOST_PER = 8, ENOUGH_WAVES = 8192;
+// first rows of a vocabulary are often those of its most frequent tokens), or more where a launch of MOST_GRID workgroups would not
+// hold the table otherwise.
+constexpr int MOST_PER = 8, ENOUGH_WAVES = 8192, MOST_GRID = 1 << 23;
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
   const int lane = threadIdx.x & 63, all = p.workers * p.vocabulary;
@@ -387,7 +388,7 @@ extern "C" int dynb_embedding(const dynb_embedding_desc* d, const int32_t* ids, 
   if (!ids || !table || !out) return fail(DYNB_ERR_BADARG, "embedding: null pointer");
   const int granules = (d->cols + GRANULE - 1) / GRANULE;
   const int64_t blocks = (d->tokens * granules + 255) / 256;
-  if (blocks > INT32_MAX / 256) return fail(DYNB_ERR_UNSUPPORTED, "embedding: more than 2^31 granules of rows");
+  if (blocks > INT32_MAX / 256) return fail(DYNB_ERR_UNSUPPORTED, "embedding: rows of more than 2^31 - 256 pieces of 8 columns");
   const int64_t lt = d->ld_table ? d->ld_table : d->cols, lo = d->ld_out ? d->ld_out : d->cols;
   Timed t(KC_EMBEDDING, stream, (double)d->tokens * d->cols, 2.0 * size * d->tokens * d->cols);
   if (d->dtype == DYNB_F32)
@@ -420,10 +421,10 @@ extern "C" int dynb_embedding_backward(const dynb_embedding_desc* d, const int32
   const Parts w = parts_of(d);
   if (w.end && (!workspace || workspace_bytes < (size_t)w.end || off_by(workspace, 16)))
     return fail(DYNB_ERR_BADARG, "embedding_backward: workspace is null, too small or not 16-byte aligned");
-  const int per = (int)std::max<int64_t>(1, std::min<int64_t>(MOST_PER, K * d->vocabulary / ENOUGH_WAVES));
+  const int64_t table_rows = K * d->vocabulary, at_once = (int64_t)4 * (MOST_GRID / ((d->cols + SPAN - 1) / SPAN));
+  const int per = (int)std::max({(int64_t)1, std::min<int64_t>(MOST_PER, table_rows / ENOUGH_WAVES), (table_rows + at_once - 1) / at_once});
   TableGrad grad = {nullptr, nullptr, dout, d->ld_dout ? d->ld_dout : d->cols, (float*)((char*)workspace + w.sums), dtable,
                        worker_stride, d->tokens, (int)d->vocabulary, d->cols, K, per, d->scale};
-  if (table_grad_blocks(grad) > 1 << 23) return fail(DYNB_ERR_UNSUPPORTED, "embedding_backward: more than 2^37 elements");
   const hipStream_t st = (hipStream_t)stream;
   Timed t(KC_EMBEDDING, stream, (double)d->tokens * d->cols,
           4.0 * K * d->vocabulary * d->cols + (double)size * d->tokens * d->cols);

@@ -7,7 +7,7 @@ import pytest
 
 from oracle import products as op
 from paper_2305_12213_amd import binding
-from tests.operators_harness import EPS, STORED, assert_within, device_rows, empty_rows, host, untouched
+from tests.operators_harness import EPS, STORED, assert_within, device_rows, empty_rows, host, torch_type, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +155,28 @@ def test_replays(dynb):
         step()
         torch.cuda.synchronize()
         assert torch.equal(a, g) and torch.equal(c, out)
+
+
+
+def test_narrow_tables_of_many_rows(dynb):
+    """64 workers, 2^23 tokens of one column: 2^29 rows of gradients."""
+    import torch
+    K, V, T = 64, 1 << 23, 6000
+    g = torch.Generator("cuda").manual_seed(5)
+    ids = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    ids[:4] = torch.tensor([0, V - 1, V, -1], device="cuda")
+    ids[-2:] = V - 1
+    dout = torch.randn(T, 1, generator=g, device="cuda")
+    b = [T // K] * (K - 1)
+    b.append(T - sum(b))
+    d = binding.embedding_desc("f32", 1, V, T)
+    out = torch.full((K * V,), float("nan"), device="cuda")
+    n = binding.embedding_backward_workspace_bytes(d, K)
+    binding.embedding_backward(d, b, ids, dout, out, V, torch.empty(n + 16, device="cuda", dtype=torch.uint8), n)
+    worker = torch.arange(K, device="cuda").repeat_interleave(torch.tensor(b, device="cuda"))
+    live = (ids >= 0) & (ids < V)
+    key = (worker * V + ids.long())[live]
+    want = torch.zeros(K * V, device="cuda", dtype=torch.float64).index_add_(0, key, dout[live, 0].double())
+    size = torch.zeros_like(want).index_add_(0, key, dout[live, 0].double().abs())
+    most = int(torch.bincount(key - key.min()).max())
+    assert bool(((out.double() - want).abs() <= (most + 2) * EPS * size).all())

@@ -163,3 +163,9 @@ def test_all_products_of_a_call_are_looked_at_before_its_first_launch():
     d = binding.gated_block_desc("bf16", 4096, 64, 1, 1 << 28)      # 2^20 tiles of hidden, 2^24 of y and dx
     too_large(binding.gated_block, d, None, *A[:7], WS, BIG)
     too_large(binding.gated_block_backward, d, 1, None, None, *A[:11], BIG, WS, BIG)
+
+
+def test_more_looked_up_rows_than_one_launch_holds():
+    """Pieces of 8 columns: 2^31 - 256 at most."""
+    for tokens, cols in (((1 << 31) - 255, 1), ((1 << 31) - 1, 8), (1 << 30, 9), (1 << 29, 25)):
+        too_large(binding.embedding, binding.embedding_desc("bf16", cols, 10, tokens), *A[:3])
