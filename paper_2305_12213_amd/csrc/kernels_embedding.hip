@@ -159,21 +159,40 @@ __global__ __launch_bounds__(THREADS) void digit_place_kernel(SortPass p, Segs s
 }
 
 // ---- the sums ----------------------------------------------------------------------------------------------------
-// A token that appears often (a padding token may be all of them) would be one wave's long chain: the sorted tokens are cut
-// into chunks of 16, and one whose tokens are all the same is summed beforehand.  A run is then its first tokens up to a
-// chunk's end, its whole chunks, and the rest.  A lane has four neighbouring columns twice, 256 apart, so that every access of a
+// A token that appears often (a padding token may be all of them) would be one wave's long chain, and one fp32 sum whose
+// roundings add up: the sorted tokens are cut into chunks of 16, and one whose tokens are all the same is summed beforehand; while
+// a level has more than MOST_SUMS sums, 64 neighbouring ones of the same token are summed to one of the next.  A run is then its first
+// tokens up to a chunk's end, its whole chunks up to the end of a sum of the next level and so on, and what is left of each level on
+// the way back: every term goes through less than 1500 additions, whatever the run's length (2^22 equal rows in bf16 were off by 4e-3
+// in one sum of their chunks).  131072 tokens of 32000 x 512, half of them one token: 127 us, 529 with chunks alone.  A level costs
+// 2 to 9 us, which is why 1024 sums go without (16384 tokens of 32000 x 2048: 74 us, 83 with one; all of them one token: 166, 93).
+// A lane has four neighbouring columns twice, 256 apart, so that every access of a
 // wave is one stretch of memory; the numbers of 64 tokens are loaded at once and AHEAD of their rows are asked for together.
 constexpr int CHUNK = 16, QUAD = 4, HALF = 64 * QUAD, SPAN = 2 * HALF;   // SPAN: columns of a wave
-constexpr int AHEAD = 8;
+constexpr int AHEAD = 8, EACH = 64, MOST_SUMS = 1024;
+// Sums of a level over n tokens, each over 16 * 64^level of them, and levels.  All sums are in one array, level by level.
+__host__ __device__ constexpr int level_bits(int level) { return 4 + 6 * level; }
+__host__ __device__ inline int64_t sums_of_level(int64_t n, int level) { return n >> level_bits(level); }
+static_assert(1 << level_bits(0) == CHUNK && 1 << level_bits(1) == CHUNK * EACH, "bits of a level");
+int levels_of(int64_t n) {
+  int levels = 1;
+  while (sums_of_level(n, levels - 1) > MOST_SUMS) ++levels;
+  return levels;
+}
+int64_t sums_of(int64_t n) {
+  int64_t sums = 0;
+  for (int l = 0; l < levels_of(n); ++l) sums += sums_of_level(n, l);
+  return sums;
+}
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 struct TableGrad {
   const int32_t* keys; const int32_t* tokens;    // sorted
   const void* dout; int64_t ld_dout;
-  float* chunk_sums;                             // [chunks][cols]
+  float* sums;                                   // [levels: sums][cols]
   float* dtable; int64_t worker_stride;
   int64_t n; int vocabulary;
-  int cols, workers, per;
+  int cols, workers, per, levels;
   float scale;
 };
 
@@ -257,10 +276,35 @@ __global__ __launch_bounds__(256) void chunk_rows_kernel(TableGrad p) {
     if (key != p.keys[first + CHUNK - 1] || key >= p.workers * p.vocabulary) continue;
     f32x4_any s[2] = {};
     add_rows<T>(p, first, first + CHUNK, c, s);
-    float* const to = p.chunk_sums + chunk * p.cols + c;
+    float* const to = p.sums + chunk * p.cols + c;
     store_quad<false>(to, p.cols - c, s[0]);
     store_quad<false>(to + HALF, p.cols - c - HALF, s[1]);
   }
+}
+
+// s += the sums [from, to) of all levels' (from and to the same in the whole wave)
+__device__ inline void add_sums(const TableGrad& p, int64_t from, int64_t to, int c, f32x4_any (&s)[2]) {
+  const int n0 = p.cols - c, n1 = n0 - HALF;
+#pragma unroll 8
+  for (int64_t q = from; q < to; ++q) {
+    const float* const at = p.sums + q * p.cols + c;
+    s[0] += values(load_quad(at, n0));
+    s[1] += values(load_quad(at + HALF, n1));
+  }
+}
+
+// The sums of a level from those of the one below, which begin at `below`, where all their tokens are the same.
+__global__ __launch_bounds__(256) void level_kernel(TableGrad p, int level, int64_t below) {
+  const int c = blockIdx.y * SPAN + (threadIdx.x & 63) * QUAD, bits = level_bits(level);
+  const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (i >= sums_of_level(p.n, level)) return;
+  const int key = p.keys[i << bits];
+  if (key != p.keys[((i + 1) << bits) - 1] || key >= p.workers * p.vocabulary) return;
+  f32x4_any s[2] = {};
+  add_sums(p, below + i * EACH, below + (i + 1) * EACH, c, s);
+  float* const to = p.sums + (below + sums_of_level(p.n, level - 1) + i) * p.cols + c;
+  store_quad<false>(to, p.cols - c, s[0]);
+  store_quad<false>(to + HALF, p.cols - c - HALF, s[1]);
 }
 
 // Sorted tokens with keys below `key` (the whole wave takes part): 64 places at a time.
@@ -306,16 +350,25 @@ __global__ __launch_bounds__(256) void table_grad_kernel(TableGrad p) {
     }
     f32x4_any s[2] = {};
     if (begin < end) {
-      const int64_t chunk = (begin + CHUNK - 1) / CHUNK, last = end / CHUNK;
-      if (chunk < last) {
-        add_rows<T>(p, begin, chunk * CHUNK, c, s);
-#pragma unroll 8
-        for (int64_t q = chunk; q < last; ++q) {
-          const float* const from = p.chunk_sums + q * p.cols + c;
-          s[0] += values(load_quad(from, n0));
-          s[1] += values(load_quad(from + HALF, n1));
+      int64_t sum = (begin + CHUNK - 1) / CHUNK;                    // the next sum of the level, of those in the run
+      if (sum < end / CHUNK) {
+        add_rows<T>(p, begin, sum * CHUNK, c, s);
+        int level = 0;
+        int64_t base = 0;                                           // where the level's sums begin
+        for (; level + 1 < p.levels; ++level) {
+          const int64_t above = (sum + EACH - 1) / EACH;
+          if (above >= end >> level_bits(level + 1)) break;
+          add_sums(p, base + sum, base + above * EACH, c, s);
+          base += sums_of_level(p.n, level);
+          sum = above;
         }
-        add_rows<T>(p, last * CHUNK, end, c, s);
+        for (;;) {
+          add_sums(p, base + sum, base + (end >> level_bits(level)), c, s);
+          if (level == 0) break;
+          sum = (end >> level_bits(level)) * EACH;
+          base -= sums_of_level(p.n, --level);
+        }
+        add_rows<T>(p, end / CHUNK * CHUNK, end, c, s);
       } else {
         add_rows<T>(p, begin, end, c, s);
       }
@@ -346,7 +399,7 @@ int check(const dynb_embedding_desc* d, const char* who) {
 
 int64_t sort_blocks(int64_t n) { return n <= ALONE ? 1 : std::min<int64_t>((n + THREADS * 2 - 1) / (THREADS * 2), MOST_BLOCKS); }
 
-// Where the parts of the workspace begin: keys and tokens twice, counts, the chunks' sums.
+// Where the parts of the workspace begin: keys and tokens twice, counts, the sums.
 struct Parts {
   int64_t keys, tokens, counts, sums, end;       // (keys, tokens: the second ones follow the first)
 };
@@ -357,7 +410,7 @@ Parts parts_of(const dynb_embedding_desc* d) {
   w.tokens = 2 * each;
   w.counts = 4 * each;
   w.sums = w.counts + (B > 1 ? B * DIGITS * 4 : 0);
-  w.end = w.sums + round_up(d->tokens / CHUNK * d->cols * 4, 16);
+  w.end = w.sums + round_up(sums_of(d->tokens) * d->cols * 4, 16);
   return w;
 }
 
@@ -369,6 +422,9 @@ template <typename T>
 void launch_table_grad(const TableGrad& p, hipStream_t st) {
   if (p.n >= CHUNK)
     hipLaunchKernelGGL(chunk_rows_kernel<T>, dim3((unsigned)std::min<int64_t>((p.n / CHUNK + 3) / 4, 1 << 20), (p.cols + SPAN - 1) / SPAN), dim3(256), 0, st, p);
+  int64_t below = 0;
+  for (int l = 1; l < p.levels; below += sums_of_level(p.n, l - 1), ++l)
+    hipLaunchKernelGGL(level_kernel, dim3((unsigned)((sums_of_level(p.n, l) + 3) / 4), (p.cols + SPAN - 1) / SPAN), dim3(256), 0, st, p, l, below);
   const dim3 grid((unsigned)table_grad_blocks(p));
   if (past_caches(4.0 * p.workers * p.vocabulary * p.cols)) hipLaunchKernelGGL((table_grad_kernel<T, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((table_grad_kernel<T, false>), grid, dim3(256), 0, st, p);
@@ -424,7 +480,7 @@ extern "C" int dynb_embedding_backward(const dynb_embedding_desc* d, const int32
   const int64_t table_rows = K * d->vocabulary, at_once = (int64_t)4 * (MOST_GRID / ((d->cols + SPAN - 1) / SPAN));
   const int per = (int)std::max({(int64_t)1, std::min<int64_t>(MOST_PER, table_rows / ENOUGH_WAVES), (table_rows + at_once - 1) / at_once});
   TableGrad grad = {nullptr, nullptr, dout, d->ld_dout ? d->ld_dout : d->cols, (float*)((char*)workspace + w.sums), dtable,
-                       worker_stride, d->tokens, (int)d->vocabulary, d->cols, K, per, d->scale};
+                       worker_stride, d->tokens, (int)d->vocabulary, d->cols, K, per, levels_of(d->tokens), d->scale};
   const hipStream_t st = (hipStream_t)stream;
   Timed t(KC_EMBEDDING, stream, (double)d->tokens * d->cols,
           4.0 * K * d->vocabulary * d->cols + (double)size * d->tokens * d->cols);

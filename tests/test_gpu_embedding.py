@@ -180,3 +180,28 @@ def test_narrow_tables_of_many_rows(dynb):
     size = torch.zeros_like(want).index_add_(0, key, dout[live, 0].double().abs())
     most = int(torch.bincount(key - key.min()).max())
     assert bool(((out.double() - want).abs() <= (most + 2) * EPS * size).all())
+
+
+@pytest.mark.parametrize("dtype,tokens", [("f32", 1 << 20), ("bf16", 1 << 22), ("f32", (1 << 18) + 777)])
+def test_one_id_in_a_long_batch(dynb, dtype, tokens):
+    """Equal rows, whose roundings all point the same way.  A row is in a sum of 16, then in sums of 64 while more than 1024 are
+    left, then in one sum of what is left with at most 63 of each shorter kind and 15 rows on either side: at most
+    16 + 64 n + 2 (63 n + 15) + 1024 + 2 roundings with n levels of 64, each of 2^-24."""
+    import torch
+    V, H, b = 5, 24, [3, tokens - 3]
+    ids = torch.full((tokens,), 3, device="cuda", dtype=torch.int32)
+    ids[:40] = torch.arange(40, device="cuda") % 5
+    ids[-1] = 0
+    dout = torch.full((tokens, H), 1.1, device="cuda").to(torch_type(dtype)) * (1 + torch.arange(H, device="cuda") % 8 / 8).to(torch_type(dtype))
+    got = gradient(b, ids, dout, V, H, 0, 1.0, dtype)
+    here = ids[3:] == 3
+    want = float(here.sum()) * dout[0].double()
+    levels, left = 0, tokens // 16
+    while left > 1024:
+        levels, left = levels + 1, left // 64
+    most = 16 + 64 * levels + 2 * (63 * levels + 15) + 1024 + 2
+    assert bool(((got[1, 3].double() - want).abs() <= most * EPS * want).all()), float(((got[1, 3].double() - want).abs() / want).max())
+    for v in (0, 1, 2, 4):
+        many = float((ids[3:] == v).sum())
+        assert bool(((got[1, v].double() - many * dout[0].double()).abs() <= 40 * EPS * many * dout[0].double()).all())
+    assert torch.equal(got, gradient(b, ids, dout, V, H, 0, 1.0, dtype))
