@@ -437,7 +437,8 @@ int dynb_adamw_read_states(dynb_adamw* h, void* const* out1, void* const* out2, 
  * looked-up rows of more than 2^31 - 256 pieces of 8 columns).  A refused call has launched nothing.
  * Values past the rows, or between them, are neither read nor written. */
 enum { DYNB_ACT_NONE = 0, DYNB_ACT_RELU = 1, DYNB_ACT_SILU = 2, DYNB_ACT_GELU = 3 };
-/*   RELU max(v, 0);  SILU v / (1 + e^-v);  GELU v (1 + erf(v / sqrt 2)) / 2;  a NaN stays one */
+/*   RELU max(v, 0);  SILU v / (1 + e^-v);  GELU v (1 + erf(v / sqrt 2)) / 2;  a NaN stays one;
+ *   at +infinity they are +infinity and their slopes 1, at -infinity both are 0 */
 
 /* A dense layer with what surrounds it.  n_in, n_out: 1 .. 2^20. */
 typedef struct {

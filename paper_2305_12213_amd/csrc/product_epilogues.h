@@ -12,11 +12,15 @@ namespace dynb {
 // act(v) and its derivative, in fp32.
 //   silu  v p, p = 1 / (1 + e^-v);             p (1 + v (1 - p))
 //   gelu  v P, P = (1 + erf(v / sqrt 2)) / 2;  P + v e^(-v^2 / 2) / sqrt(2 pi)
-// (where v's magnitude is beyond an exponential's range p and P are 0 or 1, and the products with 0 vanish.)  Values that are
+// (where v's magnitude is beyond an exponential's range p and P are 0 or 1, and the products with 0 vanish; an infinite v is the
+// largest finite one in them, which gives the limits, and a NaN stays one by p and P.)  Values that are
 // rounded to 16 bits take the hardware's exponential and reciprocal and erf by Abramowitz and Stegun 7.1.26
 // (off by 1.5e-7 at most), which shares its exponential with gelu's derivative.
 template <typename T> struct Curve {
   static constexpr bool SHORT = sizeof(T) == 2;
+  static constexpr float MOST = 3.40282347e38f;
+  static __device__ float finite(float v) { return __builtin_amdgcn_fmed3f(v, -MOST, MOST); }
+  static __device__ float bounded_below(float v) { return __builtin_amdgcn_fmed3f(v, -MOST, __builtin_inff()); }
   static __device__ float power(float v) { return SHORT ? __expf(v) : expf(v); }
   static __device__ float inverse(float v) { return SHORT ? __builtin_amdgcn_rcpf(v) : 1.f / v; }
   // P, and e^(-v^2 / 2)
@@ -38,14 +42,14 @@ template <typename T> struct Curve {
         return v < 0.f ? 0.f : v;            // (a NaN stays one)
       case DYNB_ACT_SILU: {
         const float p = inverse(1.f + power(-v));
-        slope = p * (1.f + v * (1.f - p));
-        return v * p;
+        slope = p * (1.f + finite(v) * (1.f - p));
+        return bounded_below(v) * p;
       }
       case DYNB_ACT_GELU: {
         float bell;
         const float p = normal(v, bell);
-        slope = p + v * bell * 0.39894228f;
-        return v * p;
+        slope = p + finite(v) * bell * 0.39894228f;
+        return bounded_below(v) * p;
       }
       default:
         slope = 1.f;

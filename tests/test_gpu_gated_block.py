@@ -359,3 +359,21 @@ def test_infinities_and_nan_stay_where_they_are(dynb):
     clean = torch.ones(c.R, dtype=torch.bool, device="cuda")
     clean[7] = clean[50] = False
     assert torch.equal(y[clean], y0[clean]) and bool(y[50].isnan().all()) and not bool(y[7].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_infinite_gates(dynb, act, dtype):
+    """Gradients where gates are infinite (one that was finite may have been rounded to infinity): the slopes are 1 and 0."""
+    import torch
+    c = Case([[6], [5]], 64, 48, dtype, act)
+    gate, up, dy = c.rows(48, 1.0), c.rows(48, 1.0), c.rows(64, 0.1)
+    gate[:6], gate[6:] = float("inf"), float("-inf")
+    dx, dg, du, dd = c.backward(gate, up, dy)
+    torch.cuda.synchronize()
+    x, hu, hdy, wd = host(c.x)[:6], host(up)[:6], host(dy)[:6], host(c.wd)[0]
+    dgate = (hdy @ wd.T) * hu
+    off = stored(dtype, dgate, summed(hdy, wd.T) * np.abs(hu) + 3 * EPS * np.abs(dgate))
+    assert_within(host(dg[0, 0]), x.T @ dgate, stored("f32", x.T @ dgate, summed(x.T, dgate) + 1.01 * (np.abs(x.T) @ off)), "dw_gate")
+    for t in (dx[6:], dg[0, 1], du[0, 1], dd[0, 1]):
+        assert not bool(t.isnan().any()) and not bool(t.any())

@@ -221,3 +221,37 @@ def test_replays_on_another_stream(dynb):
         assert all(torch.equal(a, b) for a, b in zip((pre, out, dx, dw, db), want))
         step()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinite_pre_activations(dynb, dtype):
+    """Activations and slopes at the infinities are their limits there, so that a pre-activation which has become infinite by its
+    rounding gives no NaN.  A product of zeros with an infinite bias is that bias."""
+    import torch
+    m, rows = 24, 40
+    z = torch.zeros(m, device="cuda")
+    z[::3], z[1::3] = float("inf"), float("-inf")
+    t = torch_type(dtype)
+    x, w = torch.zeros(rows, 16, device="cuda", dtype=t), torch.zeros(16, m, device="cuda", dtype=t)
+    dout = torch.randn(rows, m, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(t)
+    one = torch.eye(m, device="cuda", dtype=t)
+    for act, middle in (("none", 1.0), ("relu", 0.0), ("silu", 0.5), ("gelu", 0.5)):
+        d = binding.linear_desc(dtype, 16, m, act)
+        out, pre, dx = (torch.empty(rows, m, device="cuda", dtype=t) for _ in range(3))
+        n = binding.linear_workspace_bytes(d, rows)
+        binding.linear(d, rows, x, w, z, None, pre, out, room(n), n)
+        assert torch.equal(pre, z.to(t).expand(rows, m))
+        want = z.clone()
+        if act != "none":
+            want[1::3] = 0.0
+        assert torch.equal(out, want.to(t).expand(rows, m)), act
+        # through a unit weight dx is dz, whose slopes are 1, 0 and the middle one (all exact)
+        d = binding.linear_desc(dtype, m, m, act)
+        n = binding.linear_backward_workspace_bytes(d, [rows])
+        db = torch.empty(m, device="cuda")
+        binding.linear_backward(d, [rows], dx, one, pre, dout, dx, None, 0, db, m, room(n), n)
+        slope = torch.ones(m, device="cuda")
+        if act != "none":
+            slope[1::3], slope[2::3] = 0.0, middle
+        assert torch.equal(dx, dout * slope.to(t)), act
+        assert bool(db.isfinite().all()), act
