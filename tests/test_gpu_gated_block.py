@@ -377,3 +377,56 @@ def test_infinite_gates(dynb, act, dtype):
     assert_within(host(dg[0, 0]), x.T @ dgate, stored("f32", x.T @ dgate, summed(x.T, dgate) + 1.01 * (np.abs(x.T) @ off)), "dw_gate")
     for t in (dx[6:], dg[0, 1], du[0, 1], dd[0, 1]):
         assert not bool(t.isnan().any()) and not bool(t.any())
+
+
+class Far(Case):
+    """Three experts' rows in a call of 600, at experts 0, 512 and 599: weights of 2048 x 2048, so that the last ones are 2^31 elements
+    and 2^32 bytes from the first.  The three weights are views of one allocation, an expert apart, whose other experts hold NaN."""
+
+    AT, EXPERTS = (0, 512, 599), 600
+
+    def __init__(self):
+        import torch
+        super().__init__([[3], [2], [4]], 2048, 2048, "bf16", behind=1)
+        size, E = self.H * self.F, self.EXPERTS
+        all_of_them = torch.full(((E + 2) * size,), float("nan"), device="cuda", dtype=torch.bfloat16)
+        self.far = [all_of_them[i * size:(i + E) * size].view(E, self.H, self.F) for i in range(3)]
+        for view, w in zip(self.far, (self.wg, self.wu, self.wd)):
+            for i, e in enumerate(self.AT):
+                view[e] = w[i]
+        counts = np.zeros(E, np.int64)
+        counts[list(self.AT)] = [3, 2, 4]
+        self.far_offsets = self.dev(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32))
+
+    def far_desc(self, grad):
+        return binding.gated_block_desc("bf16", self.H, self.F, self.EXPERTS, self.R, activation=self.act, grad=grad)
+
+    def forward(self, keep=True):
+        d = self.far_desc("bf16")
+        y, gate, up = (empty_rows(self.R, 2048, "bf16") for _ in range(3))
+        if not keep:
+            gate = up = None
+        n = binding.gated_block_workspace_bytes(d)
+        ws = room(n)
+        binding.gated_block(d, self.far_offsets, self.x, *self.far, gate, up, y, ws, n)
+        assert marked_after(ws, n)
+        return y, gate, up
+
+    def backward(self, gate, up, dy, grad="f32", K=None):
+        import torch
+        d = self.far_desc(grad)
+        dx = empty_rows(self.R, self.H, "bf16")
+        g = [torch.full((self.EXPERTS, 2048, 2048), float("nan"), device="cuda", dtype=torch_type(grad)) for _ in range(3)]
+        n = binding.gated_block_backward_workspace_bytes(d, 1)
+        ws = room(n)
+        binding.gated_block_backward(d, 1, self.far_offsets, None, self.x, *self.far, gate, up, dy, dx, *g, 0, ws, n)
+        assert marked_after(ws, n)
+        assert not any(bool(t[e].any()) or bool(t[e].isnan().any()) for t in g for e in (1, 2, 511, 513, 598))
+        return (dx,) + tuple(t[list(self.AT)][None] for t in g)
+
+
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+def test_every_value_of_experts_beyond_32_bits(dynb, grad):
+    c = Far()
+    c.check_forward()
+    c.check_backward(grad)
