@@ -429,8 +429,8 @@ int dynb_adamw_read_states(dynb_adamw* h, void* const* out1, void* const* out2, 
 
 /* ---- products around routed experts: dense layers, gated feed-forward blocks, embeddings ---------------------
  * Rows, weights and pitches as in the operators above: dtype is the type of all rows and weights, products and sums are
- * fp32 and each stored value is rounded once (nearest-even); what a backward pass keeps between two of its products (the
- * gradients of pre-activations, and `hidden`) is stored in dtype.  Weights are dense, in C order, at any multiple of their
+ * fp32 and each stored value is rounded once (nearest-even); what a call keeps between two of its products (`hidden` in the
+ * forward pass and in its gradients, the gradients of pre-activations) is stored in dtype.  Weights are dense, in C order, at any multiple of their
  * element's size.  Gradients of weights and biases are per worker, fp32 or (grad_dtype) of the rows' type.
  * Results are the same from run to run.  Calls may be captured into a graph; a workspace is used by one call at a time.
  * DYNB_ERR_UNSUPPORTED: more work than one launch holds (a product of 2^22 tiles, the smallest of which have 32 x 64 results;

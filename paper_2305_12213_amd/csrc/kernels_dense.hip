@@ -19,7 +19,10 @@ int64_t row_tiles_of(int64_t rows, int groups, int size) {
 bool whole_granules(int dtype, int64_t n) { return n % (dtype == DYNB_F32 ? 4 : 8) == 0; }
 // Into how many parts a reduction of `stages` is divided.  A workgroup takes about its share of the stages; where two share a
 // compute unit (paired) they take twice as long, one alone there 1.5 times.  `worth`: what a part costs to be written and
-// joined, in halves of a stage.
+// joined, in halves of a stage.  Measured in bf16 with 64 to 512 rows, 1024 to 4096 columns: reductions of 4096 13 to 32 us, in one
+// part 29 to 38; of 16384 19 to 91 us, in one part 87 to 151; of 1024, 16 stages, one part is taken, 14 to 16 us, where half of
+// `worth` would take two and 11 to 15 us (20 for 512 rows of 4096 columns), and be up to 7 % slower at 16384; twice `worth` is
+// up to 19 % slower at 4096 and 16384.  Worst of what was measured: gradients of 1024 x 2048 from 2048 rows, 45 us, in one part 38.
 int parts(int64_t tiles, int64_t stages, bool paired, int worth) {
   int best = 1;
   int64_t least = 0;
@@ -35,7 +38,8 @@ int parts(int64_t tiles, int64_t stages, bool paired, int worth) {
 }
 
 // The same for fp32 on 64 x 64 tiles (64 x 128 for two products): matrix instructions bound several workgroups on a compute unit
-// together, fewer than three leave them waiting.
+// together, fewer than three leave them waiting.  (128 to 1500 rows, reductions of 1024 and 4096, 512 and 2048 columns: 13 to 204 us,
+// in one part 1 to 4.7 times as long; the cost of a part halved 0 to 7 % slower, doubled 0 to 31 %)
 int parts_of_small(int64_t tiles, int64_t stages) {
   int best = 1;
   int64_t least = 0;
@@ -57,7 +61,10 @@ ProductPlan plan_rows(int dtype, int64_t rows, int groups, int N, int64_t reduct
   const int half = dual ? 2 : 1;
   const int64_t stages = tiles_of(reduction, dtype == DYNB_F32 ? 32 : 64);
   const int64_t each = rows / std::min<int64_t>(groups, std::max<int64_t>(rows, 1));
-  if (each <= 48) {                        // (memory bounds these: parts only until every compute unit has work)
+  // (memory bounds these: parts only until every compute unit has work.  192 narrow tiles and more are not divided: one row of 2048,
+  // 4096 and 8192 through 12800 columns 12.7, 24.6 and 47.6 us, in two parts 14.6, 25.8 and 47.6, through 16384 9 to 14 % in favour;
+  // with 40 rows it goes either way, 2048, 4096 and 8192 through 6144 columns 13.6, 21.5 and 39.8 us, in two parts 12.4, 16.7 and 37.4)
+  if (each <= 48) {
     const int64_t row_tiles = row_tiles_of(rows, groups, 32);
     const bool narrow = !dual && row_tiles * tiles_of(N, 128) < 256;
     const int64_t tiles = row_tiles * tiles_of(N, narrow ? 64 : 128 / half);
@@ -114,7 +121,8 @@ template <class Products> int whole_call(void* stream, Products products) {
 
 // ---- gradient of what an activation was taken of, and sums of its columns ------------------------------------------
 // dpre = dout act'(pre), and over the rows of each chunk its sums (fp32, the rows in order: four waves take every
-// fourth row each, their sums are added in turn).  Memory bounds it: 4096 x 4096 in bf16, 16 workers, 101 MB in 31 us.
+// fourth row each, their sums are added in turn).  4096 x 4096 in bf16, 16 workers: 101 MB in 31 us, 3.2 TB/s, 0.64 of a large copy's
+// rate: chunks are of 32 rows, so that a wave asks twice for four rows and ends.
 constexpr int TOGETHER = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void dense_grad_kernel(const T* dout, int64_t ld_dout, const T* pre, int64_t ld_pre, int act,

@@ -18,9 +18,10 @@
 // What bounds it.  Long reductions in bf16: the matrix instructions at the clock that they leave (8192^3 915 us, 1200 TFLOP/s; the clock
 // falls to 1.8 GHz).  Short ones (gradients of weights from a few hundred rows): the stores, which all workgroups come to
 // at about the same time -- 16 workers of 256 rows, 4096 x 4096 in bf16: 220 us, of which 115 are products and 140 would be the stores
-// alone.  Workgroups that stay and copy the next tile's stages while they store were measured too: 8 % slower where
+// alone.  Workgroups that stay and copy the next tile's stages while they store were measured too, on tiles of 256 x 256 with eight
+// waves of 128 sums a lane: 8 % slower where
 // tiles are many (registers run out around the longer code, and wait counters are in order, so that the next stage waits for the
-// stores all the same), equal where reductions are short.  fp32: the matrix instructions, 4096^3 982 to 1060 us, 130 to 140 TFLOP/s.
+// stores all the same), equal where reductions are short; not with smaller tiles to a wave.  fp32: the matrix instructions, 4096^3 982 to 1060 us, 130 to 140 TFLOP/s.
 // Few rows: the weights' way from memory (64 experts of 3 x 2048 x 1024 in bf16, two rows each: 130 us, 6.2 TB/s).
 #ifndef DYNB_TILE_PRODUCT_H
 #define DYNB_TILE_PRODUCT_H
